@@ -21,7 +21,7 @@
  *     HIP error code (thread-local).
  *   - Return value: NOVA_OK (0) or a negative NOVA_E* code; nothing throws or aborts.
  *   - dtype selects the storage format of x, w, U, V, y: NOVA_F16 (IEEE binary16) or
- *     NOVA_F32.  Arithmetic: transforms in binary32 (filter transform in binary64),
+ *     NOVA_F32; the calls behind a convolution stack (4-bit layers, log probabilities) take NOVA_BF16 too.  Arithmetic: transforms in binary32 (filter transform in binary64),
  *     channel contraction on the matrix cores with binary32 accumulation.
  */
 #ifndef NOVA_H
@@ -50,7 +50,7 @@ enum {
     NOVA_ENOMEM = -8        /* host allocation failed */
 };
 
-enum { NOVA_F32 = 0, NOVA_F16 = 1 };
+enum { NOVA_F32 = 0, NOVA_F16 = 1, NOVA_BF16 = 2 };   /* NOVA_BF16 (bfloat16): the nova_q4_* and nova_logprobs* calls only */
 enum { NOVA_MATRIX_A = 0, NOVA_MATRIX_BT = 1, NOVA_MATRIX_G = 2 };
 
 /* flags of nova_winograd_conv2d / nova_output_transform / nova_contract */
@@ -357,6 +357,93 @@ int nova_contract_output_fused(const nova_transforms *t, const void *U, const vo
 /* out = maxpool2x2(max(in, 0)), stride 2, floor; in [N][C][H][W] -> out [N][C][H/2][W/2] (device).
  * The step between the blocks of a VGG-style stack. */
 int nova_relu_maxpool2x2(const void *in, void *out, int N, int C, int H, int W, int dtype, void *stream);
+
+/* ------------------------------------------------------------------ layers with 4-bit weights */
+
+/*
+ * A fully connected layer whose weights are integer codes of 4 bits with one scale per group of consecutive inputs:
+ *     W[n][k] = c[n][k] * s[n][k / group],   c in [-8, 7],   group 32, 64 or 128 (the last group of a row may be shorter),
+ * the scales stored in the layer's dtype (NOVA_F32, NOVA_F16, NOVA_BF16), as x, y and the bias are.
+ * N: outputs, K: inputs, each 1 .. 2^24; M: rows (images, tokens), 0 .. 2^31 - 1; none needs to be a multiple of anything.
+ *
+ * Codes and scales are laid out once per weight set, for one direction:
+ *   NOVA_Q4_FORWARD   nova_q4_linear:           R = N rows, reduction over C = K
+ *   NOVA_Q4_BACKWARD  nova_q4_linear_backward:  R = K rows, reduction over C = N
+ * as [ceil(R/16)][ceil(C/128)] panels of 1024 bytes: 64 lanes of four 32-bit words, word w of lane 16 b + i holding the eight codes
+ * of row 16 r + i at positions 128 c + 32 w + 8 b + v of the reduction, v = 0 .. 7, in bits 4 (v / 2) + 16 (v % 2) and the three above, two's
+ * complement; then the scales: forward [ceil(R/16)][ceil(C/128) * 128 / group][16], backward [ceil(K/group)][ceil(N/128) * 128]; padding is zero.
+ *
+ * nova_q4_bytes: size of a layout (0 for invalid arguments).
+ * nova_q4_quantize: from weights w [N][K] (device, dtype): s = max|w| / 7 of the group, formed in binary32 and rounded to dtype, c = w / s
+ *   (binary32) rounded to nearest, ties to even, and kept within [-8, 7].  A group of zeros, or one whose scale rounds to zero, gets s = 0 and
+ *   codes 0; a group that holds an infinity or a NaN comes back as NaN.
+ * nova_q4_pack: from codes [N][K] (device, one byte each; kept within [-8, 7]) and scales [N][ceil(K/group)] (device, dtype).
+ * nova_q4_unpack: the inverse, from a layout of either direction; scales may be NULL.
+ * Wq: device, 16-byte aligned, at least nova_q4_bytes; fully overwritten by the first two (padding included).
+ * Errors: NOVA_EINVAL; NOVA_ENOSPC if Wq_bytes is less than the layout's size; NOVA_EHIP.
+ */
+enum { NOVA_Q4_FORWARD = 0, NOVA_Q4_BACKWARD = 1 };
+size_t nova_q4_bytes(int N, int K, int group, int dtype, int direction);
+int nova_q4_quantize(const void *w, int N, int K, int group, int dtype, int direction, void *Wq, size_t Wq_bytes, void *stream);
+int nova_q4_pack(const int8_t *codes, const void *scales, int N, int K, int group, int dtype, int direction, void *Wq, size_t Wq_bytes, void *stream);
+int nova_q4_unpack(const void *Wq, size_t Wq_bytes, int N, int K, int group, int dtype, int direction, int8_t *codes, void *scales, void *stream);
+
+/*
+ * y[m][n] = sum_k x[m][k] W[n][k] + bias[n], with NOVA_FLAG_RELU then max(., 0) (NaN stays NaN).  x: device [M][K] with ldx elements from
+ * row to row (ldx >= K, or 0 for one row that stands for all; with one row it does not matter), y: device [M][N] with ldy >= N; rows need no alignment beyond the element's.
+ * bias: device [N] or NULL.  Wq: NOVA_Q4_FORWARD layout of dtype.
+ * Products and sums in binary32: the codes are exact on the matrix unit, a group's sum is scaled in binary32, and y is rounded once.  Sums are formed in a
+ * fixed order: equal calls give equal bits.
+ *
+ * nova_q4_linear_backward: dx[m][k] = sum_n d[m][n] W[n][k], d = dy, or with y (the layer's result after its ReLU) d = y > 0 ? dy : 0; y may
+ * be NULL.  The weights of a stored layer are constants: there is no gradient of codes, scales or bias.  dy: [M][N], y: [M][N], dx: [M][K] with
+ * their row lengths; Wq: NOVA_Q4_BACKWARD layout.  d * s is formed in binary32 and enters the matrix unit in two pieces of 8 bits of mantissa
+ * (three for NOVA_F32), so it is rounded to 16 (24) bits; sums in binary32.
+ *
+ * workspace: device, 16-byte aligned, at least nova_q4_linear_workspace_bytes(.. direction) bytes (it may be 0, and the pointer then NULL);
+ * nothing in it has to be zero and nothing survives.  Outputs must not overlap any input or the workspace.
+ * Errors: NOVA_EINVAL, NOVA_ENOSPC (Wq_bytes or workspace_bytes too small), NOVA_EHIP.
+ */
+size_t nova_q4_linear_workspace_bytes(int M, int N, int K, int group, int dtype, int direction);
+int nova_q4_linear(const void *x, int64_t ldx, const void *Wq, size_t Wq_bytes, const void *bias, void *y, int64_t ldy, int M, int N, int K,
+                   int group, int dtype, int flags, void *workspace, size_t workspace_bytes, void *stream);
+int nova_q4_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, const void *Wq, size_t Wq_bytes, void *dx, int64_t lddx,
+                            int M, int N, int K, int group, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------ log probabilities */
+
+/*
+ * Log probabilities of given tokens (classes), entropy and the most probable alternatives, one row of logits x [rows][V] at a time:
+ *     M = max x_v,  L = ln sum_v exp(scale (x_v - M))  over the allowed entries,   ln p_v = scale (x_v - M) - L.
+ * logits: device, dtype, `stride` elements from row to row (>= V); scale: finite and > 0 (the inverse of a temperature).
+ * mask: device bytes, nonzero = allowed, [rows][V] with mask_stride >= V, or one row for all with mask_stride 0; NULL: all allowed.  What a
+ * masked entry holds does not matter (NaN and infinities included).
+ * targets: device int64 [rows] or NULL.  Outputs (device; any but stats may be NULL; top_logprobs and top_ids only with top = 0):
+ *   logprob [rows]     ln p of the target; -infinity for a masked one; 0 for a negative target ("none given"); NaN for a target >= V
+ *   entropy [rows]     - sum p ln p
+ *   stats [rows][2]    M and L (nova_logprobs_backward takes them; scale M + L is the log of the sum of exponentials)
+ *   top_logprobs, top_ids (int64) [rows][top]: the `top` (0 .. 64) largest allowed logits in falling order, equal ones by rising index; entries of
+ *                      probability zero (-infinity) are no alternatives; places left over hold -infinity and -1
+ * A row that allows nothing (or holds -infinity only): M = L = logprob = -infinity, entropy 0.  A row with a NaN or +infinity among its allowed
+ * entries: stats, logprob, entropy and top_logprobs are NaN (a negative target keeps its 0); top_ids still rank, NaN before everything.
+ * All sums are binary32; equal calls give equal bits.
+ *
+ * nova_logprobs_backward: the gradient of a logprob + h entropy,
+ *     dlogits_v = scale ( a ([v = target] - p_v) - h p_v (ln p_v + entropy) ),   0 where masked, p_v = exp(scale (x_v - M) - L) from stats;
+ * a = g_logprob [rows] (NULL: 0; needs targets), h = g_entropy [rows] (NULL: 0; needs entropy).  A negative target adds nothing for a; a target >= V
+ * makes the row NaN.  A row that allows nothing has gradient 0, a masked target only the terms of the others' p.  dlogits: device, dtype, dstride >= V;
+ * it may be logits itself (same pointer and stride); otherwise it must not overlap an input.
+ *
+ * workspace: device, 16-byte aligned, at least nova_logprobs_workspace_bytes bytes (it may be 0, and the pointer then NULL).
+ * rows 0 .. 2^31 - 1, V 1 .. 2^31 - 1.  Errors: NOVA_EINVAL, NOVA_ENOSPC, NOVA_EHIP.
+ */
+size_t nova_logprobs_workspace_bytes(int rows, int V, int top, int dtype);
+int nova_logprobs(const void *logits, int64_t stride, const int64_t *targets, const uint8_t *mask, int64_t mask_stride, int rows, int V, float scale,
+                  int top, int dtype, float *logprob, float *entropy, float *stats, float *top_logprobs, int64_t *top_ids, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int nova_logprobs_backward(const void *logits, int64_t stride, const float *stats, const int64_t *targets, const float *g_logprob,
+                           const float *entropy, const float *g_entropy, const uint8_t *mask, int64_t mask_stride, int rows, int V, float scale,
+                           int dtype, void *dlogits, int64_t dstride, void *stream);
 
 /* ------------------------------------------------------------------ misc */
 const char *nova_strerror(int code);

@@ -1,5 +1,6 @@
 // The device-facing entry points of libnova: argument checks, tensor geometry, the slab loop of
 // nova_winograd_conv2d.  All device work is done by the launchers in the .hip files.
+#include <cmath>
 #include <cstring>
 
 #include "internal.hpp"
@@ -413,6 +414,132 @@ extern "C" int nova_relu_maxpool2x2(const void *in, void *out, int N, int C, int
 {
     if (!in || !out || !dims_ok(N, C, H, W, 1) || !dtype_ok(dtype)) return NOVA_EINVAL;
     return hip_result(launch_relu_maxpool2x2(in, out, N, C, H, W, dtype, stream));
+}
+
+// ---- layers with 4-bit weights ----
+
+static bool any_dtype_ok(int dtype) { return dtype == NOVA_F32 || dtype == NOVA_F16 || dtype == NOVA_BF16; }
+
+static bool q4_ok(int N, int K, int group, int dtype, int direction)
+{
+    return N >= 1 && K >= 1 && N <= (1 << 24) && K <= (1 << 24) && (group == 32 || group == 64 || group == 128) && any_dtype_ok(dtype) &&
+           (direction == NOVA_Q4_FORWARD || direction == NOVA_Q4_BACKWARD);
+}
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+static size_t q4_layout_bytes(const Q4Layout &q, int dtype)
+{
+    return q.code_bytes + ((q.scale_count * dtype_size(dtype) + 15) & ~(size_t)15);
+}
+
+extern "C" size_t nova_q4_bytes(int N, int K, int group, int dtype, int direction)
+{
+    if (!q4_ok(N, K, group, dtype, direction)) return 0;
+    return q4_layout_bytes(make_q4_layout(N, K, group, direction), dtype);
+}
+
+extern "C" int nova_q4_quantize(const void *w, int N, int K, int group, int dtype, int direction, void *Wq, size_t Wq_bytes, void *stream)
+{
+    if (!w || !Wq || !q4_ok(N, K, group, dtype, direction) || !aligned16(Wq)) return NOVA_EINVAL;
+    const Q4Layout q = make_q4_layout(N, K, group, direction);
+    if (Wq_bytes < q4_layout_bytes(q, dtype)) return NOVA_ENOSPC;
+    return hip_result(launch_q4_quantize(w, q, dtype, Wq, stream));
+}
+
+extern "C" int nova_q4_pack(const int8_t *codes, const void *scales, int N, int K, int group, int dtype, int direction, void *Wq, size_t Wq_bytes,
+                            void *stream)
+{
+    if (!codes || !scales || !Wq || !q4_ok(N, K, group, dtype, direction) || !aligned16(Wq)) return NOVA_EINVAL;
+    const Q4Layout q = make_q4_layout(N, K, group, direction);
+    if (Wq_bytes < q4_layout_bytes(q, dtype)) return NOVA_ENOSPC;
+    return hip_result(launch_q4_pack(codes, scales, q, dtype, Wq, stream));
+}
+
+extern "C" int nova_q4_unpack(const void *Wq, size_t Wq_bytes, int N, int K, int group, int dtype, int direction, int8_t *codes, void *scales,
+                              void *stream)
+{
+    if (!Wq || !codes || !q4_ok(N, K, group, dtype, direction) || !aligned16(Wq)) return NOVA_EINVAL;
+    const Q4Layout q = make_q4_layout(N, K, group, direction);
+    if (Wq_bytes < q4_layout_bytes(q, dtype)) return NOVA_ENOSPC;
+    return hip_result(launch_q4_unpack(Wq, q, dtype, codes, scales, stream));
+}
+
+extern "C" size_t nova_q4_linear_workspace_bytes(int M, int N, int K, int group, int dtype, int direction)
+{
+    if (M < 0 || !q4_ok(N, K, group, dtype, direction)) return 0;
+    return q4_linear_workspace(M, make_q4_layout(N, K, group, direction), dtype);
+}
+
+// rows of `width` elements that are read: ld 0 stands for one row
+static bool read_rows_ok(const void *p, int64_t ld, int rows, int width) { return p && (ld >= width || ld == 0 || rows == 1); }
+static bool write_rows_ok(const void *p, int64_t ld, int rows, int width) { return p && (ld >= width || rows == 1); }
+
+extern "C" int nova_q4_linear(const void *x, int64_t ldx, const void *Wq, size_t Wq_bytes, const void *bias, void *y, int64_t ldy, int M, int N, int K,
+                              int group, int dtype, int flags, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (M < 0 || !q4_ok(N, K, group, dtype, NOVA_Q4_FORWARD) || (flags & ~NOVA_FLAG_RELU) || !Wq || !aligned16(Wq)) return NOVA_EINVAL;
+    const Q4Layout q = make_q4_layout(N, K, group, NOVA_Q4_FORWARD);
+    if (Wq_bytes < q4_layout_bytes(q, dtype)) return NOVA_ENOSPC;
+    if (M == 0) return NOVA_OK;
+    if (!read_rows_ok(x, ldx, M, K) || !write_rows_ok(y, ldy, M, N)) return NOVA_EINVAL;
+    const size_t need = q4_linear_workspace(M, q, dtype);
+    if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
+    if (workspace_bytes < need) return NOVA_ENOSPC;
+    return hip_result(launch_q4_linear(x, ldx, Wq, bias, y, ldy, M, q, dtype, flags, workspace, stream));
+}
+
+extern "C" int nova_q4_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, const void *Wq, size_t Wq_bytes, void *dx,
+                                       int64_t lddx, int M, int N, int K, int group, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (M < 0 || !q4_ok(N, K, group, dtype, NOVA_Q4_BACKWARD) || !Wq || !aligned16(Wq)) return NOVA_EINVAL;
+    const Q4Layout q = make_q4_layout(N, K, group, NOVA_Q4_BACKWARD);
+    if (Wq_bytes < q4_layout_bytes(q, dtype)) return NOVA_ENOSPC;
+    if (M == 0) return NOVA_OK;
+    if (!read_rows_ok(dy, lddy, M, N) || (y && !read_rows_ok(y, ldy, M, N)) || !write_rows_ok(dx, lddx, M, K)) return NOVA_EINVAL;
+    const size_t need = q4_linear_workspace(M, q, dtype);
+    if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
+    if (workspace_bytes < need) return NOVA_ENOSPC;
+    return hip_result(launch_q4_linear_backward(dy, lddy, y, ldy, Wq, dx, lddx, M, q, dtype, workspace, stream));
+}
+
+// ---- log probabilities ----
+
+static bool logprobs_ok(int rows, int V, int top, int dtype) { return rows >= 0 && V >= 1 && top >= 0 && top <= 64 && any_dtype_ok(dtype); }
+
+extern "C" size_t nova_logprobs_workspace_bytes(int rows, int V, int top, int dtype)
+{
+    if (!logprobs_ok(rows, V, top, dtype)) return 0;
+    return logprobs_workspace(rows, V, top, dtype);
+}
+
+extern "C" int nova_logprobs(const void *logits, int64_t stride, const int64_t *targets, const uint8_t *mask, int64_t mask_stride, int rows, int V,
+                             float scale, int top, int dtype, float *logprob, float *entropy, float *stats, float *top_logprobs, int64_t *top_ids,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!logprobs_ok(rows, V, top, dtype) || !std::isfinite(scale) || !(scale > 0.0f) || (logprob && !targets)) return NOVA_EINVAL;
+    if (rows == 0) return NOVA_OK;
+    if (!read_rows_ok(logits, stride, rows, V) || (mask && !read_rows_ok(mask, mask_stride, rows, V)) || !stats) return NOVA_EINVAL;
+    if (top > 0 && (!top_logprobs || !top_ids)) return NOVA_EINVAL;
+    const size_t need = logprobs_workspace(rows, V, top, dtype);
+    if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
+    if (workspace_bytes < need) return NOVA_ENOSPC;
+    const LogprobsArgs a = {logits, stride, targets, mask, mask_stride, rows, V, scale, top, logprob, entropy, stats, top_logprobs, top_ids};
+    return hip_result(launch_logprobs(a, dtype, workspace, stream));
+}
+
+extern "C" int nova_logprobs_backward(const void *logits, int64_t stride, const float *stats, const int64_t *targets, const float *g_logprob,
+                                      const float *entropy, const float *g_entropy, const uint8_t *mask, int64_t mask_stride, int rows, int V,
+                                      float scale, int dtype, void *dlogits, int64_t dstride, void *stream)
+{
+    if (!logprobs_ok(rows, V, 0, dtype) || !std::isfinite(scale) || !(scale > 0.0f) || (g_logprob && !targets) || (g_entropy && !entropy))
+        return NOVA_EINVAL;
+    if (rows == 0) return NOVA_OK;
+    if (!read_rows_ok(logits, stride, rows, V) || !stats || (mask && !read_rows_ok(mask, mask_stride, rows, V)) ||
+        !write_rows_ok(dlogits, dstride, rows, V))
+        return NOVA_EINVAL;
+    const LogprobsBackwardArgs a = {logits, stride, stats, targets, g_logprob, entropy, g_entropy, mask, mask_stride, rows, V, scale, dlogits, dstride};
+    return hip_result(launch_logprobs_backward(a, dtype, stream));
 }
 
 extern "C" const char *nova_strerror(int code)

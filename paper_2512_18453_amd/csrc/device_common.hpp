@@ -10,11 +10,14 @@
 namespace nova {
 
 typedef _Float16 f16;
+typedef __bf16 bf16;
 
 // storage <-> binary32; the binary16 conversion rounds to nearest even, keeps sub-normals and
 // overflows to infinity (v_cvt_f16_f32).
 __device__ __forceinline__ float load_f32(const float *p) { return *p; }
 __device__ __forceinline__ float load_f32(const f16 *p) { return (float)*p; }
+__device__ __forceinline__ float load_f32(const bf16 *p) { return (float)*p; }
+__device__ __forceinline__ void store_from_f32(bf16 *p, float v) { *p = (bf16)v; }
 __device__ __forceinline__ void store_from_f32(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_from_f32(f16 *p, float v) { *p = (f16)v; }
 

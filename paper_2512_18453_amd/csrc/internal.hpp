@@ -74,7 +74,33 @@ inline Geometry make_geometry(int N, int C, int H, int W, int K, int m, int r)
     return g;
 }
 
-inline size_t dtype_size(int dtype) { return dtype == NOVA_F16 ? 2 : 4; }
+inline size_t dtype_size(int dtype) { return dtype == NOVA_F32 ? 4 : 2; }
+
+// A layer of 4-bit weights as it is laid out for one direction (nova_q4_pack in nova.h): `rows` results of one input row, each a sum over `reduction`.
+constexpr int kQ4Rows = 16, kQ4Chunk = 128, kQ4PanelBytes = 1024;
+struct Q4Layout {
+    int N, K, group, backward;
+    int rows, reduction;                       // N and K forward, K and N backward
+    int row_tiles, chunks;                     // panels
+    int groups;                                // ceil(K / group)
+    int scale_pitch;                           // forward: groups of a tile, padded to whole chunks; backward: outputs, padded to whole chunks
+    size_t code_bytes, scale_count;
+};
+
+inline Q4Layout make_q4_layout(int N, int K, int group, int direction)
+{
+    Q4Layout q;
+    q.N = N; q.K = K; q.group = group; q.backward = direction == NOVA_Q4_BACKWARD;
+    q.rows = q.backward ? K : N;
+    q.reduction = q.backward ? N : K;
+    q.row_tiles = ceil_div(q.rows, kQ4Rows);
+    q.chunks = ceil_div(q.reduction, kQ4Chunk);
+    q.groups = ceil_div(K, group);
+    q.scale_pitch = q.backward ? q.chunks * kQ4Chunk : q.chunks * (kQ4Chunk / group);
+    q.code_bytes = (size_t)q.row_tiles * q.chunks * kQ4PanelBytes;
+    q.scale_count = q.backward ? (size_t)q.groups * q.scale_pitch : (size_t)q.row_tiles * q.scale_pitch * kQ4Rows;
+    return q;
+}
 
 }  // namespace nova
 
@@ -159,6 +185,28 @@ int launch_contract_int8(const void *Uq, const void *Vq, void *Mo, const void *u
 // ... of V in its storage format, quantised on the way in; partials (n_part maxima, per position with kind 2) are overwritten
 int launch_contract_int8_of_v(const void *Uq, const void *V, void *Mo, const void *u_scales, float *partials, int n_part,
                               int scale_kind, const Geometry &g, int dtype, void *stream);
+// Layers of 4-bit weights (Q4Layout): lay out from weights or from codes, read back, and the two products
+int launch_q4_quantize(const void *w, const Q4Layout &q, int dtype, void *Wq, void *stream);
+int launch_q4_pack(const int8_t *codes, const void *scales, const Q4Layout &q, int dtype, void *Wq, void *stream);
+int launch_q4_unpack(const void *Wq, const Q4Layout &q, int dtype, int8_t *codes, void *scales, void *stream);
+size_t q4_linear_workspace(int M, const Q4Layout &q, int dtype);
+int launch_q4_linear(const void *x, int64_t ldx, const void *Wq, const void *bias, void *y, int64_t ldy, int M, const Q4Layout &q, int dtype, int flags,
+                     void *workspace, void *stream);
+int launch_q4_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, const void *Wq, void *dx, int64_t lddx, int M, const Q4Layout &q,
+                              int dtype, void *workspace, void *stream);
+// Log probabilities of rows of logits
+size_t logprobs_workspace(int rows, int V, int top, int dtype);
+struct LogprobsArgs {
+    const void *logits; int64_t stride; const int64_t *targets; const uint8_t *mask; int64_t mask_stride;
+    int rows, V; float scale; int top;
+    float *logprob, *entropy, *stats, *top_logprobs; int64_t *top_ids;
+};
+int launch_logprobs(const LogprobsArgs &a, int dtype, void *workspace, void *stream);
+struct LogprobsBackwardArgs {
+    const void *logits; int64_t stride; const float *stats; const int64_t *targets; const float *g_logprob, *entropy, *g_entropy;
+    const uint8_t *mask; int64_t mask_stride; int rows, V; float scale; void *dlogits; int64_t dstride;
+};
+int launch_logprobs_backward(const LogprobsBackwardArgs &a, int dtype, void *stream);
 int launch_relu_maxpool2x2(const void *in, void *out, int N, int C, int H, int W, int dtype,
                            void *stream);
 }  // namespace nova

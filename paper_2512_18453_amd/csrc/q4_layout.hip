@@ -1,0 +1,147 @@
+// Layers with 4-bit weights: from weights or codes to the layout that the products read (nova_q4_pack in nova.h), and back.  Once per weight set, so
+// these are the plain loops over the layout's words and scales: one thread per word of eight codes, one per scale.
+#include "q4_common.hpp"
+
+namespace nova {
+
+// Row (of the layout) and position of the reduction -> output n and input k
+__device__ __forceinline__ void q4_element(const Q4Layout &q, int row, int pos, int &n, int &k)
+{
+    n = q.backward ? pos : row;
+    k = q.backward ? row : pos;
+}
+
+// Index of the scale of output n and group g
+__device__ __forceinline__ size_t q4_scale_index(const Q4Layout &q, int n, int g)
+{
+    if (q.backward) return (size_t)g * q.scale_pitch + n;
+    return ((size_t)(n / kQ4Rows) * q.scale_pitch + g) * kQ4Rows + n % kQ4Rows;
+}
+
+template <int DT, bool QUANTIZE>
+__global__ void __launch_bounds__(256) q4_scales_kernel(const Storage<DT> *__restrict__ src, Storage<DT> *__restrict__ scales, const Q4Layout q)
+{
+    for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < q.scale_count; idx += (size_t)gridDim.x * 256) {
+        int n, g;
+        if (q.backward) {
+            n = (int)(idx % q.scale_pitch);
+            g = (int)(idx / q.scale_pitch);
+        } else {
+            const size_t tile_group = idx / kQ4Rows;
+            n = (int)(tile_group / q.scale_pitch) * kQ4Rows + (int)(idx % kQ4Rows);
+            g = (int)(tile_group % q.scale_pitch);
+        }
+        Storage<DT> s = (Storage<DT>)0.0f;
+        if (n < q.N && g < q.groups) {
+            if constexpr (QUANTIZE) {
+                const Storage<DT> *w = src + (size_t)n * q.K;
+                const int end = min(q.K, (g + 1) * q.group);
+                float largest = 0.0f;
+                for (int k = g * q.group; k < end; ++k) {
+                    const float a = fabsf((float)w[k]);
+                    largest = (a > largest || a != a) ? a : largest;
+                    if (largest != largest) break;
+                }
+                s = (Storage<DT>)(largest - largest == 0.0f ? largest / 7.0f : __builtin_nanf(""));     // an infinity makes NaN too
+            } else {
+                s = src[(size_t)n * q.groups + g];
+            }
+        }
+        scales[idx] = s;
+    }
+}
+
+template <int DT, bool QUANTIZE>
+__global__ void __launch_bounds__(256) q4_codes_kernel(const void *__restrict__ src, const Storage<DT> *__restrict__ scales, unsigned *__restrict__ words,
+                                                       const Q4Layout q)
+{
+    const size_t total = q.code_bytes / 4;
+    for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (size_t)gridDim.x * 256) {
+        const int w = idx % 4, lane = idx / 4 % 64;
+        const size_t panel = idx / 256;
+        const int row = (int)(panel / q.chunks) * kQ4Rows + lane % 16;
+        const int first = (int)(panel % q.chunks) * kQ4Chunk + 32 * w + 8 * (lane / 16);
+        unsigned word = 0;
+        for (int v = 0; v < 8; ++v) {
+            if (row >= q.rows || first + v >= q.reduction) break;
+            int n, k, code;
+            q4_element(q, row, first + v, n, k);
+            const size_t at = (size_t)n * q.K + k;
+            if constexpr (QUANTIZE) {
+                const float s = (float)scales[q4_scale_index(q, n, k / q.group)];
+                const float c = s > 0.0f ? rintf((float)((const Storage<DT> *)src)[at] / s) : 0.0f;        // s NaN or 0: code 0
+                code = (int)fminf(fmaxf(c, -8.0f), 7.0f);
+            } else {
+                code = min(max((int)((const int8_t *)src)[at], -8), 7);
+            }
+            word |= ((unsigned)code & 15u) << (4 * (v / 2) + 16 * (v % 2));
+        }
+        words[idx] = word;
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256) q4_unpack_kernel(const unsigned *__restrict__ words, const Storage<DT> *__restrict__ scales, int8_t *__restrict__ codes,
+                                                        Storage<DT> *__restrict__ out_scales, const Q4Layout q)
+{
+    const size_t total = (size_t)q.N * q.K;
+    for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (size_t)gridDim.x * 256) {
+        const int n = (int)(idx / q.K), k = (int)(idx % q.K);
+        const int row = q.backward ? k : n, pos = q.backward ? n : k;
+        const size_t panel = (size_t)(row / kQ4Rows) * q.chunks + pos / kQ4Chunk;
+        const int lane = row % 16 + 16 * (pos % 32 / 8), w = pos % kQ4Chunk / 32, v = pos % 8;
+        const unsigned word = words[panel * 256 + lane * 4 + w];
+        codes[idx] = (int8_t)((int)(word << (28 - 4 * (v / 2) - 16 * (v % 2))) >> 28);
+        if (out_scales && k % q.group == 0) out_scales[(size_t)n * q.groups + k / q.group] = scales[q4_scale_index(q, n, k / q.group)];
+    }
+}
+
+static unsigned q4_blocks(size_t items)
+{
+    const size_t blocks = (items + 255) / 256;
+    return (unsigned)(blocks < 65536 ? blocks : 65536);
+}
+
+template <int DT, bool QUANTIZE>
+static int lay_out(const void *src, const void *scale_src, const Q4Layout &q, void *Wq, hipStream_t s)
+{
+    Storage<DT> *scales = (Storage<DT> *)((char *)Wq + q.code_bytes);
+    q4_scales_kernel<DT, QUANTIZE><<<q4_blocks(q.scale_count), 256, 0, s>>>((const Storage<DT> *)scale_src, scales, q);
+    NOVA_HIP_TRY(hipGetLastError());
+    q4_codes_kernel<DT, QUANTIZE><<<q4_blocks(q.code_bytes / 4), 256, 0, s>>>(src, scales, (unsigned *)Wq, q);
+    return (int)hipGetLastError();
+}
+
+int launch_q4_quantize(const void *w, const Q4Layout &q, int dtype, void *Wq, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    if (dtype == NOVA_F32) return lay_out<NOVA_F32, true>(w, w, q, Wq, s);
+    if (dtype == NOVA_F16) return lay_out<NOVA_F16, true>(w, w, q, Wq, s);
+    return lay_out<NOVA_BF16, true>(w, w, q, Wq, s);
+}
+
+int launch_q4_pack(const int8_t *codes, const void *scales, const Q4Layout &q, int dtype, void *Wq, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    if (dtype == NOVA_F32) return lay_out<NOVA_F32, false>(codes, scales, q, Wq, s);
+    if (dtype == NOVA_F16) return lay_out<NOVA_F16, false>(codes, scales, q, Wq, s);
+    return lay_out<NOVA_BF16, false>(codes, scales, q, Wq, s);
+}
+
+template <int DT>
+static int unpack(const void *Wq, const Q4Layout &q, int8_t *codes, void *scales, hipStream_t s)
+{
+    q4_unpack_kernel<DT><<<q4_blocks((size_t)q.N * q.K), 256, 0, s>>>((const unsigned *)Wq, (const Storage<DT> *)((const char *)Wq + q.code_bytes), codes,
+                                                                      (Storage<DT> *)scales, q);
+    return (int)hipGetLastError();
+}
+
+int launch_q4_unpack(const void *Wq, const Q4Layout &q, int dtype, int8_t *codes, void *scales, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    if (dtype == NOVA_F32) return unpack<NOVA_F32>(Wq, q, codes, scales, s);
+    if (dtype == NOVA_F16) return unpack<NOVA_F16>(Wq, q, codes, scales, s);
+    return unpack<NOVA_BF16>(Wq, q, codes, scales, s);
+}
+
+}  // namespace nova

@@ -7,16 +7,18 @@ succeeds but the first call raises.
 """
 import ctypes
 import os
+from collections import namedtuple
 from fractions import Fraction
 
 import torch
 
-NOVA_F32, NOVA_F16 = 0, 1
+NOVA_F32, NOVA_F16, NOVA_BF16 = 0, 1, 2
 NOVA_MATRIX_A, NOVA_MATRIX_BT, NOVA_MATRIX_G = 0, 1, 2
 NOVA_ROWS_PLAIN, NOVA_ROWS_BALANCED, NOVA_ROWS_GIVEN = 0, 1, 2
 NOVA_MATRIX_F32, NOVA_MATRIX_F16, NOVA_MATRIX_INT8 = 0, 1, 2
 NOVA_FLAG_RELU, NOVA_FLAG_M_F16, NOVA_FLAG_POOL2 = 1, 2, 4
 NOVA_INT8_PER_TENSOR, NOVA_INT8_PER_CHANNEL, NOVA_INT8_PER_POSITION = 0, 1, 2
+NOVA_Q4_FORWARD, NOVA_Q4_BACKWARD = 0, 1
 NOVA_PATH_STAGES, NOVA_PATH_FEW_CHANNELS, NOVA_PATH_FUSED_OUTPUT = 0, 1, 2
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libnova.so")
@@ -31,6 +33,8 @@ EXPORTS = [
     "nova_filter_int8_bytes", "nova_input_int8_bytes", "nova_quantize_filter_int8", "nova_quantize_input_int8",
     "nova_contract_int8", "nova_conv2d_int8_workspace_bytes", "nova_winograd_conv2d_int8",
     "nova_input_transform", "nova_contract", "nova_output_transform", "nova_relu_maxpool2x2",
+    "nova_q4_bytes", "nova_q4_quantize", "nova_q4_pack", "nova_q4_unpack", "nova_q4_linear_workspace_bytes", "nova_q4_linear", "nova_q4_linear_backward",
+    "nova_logprobs_workspace_bytes", "nova_logprobs", "nova_logprobs_backward",
     "nova_strerror", "nova_last_hip_error", "nova_version",
 ]
 
@@ -105,6 +109,20 @@ def lib():
         L.nova_contract.argtypes = [vp, vp, vp, vp, sz, i, i, i, i, i, i, i, vp]
         L.nova_output_transform.argtypes = [vp, vp, sz, vp, i, i, i, i, i, i, vp]
         L.nova_relu_maxpool2x2.argtypes = [vp, vp, i, i, i, i, i, vp]
+        i64, f = ctypes.c_int64, ctypes.c_float
+        L.nova_q4_bytes.argtypes = [i] * 5
+        L.nova_q4_bytes.restype = sz
+        L.nova_q4_quantize.argtypes = [vp, i, i, i, i, i, vp, sz, vp]
+        L.nova_q4_pack.argtypes = [vp, vp, i, i, i, i, i, vp, sz, vp]
+        L.nova_q4_unpack.argtypes = [vp, sz, i, i, i, i, i, vp, vp, vp]
+        L.nova_q4_linear_workspace_bytes.argtypes = [i] * 6
+        L.nova_q4_linear_workspace_bytes.restype = sz
+        L.nova_q4_linear.argtypes = [vp, i64, vp, sz, vp, vp, i64, i, i, i, i, i, i, vp, sz, vp]
+        L.nova_q4_linear_backward.argtypes = [vp, i64, vp, i64, vp, sz, vp, i64, i, i, i, i, i, vp, sz, vp]
+        L.nova_logprobs_workspace_bytes.argtypes = [i] * 4
+        L.nova_logprobs_workspace_bytes.restype = sz
+        L.nova_logprobs.argtypes = [vp, i64, vp, vp, i64, i, i, f, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.nova_logprobs_backward.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i, i, f, i, vp, i64, vp]
         L.nova_strerror.argtypes = [i]
         L.nova_strerror.restype = ctypes.c_char_p
         L.nova_last_hip_error.restype = i
@@ -441,6 +459,148 @@ def nova_relu_maxpool2x2(x, out=None):
         out = torch.empty((N, C, H // 2, W // 2), dtype=x.dtype, device=x.device)
     _check(lib().nova_relu_maxpool2x2(_dev(x), _dev(out), N, C, H, W, _dtype_code(x), _stream()), "nova_relu_maxpool2x2")
     return out
+
+
+# ---- layers with 4-bit weights, log probabilities ----
+
+_ANY_DTYPE = {torch.float32: NOVA_F32, torch.float16: NOVA_F16, torch.bfloat16: NOVA_BF16}
+
+
+def _any_dtype_code(dtype):
+    if dtype not in _ANY_DTYPE:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _ANY_DTYPE[dtype]
+
+
+def _rows(t, shape, dtype, what):
+    """(pointer, elements from row to row) of a matrix on the device whose rows lie whole, anywhere apart."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: expected a device tensor {shape} of {dtype} with elements of a row side by side")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+
+
+def _flat(t, count, dtype, what):
+    if not t.is_cuda or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous device tensor of {count} {dtype}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _bytes(t, what):
+    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous device tensor of bytes")
+    return ctypes.c_void_p(t.data_ptr()), t.numel()
+
+
+def nova_q4_bytes(N, K, group, dtype, direction=NOVA_Q4_FORWARD):
+    return lib().nova_q4_bytes(N, K, group, _any_dtype_code(dtype), direction)
+
+
+def nova_q4_quantize(w, group, direction=NOVA_Q4_FORWARD, Wq=None):
+    """w [N,K] -> its 4-bit layout for one direction (flat uint8)."""
+    (N, K), dt = w.shape, _any_dtype_code(w.dtype)
+    if Wq is None:
+        Wq = torch.empty(lib().nova_q4_bytes(N, K, group, dt, direction), dtype=torch.uint8, device=w.device)
+    _check(lib().nova_q4_quantize(_dev(w), N, K, group, dt, direction, *_bytes(Wq, "Wq"), _stream()), "nova_q4_quantize")
+    return Wq
+
+
+def nova_q4_pack(codes, scales, group, direction=NOVA_Q4_FORWARD, Wq=None):
+    """codes int8 [N,K] in [-8, 7], scales [N, ceil(K / group)] of the layer's dtype -> the 4-bit layout (flat uint8)."""
+    (N, K), dt = codes.shape, _any_dtype_code(scales.dtype)
+    if Wq is None:
+        Wq = torch.empty(lib().nova_q4_bytes(N, K, group, dt, direction), dtype=torch.uint8, device=codes.device)
+    _check(lib().nova_q4_pack(_flat(codes, N * K, torch.int8, "codes"), _flat(scales, N * -(-K // max(group, 1)), scales.dtype, "scales"), N, K, group, dt,
+                              direction, *_bytes(Wq, "Wq"), _stream()), "nova_q4_pack")
+    return Wq
+
+
+def nova_q4_unpack(Wq, N, K, group, dtype, direction=NOVA_Q4_FORWARD):
+    """(codes int8 [N,K], scales [N, ceil(K / group)]) of a layout."""
+    dt = _any_dtype_code(dtype)
+    codes = torch.empty((N, K), dtype=torch.int8, device=Wq.device)
+    scales = torch.empty((N, -(-K // max(group, 1))), dtype=dtype, device=Wq.device)
+    _check(lib().nova_q4_unpack(*_bytes(Wq, "Wq"), N, K, group, dt, direction, _dev(codes), _dev(scales), _stream()), "nova_q4_unpack")
+    return codes, scales
+
+
+def nova_q4_linear_workspace_bytes(M, N, K, group, dtype, direction=NOVA_Q4_FORWARD):
+    return lib().nova_q4_linear_workspace_bytes(M, N, K, group, _any_dtype_code(dtype), direction)
+
+
+def nova_q4_linear(x, Wq, N, group, bias=None, y=None, flags=0, workspace=None):
+    """x [M,K] -> y [M,N] through the 4-bit weights Wq (NOVA_Q4_FORWARD layout of x's dtype)."""
+    (M, K), dt = x.shape, _any_dtype_code(x.dtype)
+    if y is None:
+        y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(lib().nova_q4_linear_workspace_bytes(M, N, K, group, dt, NOVA_Q4_FORWARD), dtype=torch.uint8, device=x.device)
+    _check(lib().nova_q4_linear(*_rows(x, (M, K), x.dtype, "x"), *_bytes(Wq, "Wq"), None if bias is None else _flat(bias, N, x.dtype, "bias"),
+                                *_rows(y, (M, N), x.dtype, "y"), M, N, K, group, dt, flags, *_bytes(workspace, "workspace"), _stream()), "nova_q4_linear")
+    return y
+
+
+def nova_q4_linear_backward(dy, Wq, K, group, y=None, dx=None, workspace=None):
+    """dy [M,N] -> dx [M,K] through Wq (NOVA_Q4_BACKWARD layout of dy's dtype); y: the layer's result if a ReLU made it."""
+    (M, N), dt = dy.shape, _any_dtype_code(dy.dtype)
+    if dx is None:
+        dx = torch.empty((M, K), dtype=dy.dtype, device=dy.device)
+    if workspace is None:
+        workspace = torch.empty(lib().nova_q4_linear_workspace_bytes(M, N, K, group, dt, NOVA_Q4_BACKWARD), dtype=torch.uint8, device=dy.device)
+    _check(lib().nova_q4_linear_backward(*_rows(dy, (M, N), dy.dtype, "dy"), *((None, 0) if y is None else _rows(y, (M, N), dy.dtype, "y")),
+                                         *_bytes(Wq, "Wq"), *_rows(dx, (M, K), dy.dtype, "dx"), M, N, K, group, dt, *_bytes(workspace, "workspace"),
+                                         _stream()), "nova_q4_linear_backward")
+    return dx
+
+
+Logprobs = namedtuple("Logprobs", "logprob entropy stats top_logprobs top_ids")
+
+
+def _mask(mask, rows, V):
+    """(pointer, stride) of a boolean mask [rows,V], or [V] or [1,V] for all rows."""
+    if mask is None:
+        return None, 0
+    if mask.dtype not in (torch.bool, torch.uint8):
+        raise TypeError(f"mask: unsupported dtype {mask.dtype}")
+    mask = mask.unsqueeze(0) if mask.dim() == 1 else mask
+    shared = mask.shape[0] == 1
+    pointer, stride = _rows(mask, (1 if shared else rows, V), mask.dtype, "mask")
+    return pointer, 0 if shared else stride
+
+
+def nova_logprobs_workspace_bytes(rows, V, top, dtype):
+    return lib().nova_logprobs_workspace_bytes(rows, V, top, _any_dtype_code(dtype))
+
+
+def nova_logprobs(logits, targets=None, mask=None, scale=1.0, top=0, workspace=None):
+    """logits [rows,V] -> Logprobs: log probability of targets (int64 [rows]; None without), entropy, stats [rows,2] for the backward call, the `top`
+    best alternatives' log probabilities and ids [rows,top]."""
+    (R, V), dt, dev = logits.shape, _any_dtype_code(logits.dtype), logits.device
+    if workspace is None:
+        workspace = torch.empty(lib().nova_logprobs_workspace_bytes(R, V, top, dt), dtype=torch.uint8, device=dev)
+    f32 = torch.float32
+    out = Logprobs(None if targets is None else torch.empty(R, dtype=f32, device=dev), torch.empty(R, dtype=f32, device=dev),
+                   torch.empty((R, 2), dtype=f32, device=dev), torch.empty((R, top), dtype=f32, device=dev),
+                   torch.empty((R, top), dtype=torch.int64, device=dev))
+    _check(lib().nova_logprobs(*_rows(logits, (R, V), logits.dtype, "logits"), None if targets is None else _flat(targets, R, torch.int64, "targets"),
+                               *_mask(mask, R, V), R, V, scale, top, dt, None if targets is None else out.logprob.data_ptr(), out.entropy.data_ptr(),
+                               out.stats.data_ptr(), out.top_logprobs.data_ptr(), out.top_ids.data_ptr(), *_bytes(workspace, "workspace"), _stream()),
+           "nova_logprobs")
+    return out
+
+
+def nova_logprobs_backward(logits, stats, targets=None, g_logprob=None, entropy=None, g_entropy=None, mask=None, scale=1.0, dlogits=None):
+    """The logits' gradient of g_logprob . logprob + g_entropy . entropy; stats and entropy from nova_logprobs."""
+    (R, V), dt = logits.shape, _any_dtype_code(logits.dtype)
+    if dlogits is None:
+        dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
+
+    def row_values(t, what):
+        return None if t is None else _flat(t, R, torch.float32, what)
+    _check(lib().nova_logprobs_backward(*_rows(logits, (R, V), logits.dtype, "logits"), _flat(stats, 2 * R, torch.float32, "stats"),
+                                        None if targets is None else _flat(targets, R, torch.int64, "targets"), row_values(g_logprob, "g_logprob"),
+                                        row_values(entropy, "entropy"), row_values(g_entropy, "g_entropy"), *_mask(mask, R, V), R, V, scale, dt,
+                                        *_rows(dlogits, (R, V), logits.dtype, "dlogits"), _stream()), "nova_logprobs_backward")
+    return dlogits
 
 
 def nova_version():
