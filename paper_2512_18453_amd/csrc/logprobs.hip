@@ -1,85 +1,294 @@
 // Log probabilities of rows of logits, entropy, the largest alternatives, and the gradient of the first two (nova_logprobs in nova.h).
 //
-// With M the largest allowed logit and d = scale (x - M): L = ln sum e^d, H = L - sum e^d d / sum e^d.  One workgroup per row: a pass for M, one for the
-// sums, one per alternative.
+// With M the largest allowed logit and d = scale (x - M): L = ln sum e^d, H = L - sum e^d d / sum e^d.  All of it in one pass over a row: every lane keeps
+// the largest logit m it has seen, s = sum e^d and u = sum e^d d relative to it, and when m grows by some D, s becomes s e^-D and u becomes (u - s D) e^-D;
+// every wave keeps its best alternatives sorted, one per lane.  Rows are cut into slices where there are few of them; a second kernel joins the slices.
 #include "q4_common.hpp"
 
 namespace nova {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kThreads = 256;
+constexpr int kVectors = 4;                       // 8-element pieces that a lane has in hand at a time
+constexpr int kMaxWaves = 4;                      // of a workgroup that reads logits
+constexpr int kJoinWaves = 16;
+constexpr int kMaxSlices = 64;
 
-// Rank of a logit: greater for greater values, NaN above everything, -0 and 0 alike, -infinity (and masked) 0; below it the index, smaller first.  Ranks of a
-// row's entries are all different.
-__device__ __forceinline__ unsigned long long rank_of(float v, unsigned index)
+typedef unsigned long long rank_t;
+
+// Rank of a logit: greater for greater values, NaN one above +infinity, -0 and 0 alike, -infinity (and masked) 0; below it the index, smaller first.  The
+// ranks of a row's entries that count are all different.
+__device__ __forceinline__ unsigned value_rank(float v)
 {
-    if (v == -INFINITY) return 0;
-    unsigned bits = __float_as_uint(v + 0.0f);
+    unsigned bits = __float_as_uint(v);
+    if (v == 0.0f) bits = 0;
     bits = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
-    if (v != v) bits = 0xff800001u;               // one above +infinity
-    return (unsigned long long)bits << 32 | (0xffffffffu - index);
+    return v != v ? 0xff800001u : v == -INFINITY ? 0 : bits;
+}
+__device__ __forceinline__ float value_of_rank(unsigned r)
+{
+    return r == 0xff800001u ? __builtin_nanf("") : r == 0 ? -INFINITY : __uint_as_float(r & 0x80000000u ? r & 0x7fffffffu : ~r);
+}
+__device__ __forceinline__ rank_t rank_of(unsigned value, unsigned index) { return value ? (rank_t)value << 32 | (0xffffffffu - index) : 0; }
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;                                      // (fmaxf makes every operand canonical first, an instruction each; NaN is looked for elsewhere)
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ T over_workgroup(T v, T *shared, F &&join)
+__device__ __forceinline__ rank_t read_lane(rank_t v, int lane)
 {
-    for (int step = 32; step; step >>= 1) v = join(v, (T)__shfl_xor(v, step));
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = shared[0];
-    for (int w = 1; w < kThreads / 64; ++w) v = join(v, shared[w]);
-    return v;
+    return (rank_t)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
 }
 
-template <int DT, bool MASK>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobsArgs a)
+// m, s, u of a part of a row (d in units of ln 2)
+struct Sums {
+    float m, s, u;
+};
+__device__ __forceinline__ float finite_reference(float m) { return m == -INFINITY ? 0.0f : m; }
+__device__ __forceinline__ Sums rebased(Sums p, float m, float c)     // m >= p.m
 {
-    __shared__ unsigned long long shared_rank[kThreads / 64];
-    __shared__ float shared[kThreads / 64];
-    const int row = blockIdx.x;
-    const Storage<DT> *x = (const Storage<DT> *)a.logits + row * a.stride;
-    const uint8_t *mask = MASK ? a.mask + row * a.mask_stride : nullptr;
-    auto logit = [&](int v) { return !MASK || mask[v] ? load_f32(x + v) : -INFINITY; };
-    auto sum = [](float p, float q) { return p + q; };
-    float best = -INFINITY;
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads) best = fmaxf(best, logit(v));
-    best = over_workgroup(best, shared, [](float p, float q) { return fmaxf(p, q); });
-    const float c = a.scale * kLog2e, ref = best == -INFINITY ? 0.0f : best;
-    float s = 0.0f, u = 0.0f;
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-        const float d = (logit(v) - ref) * c, e = __builtin_amdgcn_exp2f(d);
-        s += e;
-        u = fma32(e, fmaxf(d, -1e4f), u);
+    const float D = (p.m - finite_reference(m)) * c, f = __builtin_amdgcn_exp2f(D);
+    return {m, p.s * f, fma32(p.s, fmaxf(D, -1e4f), p.u) * f};
+}
+__device__ __forceinline__ Sums joined(Sums p, Sums q, float c)
+{
+    const float m = fmaxf(p.m, q.m);
+    const Sums a = rebased(p, m, c), b = rebased(q, m, c);
+    return {m, a.s + b.s, a.u + b.u};
+}
+__device__ __forceinline__ Sums over_wave(Sums p, float c)
+{
+    for (int step = 32; step; step >>= 1) p = joined(p, {__shfl_xor(p.m, step), __shfl_xor(p.s, step), __shfl_xor(p.u, step)}, c);
+    return p;
+}
+
+// The best 64 of a wave, best first, one per lane (0: none)
+struct Best {
+    rank_t mine = 0;
+
+    // wave-uniform r
+    __device__ __forceinline__ void insert(rank_t r)
+    {
+        const int place = __popcll(__ballot(mine > r)), lane = threadIdx.x % 64;
+        const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(mine >> 32), 0x138, 0xf, 0xf, false);       // of the lane below
+        const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)mine, 0x138, 0xf, 0xf, false);
+        mine = lane < place ? mine : lane == place ? r : (rank_t)hi << 32 | lo;
     }
-    s = over_workgroup(s, shared, sum);
-    u = over_workgroup(u, shared, sum);
-    const bool empty = best == -INFINITY && s == 0.0f;
-    const float log_sum = empty ? -INFINITY : kLn2 * __log2f(s);
-    if (threadIdx.x == 0) {
-        a.stats[2 * (int64_t)row] = s == s ? best : __builtin_nanf("");
+    // another wave's list: the larger of each pair from both ends are the best 64, falling and then rising; six exchanges sort them
+    __device__ __forceinline__ void merge(const rank_t *other)
+    {
+        const int lane = threadIdx.x % 64;
+        const rank_t theirs = other[63 - lane];
+        mine = mine > theirs ? mine : theirs;
+        for (int step = 32; step; step >>= 1) {
+            const rank_t across = __shfl_xor(mine, step);
+            mine = ((lane & step) == 0) == (mine > across) ? mine : across;
+        }
+    }
+};
+
+// The largest value rank that at least `count` lanes reach, from the top bit down
+__device__ __forceinline__ unsigned reached_by(unsigned rank, int count)
+{
+    unsigned t = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const unsigned next = t | 1u << bit;
+        const int lanes = __popcll(__ballot(rank >= next));
+        if (lanes >= count) t = next;
+        if (lanes == count) break;
+    }
+    return t;
+}
+
+// What a row's sums and list give the caller
+template <int DT, bool MASK>
+__device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p, rank_t best)
+{
+    const int lane = threadIdx.x % 64;
+    const bool empty = p.m == -INFINITY && p.s == 0.0f, bad = !(p.s == p.s);
+    const float log_sum = empty ? -INFINITY : kLn2 * __log2f(p.s), nan = __builtin_nanf("");
+    if (lane == 0) {
+        a.stats[2 * (int64_t)row] = bad ? nan : p.m;
         a.stats[2 * (int64_t)row + 1] = log_sum;
-        if (a.entropy) a.entropy[row] = empty ? 0.0f : log_sum - kLn2 * u / s;
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : log_sum - kLn2 * (p.u / p.s);
         if (a.logprob) {
             const int64_t t = a.targets[row];
-            a.logprob[row] = t < 0 ? 0.0f : t >= a.V ? __builtin_nanf("") : empty ? -INFINITY : (logit(t) - ref) * a.scale - log_sum;
+            float lp = t < 0 ? 0.0f : nan;
+            if (t >= 0 && t < a.V) {
+                const bool allowed = !MASK || a.mask[row * a.mask_stride + t];
+                const float x = allowed ? load_f32((const Storage<DT> *)a.logits + row * a.stride + t) : -INFINITY;
+                lp = bad ? nan : empty ? -INFINITY : (x - p.m) * a.scale - log_sum;
+            }
+            a.logprob[row] = lp;
         }
     }
-    unsigned long long last = ~0ull;
-    for (int j = 0; j < a.top; ++j) {
-        unsigned long long next = 0;
-        for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-            const unsigned long long r = rank_of(logit(v), (unsigned)v);
-            if (r < last && r > next) next = r;
-        }
-        last = next = over_workgroup(next, shared_rank, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
-        if (threadIdx.x == 0) {
-            const int64_t at = (int64_t)row * a.top + j, id = next ? (int64_t)(0xffffffffu - (unsigned)next) : -1;
-            a.top_ids[at] = id;
-            a.top_logprobs[at] = s != s ? __builtin_nanf("") : next ? (logit(id) - ref) * a.scale - log_sum : -INFINITY;
-        }
+    if (lane < a.top) {
+        const int64_t at = (int64_t)row * a.top + lane;
+        a.top_ids[at] = best ? (int64_t)(0xffffffffu - (unsigned)best) : -1;
+        a.top_logprobs[at] = bad ? nan : best ? (value_of_rank((unsigned)(best >> 32)) - p.m) * a.scale - log_sum : -INFINITY;
     }
 }
+
+// A slice's results in the workspace: Sums, then top ranks
+__host__ __device__ inline size_t slice_bytes(int top) { return 16 + (size_t)top * 8; }
+
+// Workgroup (row, slice): threads take pieces of 8 logits in turn, kVectors in hand
+template <int DT, bool MASK, bool TOP>
+__global__ void __launch_bounds__(kMaxWaves * 64) logprobs_kernel(const LogprobsArgs a, int slices, int slice_length, char *__restrict__ workspace)
+{
+    __shared__ Sums wave_sums[kMaxWaves];
+    __shared__ rank_t lists[TOP ? kMaxWaves : 1][64];
+    const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const Storage<DT> *x = (const Storage<DT> *)a.logits + row * a.stride;
+    const uint8_t *mask = MASK ? a.mask + row * a.mask_stride : nullptr;
+    const unsigned begin = (unsigned)slice * slice_length, length = a.V - begin < (unsigned)slice_length ? a.V - begin : slice_length, end = begin + length;
+    const unsigned stride = blockDim.x * 8;
+    const float c = a.scale * kLog2e;
+
+    Eight<Storage<DT>> next[kVectors];
+    unsigned long long next_mask[kVectors];
+    auto fetch = [&](unsigned base) {
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) {
+            const unsigned at = base + j * stride + threadIdx.x * 8;
+            if (at + 8 <= end) {
+                __builtin_memcpy(&next[j], x + at, sizeof next[j]);
+                if (MASK) __builtin_memcpy(&next_mask[j], mask + at, 8);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) next[j].v[e] = at + e < end ? x[at + e] : (Storage<DT>)-INFINITY;
+                if (MASK) {
+                    next_mask[j] = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) next_mask[j] |= (unsigned long long)(at + e < end ? mask[at + e] : 0) << (8 * e);
+                }
+            }
+        }
+    };
+
+    Sums mine = {-INFINITY, 0.0f, 0.0f};
+    Best best;
+    rank_t last = 0;                              // the list's place a.top - 1: what an alternative has to exceed
+    float last_value = -INFINITY;
+    fetch(begin);
+    for (unsigned base = begin; base < end; base += kVectors * stride) {
+        float v[kVectors * 8];
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[8 * j + e] = (float)next[j].v[e];
+                if (MASK) v[8 * j + e] = (next_mask[j] >> (8 * e) & 0xff) ? v[8 * j + e] : -INFINITY;
+            }
+        if (end - base > kVectors * stride) fetch(base + kVectors * stride);
+        float largest = v[0];
+#pragma unroll
+        for (int i = 1; i < kVectors * 8 - 1; i += 2) largest = max3(largest, v[i], v[i + 1]);
+        largest = max3(largest, v[kVectors * 8 - 1], v[kVectors * 8 - 1]);
+        mine = rebased(mine, max3(mine.m, largest, largest), c);
+        const float ref = finite_reference(mine.m);
+        float s[2] = {0, 0}, u[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < kVectors * 8; ++i) {
+            const float d = (v[i] - ref) * c, e = __builtin_amdgcn_exp2f(d);
+            s[i % 2] += e;
+            u[i % 2] = fma32(e, fmaxf(d, -1e4f), u[i % 2]);
+        }
+        mine.s += s[0] + s[1];
+        mine.u += u[0] + u[1];
+        if constexpr (TOP) {
+            const unsigned long long passing = __ballot(!(largest < last_value) || mine.s != mine.s);
+            if (passing) {
+                // at least a.top lanes hold one that reaches `least`, so what is below it is no alternative
+                float least = last_value;
+                if (__popcll(passing) > a.top && !__ballot(mine.s != mine.s)) {
+                    const float lanes = value_of_rank(reached_by(value_rank(largest), a.top));
+                    least = lanes > least ? lanes : least;
+                }
+                static_for<kVectors * 8>([&](auto I) {
+                    constexpr int i = I;
+                    unsigned long long lanes = __ballot(!(v[i] < least) && v[i] != -INFINITY);
+                    while (lanes) {
+                        const int l = __builtin_ctzll(lanes);
+                        lanes &= lanes - 1;
+                        const float value = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(v[i]), l));
+                        const rank_t r = rank_of(value_rank(value), base + i / 8 * stride + (wave * 64 + l) * 8 + i % 8);
+                        if (r > last) {
+                            best.insert(r);
+                            last = read_lane(best.mine, a.top - 1);
+                        }
+                    }
+                });
+                if (last) last_value = value_of_rank((unsigned)(last >> 32));
+            }
+        }
+    }
+
+    mine = over_wave(mine, c);
+    if (waves > 1) {
+        if (lane == 0) wave_sums[wave] = mine;
+        if (TOP) lists[wave][lane] = best.mine;
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < waves; ++w) {
+            mine = joined(mine, wave_sums[w], c);
+            if (TOP) best.merge(lists[w]);
+        }
+    }
+    if (slices == 1) {
+        write_row<DT, MASK>(a, row, mine, best.mine);
+    } else {
+        char *out = workspace + blockIdx.x * slice_bytes(a.top);
+        if (lane == 0) *(Sums *)out = mine;
+        if (TOP && lane < a.top) ((rank_t *)(out + 16))[lane] = best.mine;
+    }
+}
+
+// Joins the slices of a row: the waves take slices in turn, then pair by pair, in an order that depends on nothing but their number
+template <int DT, bool MASK>
+__global__ void __launch_bounds__(kJoinWaves * 64) logprobs_join_kernel(const LogprobsArgs a, int slices, const char *__restrict__ workspace)
+{
+    __shared__ Sums wave_sums[kJoinWaves];
+    __shared__ rank_t lists[kJoinWaves][64];
+    const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const float c = a.scale * kLog2e;
+    const char *in = workspace + (size_t)row * slices * slice_bytes(a.top);
+    Sums mine = {-INFINITY, 0.0f, 0.0f};
+    Best best;
+    for (int i = wave; i < slices; i += waves) {
+        const char *part = in + i * slice_bytes(a.top);
+        mine = joined(mine, *(const Sums *)part, c);
+        if (a.top) {
+            const rank_t r = lane < a.top ? ((const rank_t *)(part + 16))[lane] : 0;
+            if (i == wave) {
+                best.mine = r;
+            } else {
+                lists[wave][lane] = r;
+                __builtin_amdgcn_wave_barrier();
+                best.merge(lists[wave]);
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    }
+    for (int half = waves / 2; half; half /= 2) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+            if (lane == 0) wave_sums[wave] = mine;
+            lists[wave][lane] = best.mine;
+        }
+        __syncthreads();
+        if (wave < half) {
+            mine = joined(mine, wave_sums[wave + half], c);
+            if (a.top) best.merge(lists[wave + half]);
+        }
+    }
+    if (wave == 0) write_row<DT, MASK>(a, row, mine, best.mine);
+}
+
+constexpr int kThreads = 256;
 
 template <int DT, bool MASK>
 __global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(const LogprobsBackwardArgs a)
@@ -105,15 +314,49 @@ __global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(const Logpr
     }
 }
 
-size_t logprobs_workspace(int, int, int, int) { return 0; }
+// How a call is cut: threads of a workgroup, slices of a row and their length (whole pieces of what a workgroup has in hand).
+struct LogprobsShape { int threads, slices, length; };
+static LogprobsShape logprobs_shape(int rows, int V)
+{
+    LogprobsShape p;
+    p.threads = V <= 64 * kVectors * 8 ? 64 : kMaxWaves * 64;
+    const int in_hand = p.threads * kVectors * 8;
+    int64_t slices = ((int64_t)V + in_hand - 1) / in_hand;
+    const int64_t wanted = (1024 + rows - 1) / (rows > 0 ? rows : 1);
+    if (slices > wanted) slices = wanted;
+    if (slices > kMaxSlices) slices = kMaxSlices;
+    const int64_t each = (((int64_t)V + slices - 1) / slices + in_hand - 1) / in_hand * in_hand;
+    p.length = (int)(each < INT32_MAX ? each : INT32_MAX);
+    p.slices = (int)(((int64_t)V + p.length - 1) / p.length);
+    return p;
+}
+
+size_t logprobs_workspace(int rows, int V, int top, int)
+{
+    const LogprobsShape p = logprobs_shape(rows, V);
+    return p.slices > 1 ? (size_t)rows * p.slices * slice_bytes(top) : 0;
+}
 
 constexpr int kRowsPerLaunch = 1 << 22;           // below 2^31 threads
 
-template <int DT>
-static int forward(LogprobsArgs a, hipStream_t s)
+template <int DT, bool MASK>
+static int forward_rows(const LogprobsArgs &a, const LogprobsShape &p, void *workspace, hipStream_t s)
 {
-    const int rows = a.rows;
-    for (int64_t r0 = 0; r0 < rows; r0 += kRowsPerLaunch) {
+    if (a.top) logprobs_kernel<DT, MASK, true><<<a.rows * p.slices, p.threads, 0, s>>>(a, p.slices, p.length, (char *)workspace);
+    else logprobs_kernel<DT, MASK, false><<<a.rows * p.slices, p.threads, 0, s>>>(a, p.slices, p.length, (char *)workspace);
+    NOVA_HIP_TRY(hipGetLastError());
+    if (p.slices == 1) return 0;
+    int waves = 1;
+    while (waves < kJoinWaves && waves < p.slices) waves *= 2;
+    logprobs_join_kernel<DT, MASK><<<a.rows, waves * 64, 0, s>>>(a, p.slices, (const char *)workspace);
+    return (int)hipGetLastError();
+}
+
+template <int DT>
+static int forward(const LogprobsArgs &a, void *workspace, hipStream_t s)
+{
+    const LogprobsShape shape = logprobs_shape(a.rows, a.V);
+    for (int64_t r0 = 0; r0 < a.rows; r0 += kRowsPerLaunch) {
         LogprobsArgs p = a;
         p.logits = (const Storage<DT> *)a.logits + r0 * a.stride;
         if (a.targets) p.targets += r0;
@@ -122,20 +365,19 @@ static int forward(LogprobsArgs a, hipStream_t s)
         if (a.entropy) p.entropy += r0;
         p.stats += 2 * r0;
         if (a.top) p.top_logprobs += r0 * a.top, p.top_ids += r0 * a.top;
-        const unsigned blocks = (unsigned)(rows - r0 < kRowsPerLaunch ? rows - r0 : kRowsPerLaunch);
-        if (a.mask) logprobs_kernel<DT, true><<<blocks, kThreads, 0, s>>>(p);
-        else logprobs_kernel<DT, false><<<blocks, kThreads, 0, s>>>(p);
-        NOVA_HIP_TRY(hipGetLastError());
+        p.rows = (int)(a.rows - r0 < kRowsPerLaunch ? a.rows - r0 : kRowsPerLaunch);
+        const int err = a.mask ? forward_rows<DT, true>(p, shape, workspace, s) : forward_rows<DT, false>(p, shape, workspace, s);
+        if (err) return err;
     }
     return 0;
 }
 
-int launch_logprobs(const LogprobsArgs &a, int dtype, void *, void *stream)
+int launch_logprobs(const LogprobsArgs &a, int dtype, void *workspace, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == NOVA_F32) return forward<NOVA_F32>(a, s);
-    if (dtype == NOVA_F16) return forward<NOVA_F16>(a, s);
-    return forward<NOVA_BF16>(a, s);
+    if (dtype == NOVA_F32) return forward<NOVA_F32>(a, workspace, s);
+    if (dtype == NOVA_F16) return forward<NOVA_F16>(a, workspace, s);
+    return forward<NOVA_BF16>(a, workspace, s);
 }
 
 template <int DT>
