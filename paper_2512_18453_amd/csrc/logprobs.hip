@@ -1,8 +1,13 @@
 // Log probabilities of rows of logits, entropy, the largest alternatives, and the gradient of the first two (nova_logprobs in nova.h).
 //
 // With M the largest allowed logit and d = scale (x - M): L = ln sum e^d, H = L - sum e^d d / sum e^d.  All of it in one pass over a row: every lane keeps
-// the largest logit m it has seen, s = sum e^d and u = sum e^d d relative to it, and when m grows by some D, s becomes s e^-D and u becomes (u - s D) e^-D;
-// every wave keeps its best alternatives sorted, one per lane.  Rows are cut into slices where there are few of them; a second kernel joins the slices.
+// the largest logit m it has seen, s = sum e^d and u = sum e^d d relative to it, and when m grows by some D, s becomes s e^-D and u becomes (u - s D) e^-D.
+// Rows are cut into slices where there are few of them; a second kernel joins the slices.
+//
+// Alternatives.  The pass leaves the largest logit of every lane and of every cell, the up to kCells parts that a lane's share is cut into.  If `least` is the
+// top-th largest of a wave's 64 lane maxima, the slice holds `top` logits that reach it, so only cells whose maximum reaches the largest `least` of the
+// waves are read again: with 131072 logits and 8 alternatives some dozen cells of 4096.  What reaches `least` in them is sorted by one wave.  Where that is
+// more than kCandidates (equal logits over all of a row) or a NaN stands in the row, the waves go over the slice once more, keeping sorted lists.
 #include "q4_common.hpp"
 
 namespace nova {
@@ -12,6 +17,8 @@ constexpr int kVectors = 4;                       // 8-element pieces that a lan
 constexpr int kMaxWaves = 4;                      // of a workgroup that reads logits
 constexpr int kJoinWaves = 16;
 constexpr int kMaxSlices = 64;
+constexpr int kCells = 16;                        // of a lane
+constexpr int kCandidates = 512;                  // eight per lane of the wave that sorts them
 
 typedef unsigned long long rank_t;
 
@@ -89,17 +96,52 @@ struct Best {
     }
 };
 
-// The largest value rank that at least `count` lanes reach, from the top bit down
-__device__ __forceinline__ unsigned reached_by(unsigned rank, int count)
+// The largest rank (of BITS bits) that at least `count` of the lanes' N ranks reach, from the top bit down
+template <int BITS, typename R, int N>
+__device__ __forceinline__ R reached_by(const R (&rank)[N], int count)
 {
-    unsigned t = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const unsigned next = t | 1u << bit;
-        const int lanes = __popcll(__ballot(rank >= next));
-        if (lanes >= count) t = next;
-        if (lanes == count) break;
+    R t = 0;
+    for (int bit = BITS - 1; bit >= 0; --bit) {
+        const R next = t | (R)1 << bit;
+        int reaching = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) reaching += __popcll(__ballot(rank[i] >= next));
+        if (reaching >= count) t = next;
+        if (reaching == count) break;
     }
     return t;
+}
+
+// The wave's candidates (count of them in `candidates`, all ranks different), the best `top` of them sorted, one per lane; scratch: 64 ranks
+__device__ __forceinline__ rank_t sorted_best(const rank_t *candidates, int count, int top, rank_t *scratch)
+{
+    const int lane = threadIdx.x % 64;
+    rank_t mine = lane < count ? candidates[lane] : 0;
+    if (count > 64) {
+        rank_t all[kCandidates / 64];
+#pragma unroll
+        for (int i = 0; i < kCandidates / 64; ++i) all[i] = i * 64 + lane < count ? candidates[i * 64 + lane] : 0;
+        const rank_t least = reached_by<64>(all, top);
+        int kept = 0;
+        scratch[lane] = 0;
+#pragma unroll
+        for (int i = 0; i < kCandidates / 64; ++i) {
+            const unsigned long long keep = __ballot(all[i] >= least);
+            if (keep >> lane & 1) scratch[kept + __popcll(keep & ((1ull << lane) - 1))] = all[i];
+            kept += __popcll(keep);
+        }
+        __builtin_amdgcn_wave_barrier();
+        mine = scratch[lane];
+        count = top;
+        __builtin_amdgcn_wave_barrier();
+    }
+    int place = 0;
+    for (int i = 0; i < count; ++i) place += read_lane(mine, i) > mine;
+    scratch[lane] = 0;
+    __builtin_amdgcn_wave_barrier();
+    if (lane < count) scratch[place] = mine;
+    __builtin_amdgcn_wave_barrier();
+    return scratch[lane];
 }
 
 // What a row's sums and list give the caller
@@ -135,55 +177,58 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p
 __host__ __device__ inline size_t slice_bytes(int top) { return 16 + (size_t)top * 8; }
 
 // Workgroup (row, slice): threads take pieces of 8 logits in turn, kVectors in hand
-template <int DT, bool MASK, bool TOP>
-__global__ void __launch_bounds__(kMaxWaves * 64) logprobs_kernel(const LogprobsArgs a, int slices, int slice_length, char *__restrict__ workspace)
+template <int DT, bool MASK, bool TOP, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs a, int slices, int slice_length, char *__restrict__ workspace)
 {
-    __shared__ Sums wave_sums[kMaxWaves];
-    __shared__ rank_t lists[TOP ? kMaxWaves : 1][64];
+    constexpr int THREADS = WAVES * 64, CELLS = WAVES == 1 ? 1 : kCells;           // (one wave takes what it can have in hand)
+    constexpr unsigned STRIDE = THREADS * 8, IN_HAND = kVectors * STRIDE;
+    __shared__ Sums wave_sums[WAVES];
+    __shared__ float wave_least[WAVES];
+    __shared__ float cell_largest[TOP ? CELLS : 1][TOP ? THREADS : 1];
+    __shared__ unsigned short cells[TOP ? kCandidates : 1];
+    __shared__ rank_t candidates[TOP ? kCandidates : 1], lists[TOP ? WAVES : 1][64];
+    __shared__ int found_cells, found;
     const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const Storage<DT> *x = (const Storage<DT> *)a.logits + row * a.stride;
     const uint8_t *mask = MASK ? a.mask + row * a.mask_stride : nullptr;
     const unsigned begin = (unsigned)slice * slice_length, length = a.V - begin < (unsigned)slice_length ? a.V - begin : slice_length, end = begin + length;
-    const unsigned stride = blockDim.x * 8;
+    const unsigned chunks = (length + IN_HAND - 1) / IN_HAND, per_cell = (chunks + CELLS - 1) / CELLS;
     const float c = a.scale * kLog2e;
 
-    Eight<Storage<DT>> next[kVectors];
-    unsigned long long next_mask[kVectors];
-    auto fetch = [&](unsigned base) {
+    struct Piece {
+        Eight<Storage<DT>> x;
+        unsigned long long mask;
+        __device__ __forceinline__ float operator[](int e) const { return !MASK || (mask >> (8 * e) & 0xff) ? (float)x.v[e] : -INFINITY; }
+    };
+    auto load_piece = [&](unsigned at, Piece &p) {
+        if (at + 8 <= end) {
+            __builtin_memcpy(&p.x, x + at, sizeof p.x);
+            if (MASK) __builtin_memcpy(&p.mask, mask + at, 8);
+        } else {
+            p.mask = 0;
 #pragma unroll
-        for (int j = 0; j < kVectors; ++j) {
-            const unsigned at = base + j * stride + threadIdx.x * 8;
-            if (at + 8 <= end) {
-                __builtin_memcpy(&next[j], x + at, sizeof next[j]);
-                if (MASK) __builtin_memcpy(&next_mask[j], mask + at, 8);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) next[j].v[e] = at + e < end ? x[at + e] : (Storage<DT>)-INFINITY;
-                if (MASK) {
-                    next_mask[j] = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) next_mask[j] |= (unsigned long long)(at + e < end ? mask[at + e] : 0) << (8 * e);
-                }
+            for (int e = 0; e < 8; ++e) {
+                p.x.v[e] = at + e < end ? x[at + e] : (Storage<DT>)-INFINITY;
+                if (MASK) p.mask |= (unsigned long long)(at + e < end ? mask[at + e] : 0) << (8 * e);
             }
         }
     };
+    Piece next[kVectors];
+    auto fetch = [&](unsigned base) {
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) load_piece(base + j * STRIDE + threadIdx.x * 8, next[j]);
+    };
 
     Sums mine = {-INFINITY, 0.0f, 0.0f};
-    Best best;
-    rank_t last = 0;                              // the list's place a.top - 1: what an alternative has to exceed
-    float last_value = -INFINITY;
+    float in_cell = -INFINITY;
+    if (TOP && threadIdx.x == 0) found_cells = found = 0;
     fetch(begin);
-    for (unsigned base = begin; base < end; base += kVectors * stride) {
+    for (unsigned chunk = 0, left = per_cell, cell = 0; chunk < chunks; ++chunk) {
         float v[kVectors * 8];
 #pragma unroll
-        for (int j = 0; j < kVectors; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[8 * j + e] = (float)next[j].v[e];
-                if (MASK) v[8 * j + e] = (next_mask[j] >> (8 * e) & 0xff) ? v[8 * j + e] : -INFINITY;
-            }
-        if (end - base > kVectors * stride) fetch(base + kVectors * stride);
+        for (int i = 0; i < kVectors * 8; ++i) v[i] = next[i / 8][i % 8];
+        if (chunk + 1 < chunks) fetch(begin + (chunk + 1) * IN_HAND);
         float largest = v[0];
 #pragma unroll
         for (int i = 1; i < kVectors * 8 - 1; i += 2) largest = max3(largest, v[i], v[i + 1]);
@@ -200,43 +245,89 @@ __global__ void __launch_bounds__(kMaxWaves * 64) logprobs_kernel(const Logprobs
         mine.s += s[0] + s[1];
         mine.u += u[0] + u[1];
         if constexpr (TOP) {
-            const unsigned long long passing = __ballot(!(largest < last_value) || mine.s != mine.s);
-            if (passing) {
-                // at least a.top lanes hold one that reaches `least`, so what is below it is no alternative
-                float least = last_value;
-                if (__popcll(passing) > a.top && !__ballot(mine.s != mine.s)) {
-                    const float lanes = value_of_rank(reached_by(value_rank(largest), a.top));
-                    least = lanes > least ? lanes : least;
-                }
-                static_for<kVectors * 8>([&](auto I) {
-                    constexpr int i = I;
-                    unsigned long long lanes = __ballot(!(v[i] < least) && v[i] != -INFINITY);
-                    while (lanes) {
-                        const int l = __builtin_ctzll(lanes);
-                        lanes &= lanes - 1;
-                        const float value = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(v[i]), l));
-                        const rank_t r = rank_of(value_rank(value), base + i / 8 * stride + (wave * 64 + l) * 8 + i % 8);
-                        if (r > last) {
-                            best.insert(r);
-                            last = read_lane(best.mine, a.top - 1);
-                        }
-                    }
-                });
-                if (last) last_value = value_of_rank((unsigned)(last >> 32));
+            in_cell = max3(in_cell, largest, largest);
+            if (--left == 0 || chunk + 1 == chunks) {
+                cell_largest[cell++][threadIdx.x] = in_cell;
+                in_cell = -INFINITY;
+                left = per_cell;
             }
         }
     }
 
+    Best best;
+    if constexpr (TOP) {
+        const unsigned used = (chunks + per_cell - 1) / per_cell;
+        const unsigned own[1] = {value_rank(mine.m)};
+        const unsigned reached = reached_by<32>(own, a.top);
+        if (lane == 0) wave_least[wave] = value_of_rank(reached);
+        bool again = __syncthreads_or(mine.s != mine.s);
+        float least = wave_least[0];
+        for (int w = 1; w < WAVES; ++w) least = max3(least, wave_least[w], wave_least[w]);
+        if (!again) {
+            for (unsigned i = 0; i < used; ++i) {
+                const float largest = cell_largest[i][threadIdx.x];
+                if (largest >= least && largest != -INFINITY) {
+                    const int at = atomicAdd(&found_cells, 1);
+                    if (at < kCandidates) cells[at] = (unsigned short)(i * THREADS + threadIdx.x);
+                }
+            }
+            __syncthreads();
+            again = found_cells > kCandidates;
+        }
+        if (!again) {
+            const unsigned pieces = per_cell * kVectors;
+            const uint64_t items = (uint64_t)found_cells * pieces;
+            for (uint64_t item = threadIdx.x; item < items; item += THREADS) {
+                const unsigned cell = cells[item / pieces], piece = (unsigned)(item % pieces);
+                const unsigned chunk = cell / THREADS * per_cell + piece / kVectors;
+                const unsigned at = begin + chunk * IN_HAND + piece % kVectors * STRIDE + cell % THREADS * 8;
+                if (chunk >= chunks || at >= end) continue;
+                Piece p;
+                load_piece(at, p);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = p[e];
+                    if (v >= least && v != -INFINITY) {
+                        const int place = atomicAdd(&found, 1);
+                        if (place < kCandidates) candidates[place] = rank_of(value_rank(v), at + e);
+                    }
+                }
+            }
+            __syncthreads();
+            again = found > kCandidates;
+        }
+        if (!again) {
+            if (wave == 0) best.mine = sorted_best(candidates, found, a.top, lists[0]);
+        } else {
+            rank_t last = 0;
+            for (unsigned base = begin + wave * 64; base < end; base += THREADS) {
+                const unsigned at = base + lane;
+                rank_t r = 0;
+                if (at < end && (!MASK || mask[at])) r = rank_of(value_rank(load_f32(x + at)), at);
+                unsigned long long lanes = __ballot(r > last);
+                while (lanes) {
+                    const rank_t one = read_lane(r, __builtin_ctzll(lanes));
+                    lanes &= lanes - 1;
+                    if (one > last) {
+                        best.insert(one);
+                        last = read_lane(best.mine, a.top - 1);
+                    }
+                }
+            }
+            if (WAVES > 1) {
+                lists[wave][lane] = best.mine;
+                __syncthreads();
+                if (wave == 0)
+                    for (int w = 1; w < WAVES; ++w) best.merge(lists[w]);
+            }
+        }
+    }
     mine = over_wave(mine, c);
-    if (waves > 1) {
+    if (WAVES > 1) {
         if (lane == 0) wave_sums[wave] = mine;
-        if (TOP) lists[wave][lane] = best.mine;
         __syncthreads();
         if (wave > 0) return;
-        for (int w = 1; w < waves; ++w) {
-            mine = joined(mine, wave_sums[w], c);
-            if (TOP) best.merge(lists[w]);
-        }
+        for (int w = 1; w < WAVES; ++w) mine = joined(mine, wave_sums[w], c);
     }
     if (slices == 1) {
         write_row<DT, MASK>(a, row, mine, best.mine);
@@ -342,8 +433,17 @@ constexpr int kRowsPerLaunch = 1 << 22;           // below 2^31 threads
 template <int DT, bool MASK>
 static int forward_rows(const LogprobsArgs &a, const LogprobsShape &p, void *workspace, hipStream_t s)
 {
-    if (a.top) logprobs_kernel<DT, MASK, true><<<a.rows * p.slices, p.threads, 0, s>>>(a, p.slices, p.length, (char *)workspace);
-    else logprobs_kernel<DT, MASK, false><<<a.rows * p.slices, p.threads, 0, s>>>(a, p.slices, p.length, (char *)workspace);
+    const unsigned blocks = (unsigned)a.rows * p.slices;
+    auto launch = [&](auto top, auto waves) {
+        logprobs_kernel<DT, MASK, top(), waves()><<<blocks, waves() * 64, 0, s>>>(a, p.slices, p.length, (char *)workspace);
+    };
+    using std::integral_constant;
+    auto with_top = [&](auto waves) {
+        if (a.top) launch(integral_constant<bool, true>{}, waves);
+        else launch(integral_constant<bool, false>{}, waves);
+    };
+    if (p.threads == 64) with_top(integral_constant<int, 1>{});
+    else with_top(integral_constant<int, kMaxWaves>{});
     NOVA_HIP_TRY(hipGetLastError());
     if (p.slices == 1) return 0;
     int waves = 1;
