@@ -5,9 +5,8 @@
 // Rows are cut into slices where there are few of them; a second kernel joins the slices.
 //
 // Alternatives.  The pass leaves the largest logit of every lane and of every cell, the up to kCells parts that a lane's share is cut into.  If `least` is the
-// top-th largest of a wave's 64 lane maxima, the slice holds `top` logits that reach it, so only cells whose maximum reaches the largest `least` of the
-// waves are read again: with 131072 logits and 8 alternatives some dozen cells of 4096.  What reaches `least` in them is sorted by one wave.  Where that is
-// more than kCandidates (equal logits over all of a row) or a NaN stands in the row, the waves go over the slice once more, keeping sorted lists.
+// top-th largest of the lane maxima, the slice holds `top` logits that reach it, so only cells whose maximum does are read again: with 131072
+// logits and 8 alternatives some dozen cells of 4096.  What reaches `least` in them is sorted by one wave.  Where that is more than kCandidates (equal logits over all of a row) or a NaN stands in the row, the waves go over the slice once more, keeping sorted lists.
 #include "q4_common.hpp"
 
 namespace nova {
@@ -112,28 +111,38 @@ __device__ __forceinline__ R reached_by(const R (&rank)[N], int count)
     return t;
 }
 
+// The best `top` of more candidates than lanes, one per lane, in any order
+template <int N>
+__device__ __forceinline__ rank_t best_of(const rank_t *candidates, int count, int top, rank_t *scratch)
+{
+    const int lane = threadIdx.x % 64;
+    rank_t all[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) all[i] = i * 64 + lane < count ? candidates[i * 64 + lane] : 0;
+    const rank_t least = reached_by<64>(all, top);
+    int kept = 0;
+    scratch[lane] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const unsigned long long keep = __ballot(all[i] >= least);
+        if (keep >> lane & 1) scratch[kept + __popcll(keep & ((1ull << lane) - 1))] = all[i];
+        kept += __popcll(keep);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const rank_t mine = scratch[lane];
+    __builtin_amdgcn_wave_barrier();
+    return mine;
+}
+
 // The wave's candidates (count of them in `candidates`, all ranks different), the best `top` of them sorted, one per lane; scratch: 64 ranks
 __device__ __forceinline__ rank_t sorted_best(const rank_t *candidates, int count, int top, rank_t *scratch)
 {
     const int lane = threadIdx.x % 64;
     rank_t mine = lane < count ? candidates[lane] : 0;
     if (count > 64) {
-        rank_t all[kCandidates / 64];
-#pragma unroll
-        for (int i = 0; i < kCandidates / 64; ++i) all[i] = i * 64 + lane < count ? candidates[i * 64 + lane] : 0;
-        const rank_t least = reached_by<64>(all, top);
-        int kept = 0;
-        scratch[lane] = 0;
-#pragma unroll
-        for (int i = 0; i < kCandidates / 64; ++i) {
-            const unsigned long long keep = __ballot(all[i] >= least);
-            if (keep >> lane & 1) scratch[kept + __popcll(keep & ((1ull << lane) - 1))] = all[i];
-            kept += __popcll(keep);
-        }
-        __builtin_amdgcn_wave_barrier();
-        mine = scratch[lane];
+        if (count <= 128) mine = best_of<2>(candidates, count, top, scratch);
+        else mine = best_of<kCandidates / 64>(candidates, count, top, scratch);
         count = top;
-        __builtin_amdgcn_wave_barrier();
     }
     int place = 0;
     for (int i = 0; i < count; ++i) place += read_lane(mine, i) > mine;
@@ -173,6 +182,30 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p
     }
 }
 
+// Eight logits from `at` on with their mask; what is masked or not before `end` reads as -infinity
+template <int DT, bool MASK>
+struct MaskedEight {
+    Eight<Storage<DT>> x;
+    unsigned long long mask;
+
+    __device__ __forceinline__ void load(const Storage<DT> *row, const uint8_t *row_mask, unsigned at, unsigned end)
+    {
+        if (at + 8 <= end) {
+            __builtin_memcpy(&x, row + at, sizeof x);
+            if (MASK) __builtin_memcpy(&mask, row_mask + at, 8);
+        } else {
+            mask = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x.v[e] = at + e < end ? row[at + e] : (Storage<DT>)-INFINITY;
+                if (MASK) mask |= (unsigned long long)(at + e < end ? row_mask[at + e] : 0) << (8 * e);
+            }
+        }
+    }
+    __device__ __forceinline__ bool allowed(int e) const { return !MASK || (mask >> (8 * e) & 0xff); }
+    __device__ __forceinline__ float operator[](int e) const { return allowed(e) ? (float)x.v[e] : -INFINITY; }
+};
+
 // A slice's results in the workspace: Sums, then top ranks
 __host__ __device__ inline size_t slice_bytes(int top) { return 16 + (size_t)top * 8; }
 
@@ -183,7 +216,7 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
     constexpr int THREADS = WAVES * 64, CELLS = WAVES == 1 ? 1 : kCells;           // (one wave takes what it can have in hand)
     constexpr unsigned STRIDE = THREADS * 8, IN_HAND = kVectors * STRIDE;
     __shared__ Sums wave_sums[WAVES];
-    __shared__ float wave_least[WAVES];
+    __shared__ unsigned lane_ranks[TOP ? THREADS : 1];
     __shared__ float cell_largest[TOP ? CELLS : 1][TOP ? THREADS : 1];
     __shared__ unsigned short cells[TOP ? kCandidates : 1];
     __shared__ rank_t candidates[TOP ? kCandidates : 1], lists[TOP ? WAVES : 1][64];
@@ -196,24 +229,8 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
     const unsigned chunks = (length + IN_HAND - 1) / IN_HAND, per_cell = (chunks + CELLS - 1) / CELLS;
     const float c = a.scale * kLog2e;
 
-    struct Piece {
-        Eight<Storage<DT>> x;
-        unsigned long long mask;
-        __device__ __forceinline__ float operator[](int e) const { return !MASK || (mask >> (8 * e) & 0xff) ? (float)x.v[e] : -INFINITY; }
-    };
-    auto load_piece = [&](unsigned at, Piece &p) {
-        if (at + 8 <= end) {
-            __builtin_memcpy(&p.x, x + at, sizeof p.x);
-            if (MASK) __builtin_memcpy(&p.mask, mask + at, 8);
-        } else {
-            p.mask = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p.x.v[e] = at + e < end ? x[at + e] : (Storage<DT>)-INFINITY;
-                if (MASK) p.mask |= (unsigned long long)(at + e < end ? mask[at + e] : 0) << (8 * e);
-            }
-        }
-    };
+    typedef MaskedEight<DT, MASK> Piece;
+    auto load_piece = [&](unsigned at, Piece &p) { p.load(x, mask, at, end); };
     Piece next[kVectors];
     auto fetch = [&](unsigned base) {
 #pragma unroll
@@ -257,12 +274,12 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
     Best best;
     if constexpr (TOP) {
         const unsigned used = (chunks + per_cell - 1) / per_cell;
-        const unsigned own[1] = {value_rank(mine.m)};
-        const unsigned reached = reached_by<32>(own, a.top);
-        if (lane == 0) wave_least[wave] = value_of_rank(reached);
+        lane_ranks[threadIdx.x] = value_rank(mine.m);
         bool again = __syncthreads_or(mine.s != mine.s);
-        float least = wave_least[0];
-        for (int w = 1; w < WAVES; ++w) least = max3(least, wave_least[w], wave_least[w]);
+        unsigned ranks[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) ranks[w] = lane_ranks[w * 64 + lane];
+        const float least = value_of_rank(reached_by<32>(ranks, a.top));
         if (!again) {
             for (unsigned i = 0; i < used; ++i) {
                 const float largest = cell_largest[i][threadIdx.x];
@@ -379,29 +396,48 @@ __global__ void __launch_bounds__(kJoinWaves * 64) logprobs_join_kernel(const Lo
     if (wave == 0) write_row<DT, MASK>(a, row, mine, best.mine);
 }
 
-constexpr int kThreads = 256;
-
+// Gradient of a row: scale ((a [v = target]) - p (a + h (ln p + H))).  Workgroup (row, slice of kBackwardLength); every thread reads kVectors pieces of 8, writes them
+// back.  Bound by memory: a logit is read and a gradient written once.
+constexpr int kBackwardThreads = 256, kBackwardLength = kBackwardThreads * kVectors * 8;
 template <int DT, bool MASK>
-__global__ void __launch_bounds__(kThreads) logprobs_backward_kernel(const LogprobsBackwardArgs a)
+__global__ void __launch_bounds__(kBackwardThreads) logprobs_backward_kernel(const LogprobsBackwardArgs a, int slices)
 {
-    const int row = blockIdx.x;
+    const int row = blockIdx.x / slices;
+    const unsigned begin = blockIdx.x % slices * (unsigned)kBackwardLength, end = a.V - begin < (unsigned)kBackwardLength ? a.V : begin + kBackwardLength;
     const Storage<DT> *x = (const Storage<DT> *)a.logits + row * a.stride;
     Storage<DT> *dx = (Storage<DT> *)a.dlogits + row * a.dstride;
     const uint8_t *mask = MASK ? a.mask + row * a.mask_stride : nullptr;
+    MaskedEight<DT, MASK> piece[kVectors];
+#pragma unroll
+    for (int j = 0; j < kVectors; ++j) piece[j].load(x, mask, begin + (j * kBackwardThreads + threadIdx.x) * 8, end);
     const float best = a.stats[2 * (int64_t)row], log_sum = a.stats[2 * (int64_t)row + 1];
-    const bool empty = best == -INFINITY;
     const int64_t t = a.targets ? a.targets[row] : -1;
     float g = a.g_logprob && t >= 0 ? a.g_logprob[row] : 0.0f;
     if (t >= a.V) g = __builtin_nanf("");
     const float h = a.g_entropy ? a.g_entropy[row] : 0.0f, H = h != 0.0f ? a.entropy[row] : 0.0f;
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-        float d = 0.0f;
-        if ((!MASK || mask[v]) && !(empty && t < a.V)) {
-            const float lp = (load_f32(x + v) - best) * a.scale - log_sum, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-            d = g * ((v == t ? 1.0f : 0.0f) - p) - h * (p * (fmaxf(lp, -1e4f) + H));
+    const bool empty = best == -INFINITY && t < a.V;
+    const float constant = fma32(h, H, g);
+#pragma unroll
+    for (int j = 0; j < kVectors; ++j) {
+        const unsigned at = begin + (j * kBackwardThreads + threadIdx.x) * 8;
+        if (at >= end) continue;
+        Eight<Storage<DT>> out;
+        const int64_t hit = t - at;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float lp = fma32((float)piece[j].x.v[e] - best, a.scale, -log_sum), p = __builtin_amdgcn_exp2f(lp * kLog2e);
+            float d = -(p * fma32(h, fmaxf(lp, -1e4f), constant));
+            if (hit == e) d = g + d;
             d *= a.scale;
+            out.v[e] = (Storage<DT>)(piece[j].allowed(e) && !empty ? d : 0.0f);
         }
-        store_from_f32(dx + v, d);
+        if (at + 8 <= end) {
+            __builtin_memcpy(dx + at, &out, sizeof out);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (at + e < end) dx[at + e] = out.v[e];
+        }
     }
 }
 
@@ -481,10 +517,10 @@ int launch_logprobs(const LogprobsArgs &a, int dtype, void *workspace, void *str
 }
 
 template <int DT>
-static int backward(LogprobsBackwardArgs a, hipStream_t s)
+static int backward(const LogprobsBackwardArgs &a, hipStream_t s)
 {
-    const int rows = a.rows;
-    for (int64_t r0 = 0; r0 < rows; r0 += kRowsPerLaunch) {
+    const int slices = (int)(((int64_t)a.V + kBackwardLength - 1) / kBackwardLength), rows_per_launch = slices < kRowsPerLaunch ? kRowsPerLaunch / slices : 1;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += rows_per_launch) {
         LogprobsBackwardArgs p = a;
         p.logits = (const Storage<DT> *)a.logits + r0 * a.stride;
         p.stats += 2 * r0;
@@ -494,9 +530,9 @@ static int backward(LogprobsBackwardArgs a, hipStream_t s)
         if (a.g_entropy) p.g_entropy += r0;
         if (a.mask) p.mask += r0 * a.mask_stride;
         p.dlogits = (Storage<DT> *)a.dlogits + r0 * a.dstride;
-        const unsigned blocks = (unsigned)(rows - r0 < kRowsPerLaunch ? rows - r0 : kRowsPerLaunch);
-        if (a.mask) logprobs_backward_kernel<DT, true><<<blocks, kThreads, 0, s>>>(p);
-        else logprobs_backward_kernel<DT, false><<<blocks, kThreads, 0, s>>>(p);
+        const unsigned blocks = (unsigned)(a.rows - r0 < rows_per_launch ? a.rows - r0 : rows_per_launch) * slices;
+        if (a.mask) logprobs_backward_kernel<DT, true><<<blocks, kBackwardThreads, 0, s>>>(p, slices);
+        else logprobs_backward_kernel<DT, false><<<blocks, kBackwardThreads, 0, s>>>(p, slices);
         NOVA_HIP_TRY(hipGetLastError());
     }
     return 0;

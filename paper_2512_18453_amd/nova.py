@@ -577,10 +577,9 @@ def nova_logprobs(logits, targets=None, mask=None, scale=1.0, top=0, workspace=N
     (R, V), dt, dev = logits.shape, _any_dtype_code(logits.dtype), logits.device
     if workspace is None:
         workspace = torch.empty(lib().nova_logprobs_workspace_bytes(R, V, top, dt), dtype=torch.uint8, device=dev)
-    f32 = torch.float32
-    out = Logprobs(None if targets is None else torch.empty(R, dtype=f32, device=dev), torch.empty(R, dtype=f32, device=dev),
-                   torch.empty((R, 2), dtype=f32, device=dev), torch.empty((R, top), dtype=f32, device=dev),
-                   torch.empty((R, top), dtype=torch.int64, device=dev))
+    # (one allocation for what is binary32: the call's host time is as long as its kernels')
+    logprob, entropy, stats, top_logprobs = torch.empty(R * (4 + top), dtype=torch.float32, device=dev).split_with_sizes((R, R, 2 * R, R * top))
+    out = Logprobs(None if targets is None else logprob, entropy, stats.view(R, 2), top_logprobs.view(R, top), torch.empty(R, top, dtype=torch.int64, device=dev))
     _check(lib().nova_logprobs(*_rows(logits, (R, V), logits.dtype, "logits"), None if targets is None else _flat(targets, R, torch.int64, "targets"),
                                *_mask(mask, R, V), R, V, scale, top, dt, None if targets is None else out.logprob.data_ptr(), out.entropy.data_ptr(),
                                out.stats.data_ptr(), out.top_logprobs.data_ptr(), out.top_ids.data_ptr(), *_bytes(workspace, "workspace"), _stream()),
