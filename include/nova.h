@@ -371,7 +371,7 @@ int nova_relu_maxpool2x2(const void *in, void *out, int N, int C, int H, int W, 
  *   NOVA_Q4_BACKWARD  nova_q4_linear_backward:  R = K rows, reduction over C = N
  * as [ceil(R/16)][ceil(C/128)] panels of 1024 bytes: 64 lanes of four 32-bit words, word w of lane 16 b + i holding the eight codes
  * of row 16 r + i at positions 128 c + 32 w + 8 b + v of the reduction, v = 0 .. 7, in bits 4 (v / 2) + 16 (v % 2) and the three above, two's
- * complement; then the scales: forward [ceil(R/16)][ceil(C/128) * 128 / group][16], backward [ceil(K/group)][ceil(N/128) * 128]; padding is zero.
+ * complement; then the scales: forward [ceil(R/16)][ceil(C/128)][16][128 / group], backward [ceil(K/group)][ceil(N/128) * 128]; padding is zero.
  *
  * nova_q4_bytes: size of a layout (0 for invalid arguments).
  * nova_q4_quantize: from weights w [N][K] (device, dtype): s = max|w| / 7 of the group, formed in binary32 and rounded to dtype, c = w / s

@@ -32,30 +32,43 @@ __device__ __forceinline__ float4v mfma(const Fragment &a, const Fragment &b, fl
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
 }
 
-// Eight codes of a word as binary16: the code with its sign bit flipped (c + 8) under the exponent of 1024 is 1024 + c + 8; 1032 comes off exactly.
+// A constant in a vector register: an instruction of three operands reads at most one scalar register, and the compiler gives up joining (w & a) ^ b rather than
+// move a constant.
+__device__ __forceinline__ unsigned in_vector(unsigned constant)
+{
+    unsigned v;
+    asm("v_mov_b32 %0, %1" : "=v"(v) : "s"(constant));
+    return v;
+}
+
+// Eight codes of a word as binary16: the code with its sign bit flipped (c + 8) under the exponent of 1024 is 1024 + c + 8; 1032 comes off exactly.  One place
+// higher it is 1024 + 16 (c + 8), of which a sixteenth less 72 is c.  Nine instructions.
 __device__ __forceinline__ Fragment codes_to_f16(unsigned word)
 {
-    word ^= 0x88888888u;
-    const half2v offset = {(f16)-1032.0f, (f16)-1032.0f};
+    const unsigned low = in_vector(0x000f000fu), low_base = in_vector(0x64086408u), high = in_vector(0x00f000f0u), high_base = in_vector(0x64806480u);
+    const half2v sixteenth = __builtin_bit_cast(half2v, in_vector(0x2c002c00u)), offset = __builtin_bit_cast(half2v, in_vector(0xe408e408u)),
+                 high_offset = __builtin_bit_cast(half2v, in_vector(0xd480d480u));
     Fragment f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const unsigned pair = ((word >> (4 * j)) & 0x000f000fu) | 0x64006400u;
-        f.words[j] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, pair) + offset);
+    for (int j = 0; j < 4; j += 2) {
+        const unsigned w = word >> (4 * j);
+        f.words[j] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, (w & low) ^ low_base) + offset);
+        f.words[j + 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & high) ^ high_base), sixteenth, high_offset));
     }
     return f;
 }
 
-// ... as bfloat16, divided by 16: v_cvt_off_f32_i4 makes c / 16 of the low four bits (exact in bfloat16: 3 bits), and the high halves of two such
-// binary32 values are the pair.
+// ... as bfloat16, divided by 16: v_cvt_off_f32_i4 makes c / 16 of the low four bits of a byte (exact in bfloat16: 3 bits), and the high halves of two such
+// binary32 values are the pair.  Thirteen instructions.
 constexpr float kCodeUnit = 16.0f;
 __device__ __forceinline__ Fragment codes_to_bf16_over_16(unsigned word)
 {
     Fragment f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float even = __builtin_amdgcn_cvt_off_f32_i4((int)(word >> (4 * j)));
-        const float odd = __builtin_amdgcn_cvt_off_f32_i4((int)(word >> (4 * j + 16)));
+        const unsigned w = word >> (4 * (j % 2));
+        const float even = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2))) & 0xff));
+        const float odd = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2) + 16)) & 0xff));
         f.words[j] = __builtin_amdgcn_perm(__float_as_uint(odd), __float_as_uint(even), 0x07060302u);
     }
     return f;
@@ -83,16 +96,24 @@ __device__ __forceinline__ void split_fragment(const float (&v)[8], Fragment (&f
     }
 }
 
-// `count` (at most 8) consecutive elements; those behind them are zero.  The rows of a caller's matrix begin anywhere, so the 16- and
-// 32-byte loads are unaligned ones.
+// `count` consecutive elements from p on, at most 8; those behind them are zero.  The rows of a caller's matrix begin anywhere, so the 16- and 32-byte loads
+// are unaligned ones.  Fewer than 8 are the end of what a load of the 8 up to there brings, if `before` says that 8 - count elements before p are the
+// caller's as well.
 template <typename T>
 struct Eight { T v[8]; };
 template <typename T>
-__device__ __forceinline__ Eight<T> load_eight(const T *p, int count)
+__device__ __forceinline__ Eight<T> load_eight(const T *p, int count, bool before = false)
 {
     Eight<T> e;
     if (count >= 8) {
         __builtin_memcpy(&e, p, sizeof e);
+    } else if (sizeof(T) == 2 && before) {
+        unsigned __int128 bits = 0;
+        if (count > 0) {
+            __builtin_memcpy(&bits, p + count - 8, sizeof bits);
+            bits >>= 16 * (8 - count);
+        }
+        __builtin_memcpy(&e, &bits, sizeof e);
     } else {
 #pragma unroll
         for (int v = 0; v < 8; ++v) e.v[v] = v < count ? p[v] : (T)0.0f;

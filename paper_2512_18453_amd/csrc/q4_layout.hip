@@ -15,7 +15,8 @@ __device__ __forceinline__ void q4_element(const Q4Layout &q, int row, int pos, 
 __device__ __forceinline__ size_t q4_scale_index(const Q4Layout &q, int n, int g)
 {
     if (q.backward) return (size_t)g * q.scale_pitch + n;
-    return ((size_t)(n / kQ4Rows) * q.scale_pitch + g) * kQ4Rows + n % kQ4Rows;
+    const int per_chunk = kQ4Chunk / q.group;
+    return ((size_t)(n / kQ4Rows) * q.scale_pitch + g / per_chunk * per_chunk) * kQ4Rows + n % kQ4Rows * per_chunk + g % per_chunk;
 }
 
 template <int DT, bool QUANTIZE>
@@ -27,9 +28,10 @@ __global__ void __launch_bounds__(256) q4_scales_kernel(const Storage<DT> *__res
             n = (int)(idx % q.scale_pitch);
             g = (int)(idx / q.scale_pitch);
         } else {
-            const size_t tile_group = idx / kQ4Rows;
-            n = (int)(tile_group / q.scale_pitch) * kQ4Rows + (int)(idx % kQ4Rows);
-            g = (int)(tile_group % q.scale_pitch);
+            const int per_chunk = kQ4Chunk / q.group;
+            const size_t chunk = idx / per_chunk / kQ4Rows;
+            n = (int)(chunk / q.chunks) * kQ4Rows + (int)(idx / per_chunk % kQ4Rows);
+            g = (int)(chunk % q.chunks) * per_chunk + (int)(idx % per_chunk);
         }
         Storage<DT> s = (Storage<DT>)0.0f;
         if (n < q.N && g < q.groups) {

@@ -1,23 +1,35 @@
 // The products of layers with 4-bit weights: y = x W^T (+ bias, ReLU) and the gradient of x, dx = d W.
 //
-// A workgroup makes 16 rows by 16 columns of the result; its waves share the reduction, a panel of 16 columns by 128 positions (1 KB of codes) at a
-// time, and add up through LDS in the order of their numbers.  Codes become operands in registers (q4_common.hpp).
+// Codes are read as panels of 16 columns by 128 positions of the reduction (1 KB, one 16-byte load per lane) and become operands of the matrix unit in
+// registers (q4_common.hpp).
 //   forward   a group's products are summed on the matrix unit with the codes as integers and the sum is scaled in binary32
 //   backward  the scales run along the reduction, so they go to the other operand: d * s in binary32, in two (three) bfloat16 pieces
+// Two kernels: up to 16 rows (q4_few_rows_kernel) the codes' bytes bind and nothing else; more rows (q4_tile_kernel) share the panels through LDS.
+// Where the result's tiles give too few workgroups, the reduction is cut over workgroups too; a third kernel adds the pieces in order.
+#ifdef Q4_TUNE
+#include <cstdio>
+#include <cstdlib>
+#endif
 #include "q4_common.hpp"
 
 namespace nova {
 
-constexpr int kWaves = 8;
+struct Q4Call {
+    const void *x, *gate, *bias;                  // x: the rows' operand; gate: the layer's result (backward)
+    const char *Wq;
+    void *out;
+    float *partial;                               // [splits][M][rows of the layout]
+    int64_t ldx, ldgate, ldout;
+    int M, relu, splits, split_chunks;
+    Q4Layout q;
+};
 
-// Operand pieces of eight elements of x: themselves, or three bfloat16 pieces of binary32
-template <int DT> constexpr int forward_pieces = DT == NOVA_F32 ? 3 : 1;
-template <int DT>
-__device__ __forceinline__ void x_fragment(const Eight<Storage<DT>> &e, Fragment (&f)[forward_pieces<DT>])
-{
-    if constexpr (DT == NOVA_F32) split_fragment<3>(e.v, f);
-    else __builtin_memcpy(&f[0], &e, 16);
-}
+// The scales of one column's groups in a panel, side by side
+template <typename T, int COUNT>
+struct alignas(sizeof(T) * COUNT) Several { T v[COUNT]; };
+
+// Operand pieces of a row's eight elements: forward themselves, or three bfloat16 pieces of binary32; backward of the product with the scales
+template <int DT, bool BACK> constexpr int kPieces = DT == NOVA_F32 ? 3 : BACK ? 2 : 1;
 
 template <bool HALF>
 __device__ __forceinline__ Fragment codes_fragment(unsigned word)
@@ -26,153 +38,443 @@ __device__ __forceinline__ Fragment codes_fragment(unsigned word)
     else return codes_to_bf16_over_16(word);
 }
 
-// The waves' sums of a 16 x 16 tile, added in order; thread t < 256 gets row t / 16, column t % 16
-__device__ __forceinline__ float sum_of_waves(float4v acc, float (*parts)[256])
+template <typename T>
+__device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, int n, float sum)
 {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int i = 0; i < 4; ++i) parts[wave][(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i];
-    __syncthreads();
-    float sum = 0.0f;
-    if (threadIdx.x < 256)
-        for (int w = 0; w < kWaves; ++w) sum += parts[w][threadIdx.x];
-    return sum;
+    if (a.splits > 1) {
+        a.partial[((size_t)split * a.M + m) * a.q.rows + n] = sum;
+    } else {
+        if (a.bias) sum += load_f32((const T *)a.bias + n);
+        if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
+        store_from_f32((T *)a.out + m * a.ldout + n, sum);
+    }
 }
 
-template <int DT, int GROUP>
-__global__ void __launch_bounds__(kWaves * 64)
-q4_linear_kernel(const Storage<DT> *__restrict__ x, int64_t ldx, const char *__restrict__ Wq, const Storage<DT> *__restrict__ bias,
-                 Storage<DT> *__restrict__ y, int64_t ldy, int M, const Q4Layout q, int relu)
+// ---- forward, up to 16 rows ----
+//
+// A wave makes 16 columns for all rows; `sharing` waves of a workgroup take the panels of the same columns in turn and add up through LDS in the order of their
+// numbers.  Bound by the codes' bytes: a wave has kAhead panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
+// along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it (read from memory as the
+// matrix unit takes it, 16 rows side by side, a load takes four times as long: each four lanes lie in four cache lines).
+template <int DT, int GROUP, int QUADS>
+struct FewRowsStage {
+    uint4v codes;
+    Eight<Storage<DT>> x[QUADS];                  // of row 4 i + lane / 16: positions 8 (lane % 16) ..
+    Several<Storage<DT>, kQ4Chunk / GROUP> scale;
+};
+
+template <int DT, int GROUP, int QUADS>
+__global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int sharing)
 {
+    typedef Storage<DT> T;
+    typedef FewRowsStage<DT, GROUP, QUADS> Stage;
     constexpr bool HALF = DT == NOVA_F16;
-    constexpr int P = forward_pieces<DT>;
-    __shared__ float parts[kWaves][256];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int tile = blockIdx.x % q.row_tiles, m0 = blockIdx.x / q.row_tiles * 16;
-    const int m = m0 + lane % 16;
-    const Storage<DT> *scales = (const Storage<DT> *)(Wq + q.code_bytes) + (size_t)tile * q.scale_pitch * kQ4Rows + lane % 16;
-    float4v acc = {0, 0, 0, 0}, part;
-    for (int c = wave; c < q.chunks; c += kWaves) {
-        const uint4v codes = *(const uint4v *)(Wq + ((size_t)tile * q.chunks + c) * kQ4PanelBytes + lane * 16);
+    constexpr int P = kPieces<DT, false>, SCALES = kQ4Chunk / GROUP, AHEAD = 4;
+    constexpr int PLANE = QUADS * 4 * 256, OWN = P * PLANE > 1024 ? P * PLANE : 1024;        // bytes of a wave: the operand, later its sums
+    extern __shared__ char lds[];
+    const Q4Layout &q = a.q;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), tiles = blockDim.x / 64 / sharing;
+    const int blocks = (q.row_tiles + tiles - 1) / tiles, split = blockIdx.x / blocks, tile0 = blockIdx.x % blocks * tiles;
+    const int tile = min(tile0 + wave / sharing, q.row_tiles - 1);           // (past the last: computed and not stored)
+    // whole panels of this wave, and the one that ends inside
+    const int whole = q.reduction / kQ4Chunk, first = split * a.split_chunks + wave % sharing, end = min(whole, (split + 1) * a.split_chunks);
+    const int count = end > first ? (end - first + sharing - 1) / sharing : 0;
+    const bool ragged = whole < q.chunks && split == a.splits - 1 && wave % sharing == (whole - split * a.split_chunks) % sharing;
+    const T *scales = (const T *)(a.Wq + q.code_bytes) + (size_t)tile * q.scale_pitch * kQ4Rows;
+    const char *codes = a.Wq + (size_t)tile * q.chunks * kQ4PanelBytes;
+    const T *x[QUADS];
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) x[i] = (const T *)a.x + min(4 * i + lane / 16, a.M - 1) * a.ldx + lane % 16 * 8;     // (as above)
+    char *own = lds + wave * OWN;
+
+    auto load_panel = [&](int c, Stage &s) {
+        s.codes = *(const uint4v *)(codes + (size_t)c * kQ4PanelBytes + lane * 16u);
+        s.scale = ((const Several<T, SCALES> *)scales)[(size_t)c * kQ4Rows + lane % 16u];
+    };
+    auto load = [&](int i, Stage &s) {
+        const int c = first + min(i, count - 1) * sharing;                      // (past the last: the last once more, and not multiplied)
+#pragma unroll
+        for (int r = 0; r < QUADS; ++r) __builtin_memcpy(&s.x[r], x[r] + c * kQ4Chunk, sizeof s.x[r]);
+        load_panel(c, s);
+    };
+
+    float4v acc = {0, 0, 0, 0}, part = {0, 0, 0, 0};
+    auto multiply = [&](const Stage &s) {
+        // 16-byte block b of row r lies at block b ^ r % 8: the eight rows that are read at a time lie in different banks
+#pragma unroll
+        for (int r = 0; r < QUADS; ++r) {
+            const int row = 4 * r + lane / 16;
+            Fragment f[P];
+            if constexpr (DT == NOVA_F32) split_fragment<P>(s.x[r].v, f);
+            else __builtin_memcpy(&f[0], &s.x[r], 16);
+#pragma unroll
+            for (int p = 0; p < P; ++p) *(uint4v *)(own + p * PLANE + row * 256 + ((lane % 16) ^ (row % 8)) * 16) = f[p].vec;
+        }
+#pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const int k = c * kQ4Chunk + w * 32 + lane / 16 * 8;
-            Fragment a[P];
-            x_fragment<DT>(load_eight(x + (int64_t)m * ldx + k, m < M ? q.K - k : 0), a);
-            const Fragment b = codes_fragment<HALF>(codes[w]);
+            const int row = lane % (4 * QUADS);
+            Fragment rows[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) rows[p].vec = *(const uint4v *)(own + p * PLANE + row * 256 + ((w * 4 + lane / 16) ^ (row % 8)) * 16);
+            const Fragment columns = codes_fragment<HALF>(s.codes[w]);
             if (w * 32 % GROUP == 0) part = (float4v){0, 0, 0, 0};
 #pragma unroll
-            for (int p = 0; p < P; ++p) part = mfma<HALF>(a[p], b, part);
+            for (int p = 0; p < P; ++p) part = mfma<HALF>(rows[p], columns, part);
             if ((w + 1) * 32 % GROUP == 0) {
-                const float s = (float)scales[(size_t)(c * (kQ4Chunk / GROUP) + w * 32 / GROUP) * kQ4Rows] * (HALF ? 1.0f : kCodeUnit);
-                for (int i = 0; i < 4; ++i) acc[i] = fma32(s, part[i], acc[i]);
+                const float scale = (float)s.scale.v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] = fma32(scale, part[i], acc[i]);
             }
         }
+    };
+
+    Stage stage[AHEAD];
+    if (ragged) {
+#pragma unroll
+        for (int r = 0; r < QUADS; ++r) stage[AHEAD - 1].x[r] = load_eight(x[r] + whole * kQ4Chunk, q.reduction - (whole * kQ4Chunk + lane % 16 * 8), whole > 0);
+        load_panel(whole, stage[AHEAD - 1]);
     }
-    float sum = sum_of_waves(acc, parts);
-    const int row = m0 + threadIdx.x / 16, n = tile * 16 + threadIdx.x % 16;
-    if (threadIdx.x < 256 && row < M && n < q.N) {
-        if (bias) sum += load_f32(bias + n);
-        if (relu) sum = sum < 0.0f ? 0.0f : sum;
-        store_from_f32(y + (int64_t)row * ldy + n, sum);
+    if (count > 0) static_for<AHEAD - 1>([&](auto I) { load(I, stage[I]); });
+    if (ragged) multiply(stage[AHEAD - 1]);
+    for (int i = 0; i < count; i += AHEAD)
+        static_for<AHEAD>([&](auto I) {
+            load(i + I + AHEAD - 1, stage[(I + AHEAD - 1) % AHEAD]);
+            if (i + I < count) multiply(stage[I]);
+        });
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ((float *)own)[(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < tiles * 256; e += blockDim.x) {
+        float sum = 0.0f;
+        for (int w = 0; w < sharing; ++w) sum += ((const float *)(lds + (e / 256 * sharing + w) * OWN))[e % 256];
+        const int m = e % 256 / 16, n = (tile0 + e / 256) * 16 + e % 16;
+        if (m < a.M && n < q.rows) store_result<T>(a, split, m, n, sum);
     }
+}
+
+// ---- more rows, and the gradient ----
+//
+// A workgroup makes 16 MT rows by 64 NT columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces, backward
+// with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), every wave reads it whole and multiplies its own NT panels. Two
+// such stages: one is filled while the other is multiplied.  A row's 16-byte blocks are stored at block ^ row % 16, so the 16 rows that a
+// fragment's load touches lie in different banks.
+template <int DT, bool BACK, int GROUP, int MT, int NT>
+__global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
+{
+    typedef Storage<DT> T;
+    constexpr bool HALF = DT == NOVA_F16 && !BACK;
+    constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP;
+    constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
+    constexpr int PLANE = MT * 16 * 256, STAGE = VERSIONS * P * PLANE;                // bytes
+    extern __shared__ char lds[];
+    const Q4Layout &q = a.q;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int column_blocks = (q.row_tiles + 4 * NT - 1) / (4 * NT), row_blocks = (a.M + 16 * MT - 1) / (16 * MT);
+    const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
+    const int m0 = id % row_blocks * (16 * MT), tile0 = (id / row_blocks % column_blocks * 4 + wave) * NT, split = id / row_blocks / column_blocks;
+    const int first = split * a.split_chunks, end = min(q.chunks, first + a.split_chunks);
+    const T *scales = (const T *)(a.Wq + q.code_bytes);
+
+    // thread t stages row t / 16 of every 16, positions 8 (t % 16) ..
+    const int my_row = threadIdx.x / 16, my_pos = threadIdx.x % 16 * 8;
+    Eight<T> x[MT], gate[BACK ? MT : 1], row_scale[VERSIONS];
+    uint4v codes[NT];
+    Several<T, SCALES> scale[BACK ? 1 : NT];
+    const T *x_row[MT], *gate_row[BACK ? MT : 1];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int m = min(m0 + t * 16 + my_row, a.M - 1);                  // (past the last: computed and not stored)
+        x_row[t] = (const T *)a.x + m * a.ldx + my_pos;
+        if (BACK) gate_row[t] = (const T *)a.gate + m * a.ldgate + my_pos;
+    }
+    auto load = [&](int c) {
+        const int at = c * kQ4Chunk;
+        if (at + kQ4Chunk <= q.reduction) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                __builtin_memcpy(&x[t], x_row[t] + at, sizeof x[t]);
+                if (BACK && a.gate) __builtin_memcpy(&gate[t], gate_row[t] + at, sizeof x[t]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), c > 0);
+                if (BACK && a.gate) gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), c > 0);
+            }
+        }
+        if constexpr (BACK) {
+            const int group = (tile0 - wave * NT) * 16 / GROUP;
+#pragma unroll
+            for (int v = 0; v < VERSIONS; ++v)
+                __builtin_memcpy(&row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + c * kQ4Chunk + my_pos, sizeof row_scale[v]);
+        }
+    };
+    auto load_codes = [&](int c) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int tile = min(tile0 + n, q.row_tiles - 1);              // (past the last: computed and not stored)
+            codes[n] = *(const uint4v *)(a.Wq + ((size_t)tile * q.chunks + c) * kQ4PanelBytes + lane * 16);
+            if constexpr (!BACK) {
+                scale[n] = ((const Several<T, SCALES> *)scales)[((size_t)tile * q.chunks + c) * kQ4Rows + lane % 16];
+            }
+        }
+    };
+    auto fill = [&](char *stage) {
+#pragma unroll
+        for (int v = 0; v < VERSIONS; ++v)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                Fragment f[P];
+                if constexpr (BACK) {
+                    float d[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] = (float)x[t].v[i] * ((float)row_scale[v].v[i] * kCodeUnit);
+                    if (a.gate) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) d[i] = (float)gate[t].v[i] > 0.0f ? d[i] : 0.0f;
+                    }
+                    split_fragment<P>(d, f);
+                } else if constexpr (DT == NOVA_F32) {
+                    split_fragment<P>(x[t].v, f);
+                } else {
+                    __builtin_memcpy(&f[0], &x[t], 16);
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    *(uint4v *)(stage + (v * P + p) * PLANE + (t * 16 + my_row) * 256 + ((my_pos / 8) ^ my_row) * 16) = f[p].vec;
+            }
+    };
+
+    float4v acc[MT][NT], part[BACK ? 1 : MT][BACK ? 1 : NT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[t][n] = (float4v){0, 0, 0, 0};
+    const int version = VERSIONS > 1 ? wave * NT * 16 / GROUP : 0;
+    auto multiply = [&](const char *stage, const uint4v (&panel)[NT], const Several<T, SCALES> (&panel_scale)[BACK ? 1 : NT]) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            Fragment rows[MT][P], columns[NT];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) columns[n] = codes_fragment<HALF>(panel[n][w]);
+            if constexpr (BACK) {
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) acc[t][n] = mfma<false>(rows[t][p], columns[n], acc[t][n]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+                            part[t][n] = mfma<HALF>(rows[t][p], columns[n], w * 32 % GROUP == 0 && p == 0 ? (float4v){0, 0, 0, 0} : part[t][n]);
+                if ((w + 1) * 32 % GROUP == 0) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const float s = (float)panel_scale[n].v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[t][n][i] = fma32(s, part[t][n][i], acc[t][n][i]);
+                    }
+                }
+            }
+        }
+    };
+
+    load(first);
+    load_codes(first);
+    fill(lds);
+    for (int c = first; c < end; ++c) {
+        uint4v panel[NT];
+        Several<T, SCALES> panel_scale[BACK ? 1 : NT];
+        __builtin_memcpy(panel, codes, sizeof panel);
+        __builtin_memcpy(panel_scale, scale, sizeof panel_scale);
+        const bool more = c + 1 < end;
+        if (more) {
+            load(c + 1);
+            load_codes(c + 1);
+        }
+        __syncthreads();
+        multiply(lds + (c - first) % 2 * STAGE, panel, panel_scale);
+        if (more) fill(lds + (c - first + 1) % 2 * STAGE);
+    }
+
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + t * 16 + lane / 16 * 4 + i;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int column = (tile0 + n) * 16 + lane % 16;
+                if (m < a.M && column < q.rows) store_result<T>(a, split, m, column, acc[t][n][i]);
+            }
+        }
+}
+
+// The pieces of a cut reduction, in order
+template <int DT>
+__global__ void __launch_bounds__(256) q4_join_kernel(const Q4Call a)
+{
+    typedef Storage<DT> T;
+    const size_t total = (size_t)a.M * a.q.rows;
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (size_t)gridDim.x * 256) {
+        float sum = 0.0f;
+        for (int s = 0; s < a.splits; ++s) sum += a.partial[s * total + at];
+        const int m = (int)(at / a.q.rows), n = (int)(at % a.q.rows);
+        if (a.bias) sum += load_f32((const T *)a.bias + n);
+        if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
+        store_from_f32((T *)a.out + m * a.ldout + n, sum);
+    }
+}
+
+// How a call is cut: few rows (mt 0; nt: waves that share a tile's panels) or tiles of 16 mt rows by 64 nt columns; waves of a workgroup; pieces of the reduction.
+struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
+static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
+{
+    Q4Shape p;
+    p.splits = 1;
+    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16)) {
+        p.mt = 0;
+        p.nt = q.row_tiles <= 512 ? 8 : q.row_tiles <= 2048 ? 4 : 2;
+        p.waves = p.nt < 4 ? 4 : p.nt;
+    } else {
+        p.mt = M <= 16 ? 1 : M <= 32 || dtype == NOVA_F32 ? 2 : 4;
+        p.nt = q.backward && q.group < 128 ? 1 : 2;
+        p.waves = 4;
+        const int64_t blocks = (int64_t)ceil_div(q.row_tiles, 4 * p.nt) * ceil_div(M, 16 * p.mt);
+        if (blocks < 256) p.splits = (int)(512 / blocks);
+        if (p.splits > ceil_div(q.chunks, 4)) p.splits = ceil_div(q.chunks, 4);
+    }
+    p.split_chunks = ceil_div(q.chunks, p.splits);
+    p.splits = ceil_div(q.chunks, p.split_chunks);
+#ifdef Q4_TUNE
+    if (const char *e = getenv("Q4SHAPE")) {
+        int mt, nt, w, s;
+        if (sscanf(e, "%d,%d,%d,%d", &mt, &nt, &w, &s) == 4) p.mt = mt, p.nt = nt, p.waves = w, p.splits = s;
+        if (p.splits > q.chunks) p.splits = q.chunks;
+        p.split_chunks = ceil_div(q.chunks, p.splits);
+        p.splits = ceil_div(q.chunks, p.split_chunks);
+    }
+#endif
+    return p;
+}
+
+size_t q4_linear_workspace(int M, const Q4Layout &q, int dtype)
+{
+    const Q4Shape p = q4_shape(M, q, dtype);
+    return p.splits > 1 ? (size_t)p.splits * M * q.rows * 4 : 0;
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kWaves * 64)
-q4_backward_kernel(const Storage<DT> *__restrict__ dy, int64_t lddy, const Storage<DT> *__restrict__ y, int64_t ldy, const char *__restrict__ Wq,
-                   Storage<DT> *__restrict__ dx, int64_t lddx, int M, const Q4Layout q)
+static int join(const Q4Call &a, hipStream_t s)
 {
-    constexpr int P = DT == NOVA_F32 ? 3 : 2;
-    __shared__ float parts[kWaves][256];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int tile = blockIdx.x % q.row_tiles, m0 = blockIdx.x / q.row_tiles * 16;
-    const int m = m0 + lane % 16;
-    const Storage<DT> *scales = (const Storage<DT> *)(Wq + q.code_bytes) + (size_t)(tile * 16 / q.group) * q.scale_pitch;
-    float4v acc = {0, 0, 0, 0};
-    for (int c = wave; c < q.chunks; c += kWaves) {
-        const uint4v codes = *(const uint4v *)(Wq + ((size_t)tile * q.chunks + c) * kQ4PanelBytes + lane * 16);
-        for (int w = 0; w < 4; ++w) {
-            const int n = c * kQ4Chunk + w * 32 + lane / 16 * 8, count = m < M ? q.N - n : 0;
-            const Eight<Storage<DT>> d = load_eight(dy + (int64_t)m * lddy + n, count);
-            const Eight<Storage<DT>> s = load_eight(scales + n, 8);
-            float v[8];
-            for (int i = 0; i < 8; ++i) v[i] = (float)d.v[i] * ((float)s.v[i] * kCodeUnit);
-            if (y) {
-                const Eight<Storage<DT>> r = load_eight(y + (int64_t)m * ldy + n, count);
-                for (int i = 0; i < 8; ++i) v[i] = (float)r.v[i] > 0.0f ? v[i] : 0.0f;
-            }
-            Fragment a[P];
-            split_fragment<P>(v, a);
-            const Fragment b = codes_to_bf16_over_16(codes[w]);
-#pragma unroll
-            for (int p = P - 1; p >= 0; --p) acc = mfma<false>(a[p], b, acc);
-        }
-    }
-    const float sum = sum_of_waves(acc, parts);
-    const int row = m0 + threadIdx.x / 16, k = tile * 16 + threadIdx.x % 16;
-    if (threadIdx.x < 256 && row < M && k < q.K) store_from_f32(dx + (int64_t)row * lddx + k, sum);
+    if (a.splits == 1) return 0;
+    const size_t blocks = ((size_t)a.M * a.q.rows + 255) / 256;
+    q4_join_kernel<DT><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(a);
+    return (int)hipGetLastError();
 }
 
-size_t q4_linear_workspace(int, const Q4Layout &, int) { return 0; }
-
-// Rows in pieces that keep a launch below 2^31 threads
-template <typename F>
-static int in_row_pieces(int M, const Q4Layout &q, F &&launch)
+template <int DT, bool BACK, int GROUP, int MT, int NT>
+static int run_tiles(const Q4Call &a, hipStream_t s)
 {
-    int64_t tiles = ((int64_t)1 << 31) / (kWaves * 64) / q.row_tiles;
+    const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, 4 * NT) * a.splits;
+    int64_t tiles = ((int64_t)1 << 31) / 256 / columns;                      // rows in pieces that keep a launch below 2^31 threads
     if (tiles < 1) tiles = 1;
-    for (int64_t m0 = 0; m0 < M; m0 += tiles * 16) {
-        const int rows = (int)(M - m0 < tiles * 16 ? M - m0 : tiles * 16);
-        launch(m0, rows, (unsigned)(ceil_div(rows, 16) * (int64_t)q.row_tiles));
+    const int64_t M = a.M, step = tiles * 16 * MT;
+    constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
+    constexpr unsigned lds = 2 * VERSIONS * kPieces<DT, BACK> * MT * 16 * 256;
+    for (int64_t m0 = 0; m0 < M; m0 += step) {
+        Q4Call part = a;
+        part.M = (int)(M - m0 < step ? M - m0 : step);
+        part.x = (const Storage<DT> *)a.x + m0 * a.ldx;
+        if (a.gate) part.gate = (const Storage<DT> *)a.gate + m0 * a.ldgate;
+        part.out = (Storage<DT> *)a.out + m0 * a.ldout;
+        q4_tile_kernel<DT, BACK, GROUP, MT, NT><<<(unsigned)(columns * ceil_div(part.M, 16 * MT)), 256, lds, s>>>(part);
         NOVA_HIP_TRY(hipGetLastError());
+        if (int err = join<DT>(part, s)) return err;
     }
     return 0;
 }
 
-template <int DT, int GROUP>
-static int linear(const void *x, int64_t ldx, const void *Wq, const void *bias, void *y, int64_t ldy, int M, const Q4Layout &q, int relu, hipStream_t s)
+template <int DT, int GROUP, int QUADS>
+static void run_few_rows(const Q4Call &a, const Q4Shape &p, hipStream_t s)
 {
-    return in_row_pieces(M, q, [&](int64_t m0, int rows, unsigned blocks) {
-        q4_linear_kernel<DT, GROUP><<<blocks, kWaves * 64, 0, s>>>((const Storage<DT> *)x + m0 * ldx, ldx, (const char *)Wq, (const Storage<DT> *)bias,
-                                                                   (Storage<DT> *)y + m0 * ldy, ldy, rows, q, relu);
-    });
+    constexpr unsigned operand = kPieces<DT, false> * QUADS * 4 * 256, own = operand > 1024 ? operand : 1024;
+    q4_few_rows_kernel<DT, GROUP, QUADS><<<ceil_div(a.q.row_tiles, p.waves / p.nt) * a.splits, p.waves * 64, p.waves * own, s>>>(a, p.nt);
 }
 
-template <int DT>
-static int linear_of_type(const void *x, int64_t ldx, const void *Wq, const void *bias, void *y, int64_t ldy, int M, const Q4Layout &q, int relu,
-                          hipStream_t s)
+template <int DT, bool BACK, int GROUP>
+static int run_group(const Q4Call &a, const Q4Shape &p, hipStream_t s)
 {
-    if (q.group == 32) return linear<DT, 32>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
-    if (q.group == 64) return linear<DT, 64>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
-    return linear<DT, 128>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
+    if constexpr (!BACK) {
+        if (p.mt == 0) {
+            if (a.M <= 4) run_few_rows<DT, GROUP, 1>(a, p, s);
+            else if constexpr (DT != NOVA_F32) {
+                if (a.M <= 8) run_few_rows<DT, GROUP, 2>(a, p, s);
+                else run_few_rows<DT, GROUP, 4>(a, p, s);
+            }
+            NOVA_HIP_TRY(hipGetLastError());
+            return join<DT>(a, s);
+        }
+    }
+    constexpr int NT = BACK && GROUP < 128 ? 1 : 2;
+    if constexpr (!BACK && DT != NOVA_F32) {
+        if (p.mt == 4 && p.nt == 4) return run_tiles<DT, BACK, GROUP, 4, 4>(a, s);
+        if (p.mt == 2 && p.nt == 1) return run_tiles<DT, BACK, GROUP, 2, 1>(a, s);
+    }
+    if constexpr (BACK && DT != NOVA_F32 && GROUP == 128) {
+        if (p.mt == 4 && p.nt == 4) return run_tiles<DT, BACK, GROUP, 4, 4>(a, s);
+    }
+    if (p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT>(a, s);
+    if (p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT>(a, s);
+    if constexpr (DT != NOVA_F32) return run_tiles<DT, BACK, GROUP, 4, NT>(a, s);
+    return (int)hipErrorInvalidValue;
+}
+
+template <int DT, bool BACK>
+static int run(Q4Call a, void *workspace, hipStream_t s)
+{
+    const Q4Shape p = q4_shape(a.M, a.q, DT);
+    a.partial = (float *)workspace;
+    a.splits = p.splits;
+    a.split_chunks = p.split_chunks;
+    if (a.q.group == 32) return run_group<DT, BACK, 32>(a, p, s);
+    if (a.q.group == 64) return run_group<DT, BACK, 64>(a, p, s);
+    return run_group<DT, BACK, 128>(a, p, s);
+}
+
+template <bool BACK>
+static int run_type(const Q4Call &a, int dtype, void *workspace, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    if (dtype == NOVA_F32) return run<NOVA_F32, BACK>(a, workspace, s);
+    if (dtype == NOVA_F16) return run<NOVA_F16, BACK>(a, workspace, s);
+    return run<NOVA_BF16, BACK>(a, workspace, s);
 }
 
 int launch_q4_linear(const void *x, int64_t ldx, const void *Wq, const void *bias, void *y, int64_t ldy, int M, const Q4Layout &q, int dtype, int flags,
-                     void *, void *stream)
+                     void *workspace, void *stream)
 {
-    hipStream_t s = (hipStream_t)stream;
-    const int relu = (flags & NOVA_FLAG_RELU) != 0;
-    if (dtype == NOVA_F32) return linear_of_type<NOVA_F32>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
-    if (dtype == NOVA_F16) return linear_of_type<NOVA_F16>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
-    return linear_of_type<NOVA_BF16>(x, ldx, Wq, bias, y, ldy, M, q, relu, s);
-}
-
-template <int DT>
-static int backward_of_type(const void *dy, int64_t lddy, const void *y, int64_t ldy, const void *Wq, void *dx, int64_t lddx, int M, const Q4Layout &q,
-                            hipStream_t s)
-{
-    return in_row_pieces(M, q, [&](int64_t m0, int rows, unsigned blocks) {
-        q4_backward_kernel<DT><<<blocks, kWaves * 64, 0, s>>>((const Storage<DT> *)dy + m0 * lddy, lddy, y ? (const Storage<DT> *)y + m0 * ldy : nullptr,
-                                                              ldy, (const char *)Wq, (Storage<DT> *)dx + m0 * lddx, lddx, rows, q);
-    });
+    const Q4Call a = {x, nullptr, bias, (const char *)Wq, y, nullptr, ldx, 0, ldy, M, (flags & NOVA_FLAG_RELU) != 0, 1, 0, q};
+    return run_type<false>(a, dtype, workspace, stream);
 }
 
 int launch_q4_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, const void *Wq, void *dx, int64_t lddx, int M, const Q4Layout &q,
-                              int dtype, void *, void *stream)
+                              int dtype, void *workspace, void *stream)
 {
-    hipStream_t s = (hipStream_t)stream;
-    if (dtype == NOVA_F32) return backward_of_type<NOVA_F32>(dy, lddy, y, ldy, Wq, dx, lddx, M, q, s);
-    if (dtype == NOVA_F16) return backward_of_type<NOVA_F16>(dy, lddy, y, ldy, Wq, dx, lddx, M, q, s);
-    return backward_of_type<NOVA_BF16>(dy, lddy, y, ldy, Wq, dx, lddx, M, q, s);
+    const Q4Call a = {dy, y, nullptr, (const char *)Wq, dx, nullptr, lddy, ldy, lddx, M, 0, 1, 0, q};
+    return run_type<true>(a, dtype, workspace, stream);
 }
 
 }  // namespace nova

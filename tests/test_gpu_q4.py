@@ -62,7 +62,7 @@ def test_layouts_read_back(N, K, group, dtype):
         if direction == FWD:
             want = np.zeros((tiles * 16, chunks * 128 // group), np.float32)
             want[:N, :G] = s
-            want = want.reshape(tiles, 16, -1).transpose(0, 2, 1).reshape(-1)
+            want = want.reshape(tiles, 16, chunks, -1).transpose(0, 2, 1, 3).reshape(-1)
         else:
             want = np.zeros((G, chunks * 128), np.float32)
             want[:, :N] = s.T
