@@ -32,47 +32,55 @@ __device__ __forceinline__ float4v mfma(const Fragment &a, const Fragment &b, fl
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
 }
 
-// A constant in a vector register: an instruction of three operands reads at most one scalar register, and the compiler gives up joining (w & a) ^ b rather than
-// move a constant.
-__device__ __forceinline__ unsigned in_vector(unsigned constant)
-{
-    unsigned v;
-    asm("v_mov_b32 %0, %1" : "=v"(v) : "s"(constant));
-    return v;
-}
-
 // Eight codes of a word as binary16: the code with its sign bit flipped (c + 8) under the exponent of 1024 is 1024 + c + 8; 1032 comes off exactly.  One place
-// higher it is 1024 + 16 (c + 8), of which a sixteenth less 72 is c.  Nine instructions.
-__device__ __forceinline__ Fragment codes_to_f16(unsigned word)
-{
-    const unsigned low = in_vector(0x000f000fu), low_base = in_vector(0x64086408u), high = in_vector(0x00f000f0u), high_base = in_vector(0x64806480u);
-    const half2v sixteenth = __builtin_bit_cast(half2v, in_vector(0x2c002c00u)), offset = __builtin_bit_cast(half2v, in_vector(0xe408e408u)),
-                 high_offset = __builtin_bit_cast(half2v, in_vector(0xd480d480u));
-    Fragment f;
-#pragma unroll
-    for (int j = 0; j < 4; j += 2) {
-        const unsigned w = word >> (4 * j);
-        f.words[j] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, (w & low) ^ low_base) + offset);
-        f.words[j + 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & high) ^ high_base), sixteenth, high_offset));
+// higher it is 1024 + 16 (c + 8), of which a sixteenth less 72 is c.  Nine instructions: (w & a) ^ b is one if a and b are in vector registers (an
+// instruction reads one scalar register at most), so a kernel puts the constants there once.
+struct F16Codes {
+    unsigned low, low_base, high, high_base;
+    half2v sixteenth, offset, high_offset;
+
+    static __device__ __forceinline__ unsigned in_vector(unsigned constant)
+    {
+        unsigned v;
+        asm volatile("v_mov_b32 %0, %1" : "=v"(v) : "s"(constant));
+        return v;
     }
-    return f;
-}
+    __device__ __forceinline__ F16Codes()
+        : low(in_vector(0x000f000fu)), low_base(in_vector(0x64086408u)), high(in_vector(0x00f000f0u)), high_base(in_vector(0x64806480u)),
+          sixteenth(__builtin_bit_cast(half2v, in_vector(0x2c002c00u))), offset(__builtin_bit_cast(half2v, in_vector(0xe408e408u))),
+          high_offset(__builtin_bit_cast(half2v, in_vector(0xd480d480u)))
+    {
+    }
+    __device__ __forceinline__ Fragment operator()(unsigned word) const
+    {
+        Fragment f;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            const unsigned w = word >> (4 * j);
+            f.words[j] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, (w & low) ^ low_base) + offset);
+            f.words[j + 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & high) ^ high_base), sixteenth, high_offset));
+        }
+        return f;
+    }
+};
 
 // ... as bfloat16, divided by 16: v_cvt_off_f32_i4 makes c / 16 of the low four bits of a byte (exact in bfloat16: 3 bits), and the high halves of two such
 // binary32 values are the pair.  Thirteen instructions.
 constexpr float kCodeUnit = 16.0f;
-__device__ __forceinline__ Fragment codes_to_bf16_over_16(unsigned word)
-{
-    Fragment f;
+struct Bf16Codes {
+    __device__ __forceinline__ Fragment operator()(unsigned word) const
+    {
+        Fragment f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const unsigned w = word >> (4 * (j % 2));
-        const float even = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2))) & 0xff));
-        const float odd = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2) + 16)) & 0xff));
-        f.words[j] = __builtin_amdgcn_perm(__float_as_uint(odd), __float_as_uint(even), 0x07060302u);
+        for (int j = 0; j < 4; ++j) {
+            const unsigned w = word >> (4 * (j % 2));
+            const float even = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2))) & 0xff));
+            const float odd = __builtin_amdgcn_cvt_off_f32_i4((int)((w >> (8 * (j / 2) + 16)) & 0xff));
+            f.words[j] = __builtin_amdgcn_perm(__float_as_uint(odd), __float_as_uint(even), 0x07060302u);
+        }
+        return f;
     }
-    return f;
-}
+};
 
 // Eight binary32 values as PIECES operands of bfloat16 whose sum they are: each piece but the last is the value cut off behind 8 bits of mantissa, so the
 // rest is exact (and an infinity is all in the first piece); the last is the rest rounded.  Two pieces: within 2^-15 of the value; three: all of it.

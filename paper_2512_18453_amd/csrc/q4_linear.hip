@@ -31,12 +31,7 @@ struct alignas(sizeof(T) * COUNT) Several { T v[COUNT]; };
 // Operand pieces of a row's eight elements: forward themselves, or three bfloat16 pieces of binary32; backward of the product with the scales
 template <int DT, bool BACK> constexpr int kPieces = DT == NOVA_F32 ? 3 : BACK ? 2 : 1;
 
-template <bool HALF>
-__device__ __forceinline__ Fragment codes_fragment(unsigned word)
-{
-    if constexpr (HALF) return codes_to_f16(word);
-    else return codes_to_bf16_over_16(word);
-}
+template <bool HALF> using Codes = std::conditional_t<HALF, F16Codes, Bf16Codes>;
 
 template <typename T>
 __device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, int n, float sum)
@@ -86,6 +81,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) x[i] = (const T *)a.x + min(4 * i + lane / 16, a.M - 1) * a.ldx + lane % 16 * 8;     // (as above)
     char *own = lds + wave * OWN;
+    const Codes<HALF> codes_to_operand;
 
     auto load_panel = [&](int c, Stage &s) {
         s.codes = *(const uint4v *)(codes + (size_t)c * kQ4PanelBytes + lane * 16u);
@@ -116,7 +112,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
             Fragment rows[P];
 #pragma unroll
             for (int p = 0; p < P; ++p) rows[p].vec = *(const uint4v *)(own + p * PLANE + row * 256 + ((w * 4 + lane / 16) ^ (row % 8)) * 16);
-            const Fragment columns = codes_fragment<HALF>(s.codes[w]);
+            const Fragment columns = codes_to_operand(s.codes[w]);
             if (w * 32 % GROUP == 0) part = (float4v){0, 0, 0, 0};
 #pragma unroll
             for (int p = 0; p < P; ++p) part = mfma<HALF>(rows[p], columns, part);
@@ -156,30 +152,37 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 //
 // A workgroup makes 16 MT rows by 64 NT columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces, backward
 // with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), every wave reads it whole and multiplies its own NT panels. Two
-// such stages: one is filled while the other is multiplied.  A row's 16-byte blocks are stored at block ^ row % 16, so the 16 rows that a
-// fragment's load touches lie in different banks.
+// such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks are stored at
+// block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
 template <int DT, bool BACK, int GROUP, int MT, int NT>
+struct TileStage {
+    static constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
+    Eight<Storage<DT>> x[MT], gate[BACK ? MT : 1], row_scale[BACK ? VERSIONS : 1];
+    uint4v codes[NT];
+    Several<Storage<DT>, kQ4Chunk / GROUP> scale[BACK ? 1 : NT];
+};
+
+template <int DT, bool BACK, int GROUP, int MT, int NT, int AHEAD>
 __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
 {
     typedef Storage<DT> T;
+    typedef TileStage<DT, BACK, GROUP, MT, NT> Stage;
     constexpr bool HALF = DT == NOVA_F16 && !BACK;
-    constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP;
-    constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
-    constexpr int PLANE = MT * 16 * 256, STAGE = VERSIONS * P * PLANE;                // bytes
+    constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP, VERSIONS = Stage::VERSIONS;
+    constexpr int PLANE = MT * 16 * 256, LDS_STAGE = VERSIONS * P * PLANE;            // bytes
+    static_assert(AHEAD % 2 == 0, "two stages in LDS");
     extern __shared__ char lds[];
     const Q4Layout &q = a.q;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int column_blocks = (q.row_tiles + 4 * NT - 1) / (4 * NT), row_blocks = (a.M + 16 * MT - 1) / (16 * MT);
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
     const int m0 = id % row_blocks * (16 * MT), tile0 = (id / row_blocks % column_blocks * 4 + wave) * NT, split = id / row_blocks / column_blocks;
-    const int first = split * a.split_chunks, end = min(q.chunks, first + a.split_chunks);
+    const int first = split * a.split_chunks, count = min(q.chunks - first, a.split_chunks);
     const T *scales = (const T *)(a.Wq + q.code_bytes);
+    const Codes<HALF> codes_to_operand;
 
     // thread t stages row t / 16 of every 16, positions 8 (t % 16) ..
     const int my_row = threadIdx.x / 16, my_pos = threadIdx.x % 16 * 8;
-    Eight<T> x[MT], gate[BACK ? MT : 1], row_scale[VERSIONS];
-    uint4v codes[NT];
-    Several<T, SCALES> scale[BACK ? 1 : NT];
     const T *x_row[MT], *gate_row[BACK ? MT : 1];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -187,39 +190,38 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
         x_row[t] = (const T *)a.x + m * a.ldx + my_pos;
         if (BACK) gate_row[t] = (const T *)a.gate + m * a.ldgate + my_pos;
     }
-    auto load = [&](int c) {
-        const int at = c * kQ4Chunk;
+    const char *panels[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) panels[n] = a.Wq + (size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks * kQ4PanelBytes;       // (as above)
+    auto load = [&](int i, Stage &s) {
+        const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
         if (at + kQ4Chunk <= q.reduction) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                __builtin_memcpy(&x[t], x_row[t] + at, sizeof x[t]);
-                if (BACK && a.gate) __builtin_memcpy(&gate[t], gate_row[t] + at, sizeof x[t]);
+                __builtin_memcpy(&s.x[t], x_row[t] + at, sizeof s.x[t]);
+                if (BACK && a.gate) __builtin_memcpy(&s.gate[t], gate_row[t] + at, sizeof s.x[t]);
             }
         } else {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), c > 0);
-                if (BACK && a.gate) gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), c > 0);
+                s.x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), c > 0);
+                if (BACK && a.gate) s.gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), c > 0);
             }
         }
         if constexpr (BACK) {
             const int group = (tile0 - wave * NT) * 16 / GROUP;
 #pragma unroll
             for (int v = 0; v < VERSIONS; ++v)
-                __builtin_memcpy(&row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + c * kQ4Chunk + my_pos, sizeof row_scale[v]);
+                __builtin_memcpy(&s.row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + at + my_pos, sizeof s.row_scale[v]);
         }
-    };
-    auto load_codes = [&](int c) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int tile = min(tile0 + n, q.row_tiles - 1);              // (past the last: computed and not stored)
-            codes[n] = *(const uint4v *)(a.Wq + ((size_t)tile * q.chunks + c) * kQ4PanelBytes + lane * 16);
-            if constexpr (!BACK) {
-                scale[n] = ((const Several<T, SCALES> *)scales)[((size_t)tile * q.chunks + c) * kQ4Rows + lane % 16];
-            }
+            s.codes[n] = *(const uint4v *)(panels[n] + (size_t)c * kQ4PanelBytes + lane * 16u);
+            if constexpr (!BACK)
+                s.scale[n] = ((const Several<T, SCALES> *)scales)[((size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks + c) * kQ4Rows + lane % 16u];
         }
     };
-    auto fill = [&](char *stage) {
+    auto fill = [&](char *stage, const Stage &s) {
 #pragma unroll
         for (int v = 0; v < VERSIONS; ++v)
 #pragma unroll
@@ -228,16 +230,16 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
                 if constexpr (BACK) {
                     float d[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = (float)x[t].v[i] * ((float)row_scale[v].v[i] * kCodeUnit);
+                    for (int i = 0; i < 8; ++i) d[i] = (float)s.x[t].v[i] * ((float)s.row_scale[v].v[i] * kCodeUnit);
                     if (a.gate) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) d[i] = (float)gate[t].v[i] > 0.0f ? d[i] : 0.0f;
+                        for (int i = 0; i < 8; ++i) d[i] = (float)s.gate[t].v[i] > 0.0f ? d[i] : 0.0f;
                     }
                     split_fragment<P>(d, f);
                 } else if constexpr (DT == NOVA_F32) {
-                    split_fragment<P>(x[t].v, f);
+                    split_fragment<P>(s.x[t].v, f);
                 } else {
-                    __builtin_memcpy(&f[0], &x[t], 16);
+                    __builtin_memcpy(&f[0], &s.x[t], 16);
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p)
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[t][n] = (float4v){0, 0, 0, 0};
     const int version = VERSIONS > 1 ? wave * NT * 16 / GROUP : 0;
-    auto multiply = [&](const char *stage, const uint4v (&panel)[NT], const Several<T, SCALES> (&panel_scale)[BACK ? 1 : NT]) {
+    auto multiply = [&](const char *stage, const Stage &s) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             Fragment rows[MT][P], columns[NT];
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
                 for (int p = 0; p < P; ++p)
                     rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) columns[n] = codes_fragment<HALF>(panel[n][w]);
+            for (int n = 0; n < NT; ++n) columns[n] = codes_to_operand(s.codes[n][w]);
             if constexpr (BACK) {
 #pragma unroll
                 for (int p = P - 1; p >= 0; --p)
@@ -280,34 +282,29 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
                 if ((w + 1) * 32 % GROUP == 0) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const float s = (float)panel_scale[n].v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
+                        const float scale = (float)s.scale[n].v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
 #pragma unroll
                         for (int t = 0; t < MT; ++t)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[t][n][i] = fma32(s, part[t][n][i], acc[t][n][i]);
+                            for (int i = 0; i < 4; ++i) acc[t][n][i] = fma32(scale, part[t][n][i], acc[t][n][i]);
                     }
                 }
             }
         }
     };
 
-    load(first);
-    load_codes(first);
-    fill(lds);
-    for (int c = first; c < end; ++c) {
-        uint4v panel[NT];
-        Several<T, SCALES> panel_scale[BACK ? 1 : NT];
-        __builtin_memcpy(panel, codes, sizeof panel);
-        __builtin_memcpy(panel_scale, scale, sizeof panel_scale);
-        const bool more = c + 1 < end;
-        if (more) {
-            load(c + 1);
-            load_codes(c + 1);
-        }
-        __syncthreads();
-        multiply(lds + (c - first) % 2 * STAGE, panel, panel_scale);
-        if (more) fill(lds + (c - first + 1) % 2 * STAGE);
-    }
+    Stage stage[AHEAD];
+    static_for<AHEAD - 1>([&](auto I) { load(I, stage[I]); });
+    fill(lds, stage[0]);
+    for (int i = 0; i < count; i += AHEAD)
+        static_for<AHEAD>([&](auto I) {
+            if (i + I < count) {
+                load(i + I + AHEAD - 1, stage[(I + AHEAD - 1) % AHEAD]);
+                __syncthreads();
+                multiply(lds + I % 2 * LDS_STAGE, stage[I]);
+                if (i + I + 1 < count) fill(lds + (I + 1) % 2 * LDS_STAGE, stage[(I + 1) % AHEAD]);
+            }
+        });
 
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -330,7 +327,13 @@ __global__ void __launch_bounds__(256) q4_join_kernel(const Q4Call a)
     const size_t total = (size_t)a.M * a.q.rows;
     for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (size_t)gridDim.x * 256) {
         float sum = 0.0f;
-        for (int s = 0; s < a.splits; ++s) sum += a.partial[s * total + at];
+        for (int s = 0; s < a.splits; s += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = s + i < a.splits ? a.partial[(s + i) * total + at] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
         const int m = (int)(at / a.q.rows), n = (int)(at % a.q.rows);
         if (a.bias) sum += load_f32((const T *)a.bias + n);
         if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
@@ -372,6 +375,7 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
 
 size_t q4_linear_workspace(int M, const Q4Layout &q, int dtype)
 {
+    if (M == 0) return 0;
     const Q4Shape p = q4_shape(M, q, dtype);
     return p.splits > 1 ? (size_t)p.splits * M * q.rows * 4 : 0;
 }
@@ -385,22 +389,21 @@ static int join(const Q4Call &a, hipStream_t s)
     return (int)hipGetLastError();
 }
 
-template <int DT, bool BACK, int GROUP, int MT, int NT>
+template <int DT, bool BACK, int GROUP, int MT, int NT, int AHEAD>
 static int run_tiles(const Q4Call &a, hipStream_t s)
 {
     const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, 4 * NT) * a.splits;
     int64_t tiles = ((int64_t)1 << 31) / 256 / columns;                      // rows in pieces that keep a launch below 2^31 threads
     if (tiles < 1) tiles = 1;
     const int64_t M = a.M, step = tiles * 16 * MT;
-    constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
-    constexpr unsigned lds = 2 * VERSIONS * kPieces<DT, BACK> * MT * 16 * 256;
+    constexpr unsigned lds = 2 * TileStage<DT, BACK, GROUP, MT, NT>::VERSIONS * kPieces<DT, BACK> * MT * 16 * 256;
     for (int64_t m0 = 0; m0 < M; m0 += step) {
         Q4Call part = a;
         part.M = (int)(M - m0 < step ? M - m0 : step);
         part.x = (const Storage<DT> *)a.x + m0 * a.ldx;
         if (a.gate) part.gate = (const Storage<DT> *)a.gate + m0 * a.ldgate;
         part.out = (Storage<DT> *)a.out + m0 * a.ldout;
-        q4_tile_kernel<DT, BACK, GROUP, MT, NT><<<(unsigned)(columns * ceil_div(part.M, 16 * MT)), 256, lds, s>>>(part);
+        q4_tile_kernel<DT, BACK, GROUP, MT, NT, AHEAD><<<(unsigned)(columns * ceil_div(part.M, 16 * MT)), 256, lds, s>>>(part);
         NOVA_HIP_TRY(hipGetLastError());
         if (int err = join<DT>(part, s)) return err;
     }
@@ -429,16 +432,14 @@ static int run_group(const Q4Call &a, const Q4Shape &p, hipStream_t s)
         }
     }
     constexpr int NT = BACK && GROUP < 128 ? 1 : 2;
-    if constexpr (!BACK && DT != NOVA_F32) {
-        if (p.mt == 4 && p.nt == 4) return run_tiles<DT, BACK, GROUP, 4, 4>(a, s);
-        if (p.mt == 2 && p.nt == 1) return run_tiles<DT, BACK, GROUP, 2, 1>(a, s);
-    }
-    if constexpr (BACK && DT != NOVA_F32 && GROUP == 128) {
-        if (p.mt == 4 && p.nt == 4) return run_tiles<DT, BACK, GROUP, 4, 4>(a, s);
-    }
-    if (p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT>(a, s);
-    if (p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT>(a, s);
-    if constexpr (DT != NOVA_F32) return run_tiles<DT, BACK, GROUP, 4, NT>(a, s);
+#ifdef Q4_TUNE
+    if (p.waves == 2 && p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT, 2>(a, s);
+    if (p.waves == 2 && p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT, 2>(a, s);
+    if constexpr (DT != NOVA_F32) if (p.waves == 2) return run_tiles<DT, BACK, GROUP, 4, NT, 2>(a, s);
+#endif
+    if (p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT, 4>(a, s);
+    if (p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT, 4>(a, s);
+    if constexpr (DT != NOVA_F32) return run_tiles<DT, BACK, GROUP, 4, NT, 4>(a, s);
     return (int)hipErrorInvalidValue;
 }
 

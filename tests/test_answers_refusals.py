@@ -110,3 +110,11 @@ def test_binding():
         nova.nova_q4_linear(x.double(), torch.zeros(10, dtype=torch.uint8), 20, 32)
     with pytest.raises(TypeError):
         nova.nova_logprobs(x.long())
+
+
+@pytest.mark.parametrize("direction", [0, 1])
+def test_no_rows_need_no_workspace(direction):
+    # (the host divides by the number of tiles, of which there are none)
+    for N, K in ((1, 1), (20, 40), (4096, 25088)):
+        assert nova.lib().nova_q4_linear_workspace_bytes(0, N, K, 32, F16, direction) == 0
+    assert nova.lib().nova_logprobs_workspace_bytes(0, 200000, 5, F16) == 0
