@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
     const Codes<HALF> codes_to_operand;
 
     auto load_panel = [&](int c, Stage &s) {
-        s.codes = *(const uint4v *)(codes + (size_t)c * kQ4PanelBytes + lane * 16u);
+        s.codes = __builtin_nontemporal_load((const uint4v *)(codes + (size_t)c * kQ4PanelBytes + lane * 16u));
         s.scale = ((const Several<T, SCALES> *)scales)[(size_t)c * kQ4Rows + lane % 16u];
     };
     auto load = [&](int i, Stage &s) {
@@ -150,43 +150,54 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 
 // ---- more rows, and the gradient ----
 //
-// A workgroup makes 16 MT rows by 64 NT columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces, backward
-// with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), every wave reads it whole and multiplies its own NT panels. Two
-// such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks are stored at
-// block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
-template <int DT, bool BACK, int GROUP, int MT, int NT>
-struct TileStage {
-    static constexpr int VERSIONS = BACK && 64 * NT > GROUP ? 64 * NT / GROUP : 1;
-    Eight<Storage<DT>> x[MT], gate[BACK ? MT : 1], row_scale[BACK ? VERSIONS : 1];
-    uint4v codes[NT];
-    Several<Storage<DT>, kQ4Chunk / GROUP> scale[BACK ? 1 : NT];
+// A workgroup of WM x WN waves makes 16 MT WM rows by 16 NT WN columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces,
+// backward with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), a wave reads its rows of it and multiplies its own NT
+// panels.  Two such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks
+// are stored at block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
+template <int MT_, int NT_, int WM_, int WN_, int AHEAD_>
+struct Tile {
+    static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, AHEAD = AHEAD_, THREADS = 64 * WM * WN, ROWS = 16 * MT * WM, PANELS = NT * WN;
+    static constexpr int PIECES = ROWS * 16 / THREADS;                       // 8-element pieces of a stage that a thread loads
+    template <bool BACK, int GROUP> static constexpr int versions = BACK && 16 * PANELS > GROUP ? 16 * PANELS / GROUP : 1;
+    template <int DT, bool BACK, int GROUP> static constexpr unsigned lds_bytes = 2 * versions<BACK, GROUP> * kPieces<DT, BACK> * ROWS * 256;
+    static_assert(AHEAD % 2 == 0, "two stages in LDS");
 };
 
-template <int DT, bool BACK, int GROUP, int MT, int NT, int AHEAD>
-__global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
+template <int DT, bool BACK, int GROUP, typename Shape>
+struct TileStage {
+    Eight<Storage<DT>> x[Shape::PIECES], gate[BACK ? Shape::PIECES : 1], row_scale[Shape::template versions<BACK, GROUP>];
+    uint4v codes[Shape::NT];
+    Several<Storage<DT>, kQ4Chunk / GROUP> scale[BACK ? 1 : Shape::NT];
+};
+
+template <int DT, bool BACK, int GROUP, typename Shape>
+__global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call a)
 {
     typedef Storage<DT> T;
-    typedef TileStage<DT, BACK, GROUP, MT, NT> Stage;
+    typedef TileStage<DT, BACK, GROUP, Shape> Stage;
+    constexpr int MT = Shape::MT, NT = Shape::NT, AHEAD = Shape::AHEAD, PIECES = Shape::PIECES;
     constexpr bool HALF = DT == NOVA_F16 && !BACK;
-    constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP, VERSIONS = Stage::VERSIONS;
-    constexpr int PLANE = MT * 16 * 256, LDS_STAGE = VERSIONS * P * PLANE;            // bytes
-    static_assert(AHEAD % 2 == 0, "two stages in LDS");
+    constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP, VERSIONS = Shape::template versions<BACK, GROUP>;
+    static_assert(VERSIONS == 1 || NT * 16 <= GROUP, "a wave's columns lie in one group");
+    constexpr int PLANE = Shape::ROWS * 256, LDS_STAGE = VERSIONS * P * PLANE;        // bytes
     extern __shared__ char lds[];
     const Q4Layout &q = a.q;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int column_blocks = (q.row_tiles + 4 * NT - 1) / (4 * NT), row_blocks = (a.M + 16 * MT - 1) / (16 * MT);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave_row = wave / Shape::WN * (16 * MT);
+    const int column_blocks = (q.row_tiles + Shape::PANELS - 1) / Shape::PANELS, row_blocks = (a.M + Shape::ROWS - 1) / Shape::ROWS;
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
-    const int m0 = id % row_blocks * (16 * MT), tile0 = (id / row_blocks % column_blocks * 4 + wave) * NT, split = id / row_blocks / column_blocks;
+    const int m0 = id % row_blocks * Shape::ROWS, block_tile = id / row_blocks % column_blocks * Shape::PANELS, split = id / row_blocks / column_blocks;
+    const int tile0 = block_tile + wave % Shape::WN * NT;
     const int first = split * a.split_chunks, count = min(q.chunks - first, a.split_chunks);
     const T *scales = (const T *)(a.Wq + q.code_bytes);
     const Codes<HALF> codes_to_operand;
 
-    // thread t stages row t / 16 of every 16, positions 8 (t % 16) ..
+    // thread t stages row t / 16 of every THREADS / 16, positions 8 (t % 16) ..
     const int my_row = threadIdx.x / 16, my_pos = threadIdx.x % 16 * 8;
-    const T *x_row[MT], *gate_row[BACK ? MT : 1];
+    constexpr int STEP = Shape::THREADS / 16;
+    const T *x_row[PIECES], *gate_row[BACK ? PIECES : 1];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int m = min(m0 + t * 16 + my_row, a.M - 1);                  // (past the last: computed and not stored)
+    for (int t = 0; t < PIECES; ++t) {
+        const int m = min(m0 + t * STEP + my_row, a.M - 1);                // (past the last: computed and not stored)
         x_row[t] = (const T *)a.x + m * a.ldx + my_pos;
         if (BACK) gate_row[t] = (const T *)a.gate + m * a.ldgate + my_pos;
     }
@@ -197,19 +208,19 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
         const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
         if (at + kQ4Chunk <= q.reduction) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
+            for (int t = 0; t < PIECES; ++t) {
                 __builtin_memcpy(&s.x[t], x_row[t] + at, sizeof s.x[t]);
                 if (BACK && a.gate) __builtin_memcpy(&s.gate[t], gate_row[t] + at, sizeof s.x[t]);
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
+            for (int t = 0; t < PIECES; ++t) {
                 s.x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), c > 0);
                 if (BACK && a.gate) s.gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), c > 0);
             }
         }
         if constexpr (BACK) {
-            const int group = (tile0 - wave * NT) * 16 / GROUP;
+            const int group = block_tile * 16 / GROUP;
 #pragma unroll
             for (int v = 0; v < VERSIONS; ++v)
                 __builtin_memcpy(&s.row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + at + my_pos, sizeof s.row_scale[v]);
@@ -225,7 +236,7 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
 #pragma unroll
         for (int v = 0; v < VERSIONS; ++v)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
+            for (int t = 0; t < PIECES; ++t) {
                 Fragment f[P];
                 if constexpr (BACK) {
                     float d[8];
@@ -243,42 +254,53 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    *(uint4v *)(stage + (v * P + p) * PLANE + (t * 16 + my_row) * 256 + ((my_pos / 8) ^ my_row) * 16) = f[p].vec;
+                    *(uint4v *)(stage + (v * P + p) * PLANE + (t * STEP + my_row) * 256 + ((my_pos / 8) ^ (my_row % 16)) * 16) = f[p].vec;
             }
     };
 
-    float4v acc[MT][NT], part[BACK ? 1 : MT][BACK ? 1 : NT];
+    float4v acc[MT][NT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[t][n] = (float4v){0, 0, 0, 0};
-    const int version = VERSIONS > 1 ? wave * NT * 16 / GROUP : 0;
+    const int version = VERSIONS > 1 ? wave % Shape::WN * NT * 16 / GROUP : 0;
+    auto read_rows = [&](const char *stage, int w, Fragment (&rows)[MT][P]) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (wave_row + t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
+    };
     auto multiply = [&](const char *stage, const Stage &s) {
+        if constexpr (BACK) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            Fragment rows[MT][P], columns[NT];
+            for (int w = 0; w < 4; ++w) {
+                Fragment rows[MT][P];
+                read_rows(stage, w, rows);
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+                for (int n = 0; n < NT; ++n) {
+                    const Fragment columns = codes_to_operand(s.codes[n][w]);
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-                    rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
+                    for (int p = P - 1; p >= 0; --p)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) columns[n] = codes_to_operand(s.codes[n][w]);
-            if constexpr (BACK) {
+                        for (int t = 0; t < MT; ++t) acc[t][n] = mfma<false>(rows[t][p], columns, acc[t][n]);
+                }
+            }
+        } else {
+            float4v part[MT][NT];
 #pragma unroll
-                for (int p = P - 1; p >= 0; --p)
+            for (int w = 0; w < 4; ++w) {
+                Fragment rows[MT][P];
+                read_rows(stage, w, rows);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) {
+                    const Fragment columns = codes_to_operand(s.codes[n][w]);
 #pragma unroll
-                        for (int t = 0; t < MT; ++t) acc[t][n] = mfma<false>(rows[t][p], columns[n], acc[t][n]);
-            } else {
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                    for (int p = 0; p < P; ++p)
 #pragma unroll
                         for (int t = 0; t < MT; ++t)
-                            part[t][n] = mfma<HALF>(rows[t][p], columns[n], w * 32 % GROUP == 0 && p == 0 ? (float4v){0, 0, 0, 0} : part[t][n]);
+                            part[t][n] = mfma<HALF>(rows[t][p], columns, w * 32 % GROUP == 0 && p == 0 ? (float4v){0, 0, 0, 0} : part[t][n]);
+                }
                 if ((w + 1) * 32 % GROUP == 0) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -310,7 +332,7 @@ __global__ void __launch_bounds__(256) q4_tile_kernel(const Q4Call a)
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int m = m0 + t * 16 + lane / 16 * 4 + i;
+            const int m = m0 + wave_row + t * 16 + lane / 16 * 4 + i;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int column = (tile0 + n) * 16 + lane % 16;
@@ -343,21 +365,46 @@ __global__ void __launch_bounds__(256) q4_join_kernel(const Q4Call a)
 
 // How a call is cut: few rows (mt 0; nt: waves that share a tile's panels) or tiles of 16 mt rows by 64 nt columns; waves of a workgroup; pieces of the reduction.
 struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
+
+// Time of a call with tiles, in us, as it measured on layers of 1000 to 30000 columns and 500 to 25088 positions at 24 to 512 rows (to some 15 %): 2 for the launch;
+// the stages of a workgroup one after the other, each `stage` long on a compute unit of its own and `load` times that where several workgroups share one;
+// and for a cut reduction a launch and the pieces written and read.
+static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, int splits)
+{
+    const double blocks = (double)ceil_div(q.row_tiles, 4 * nt) * ceil_div(M, 16 * mt) * splits, per_cu = blocks / 256;
+    const double stage = (nt == 4 ? 1.85 : mt == 4 ? 1.05 : mt == 2 ? 0.65 : 0.45) * (dtype == NOVA_F32 ? 2 : 1) * (q.backward ? 1.3 : 1);
+    double load = per_cu * (mt == 4 ? 0.6 : 0.7);
+    if (nt == 4) load = per_cu <= 1 ? 1 : 1.25 * (per_cu <= 2 ? 1 : per_cu / 2);
+    if (load < 1) load = 1;
+    return 2 + ceil_div(q.chunks, splits) * stage * load + (splits > 1 ? 2.5 + (double)splits * M * q.rows * 8 / 4e6 : 0);
+}
+
 static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
 {
     Q4Shape p;
     p.splits = 1;
-    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16)) {
+    // Up to 16 rows without sharing them, where the rows' operand, read by every 16 columns, is little: 12 rows by 16384 x 4096 (100 MB of it) 12.3 us against 11.1
+    // in tiles, 8 rows 10.3 against 10.7; 16 rows by 4096 x 4096 6.0 against 8.0
+    const double operand = (double)q.row_tiles * M * q.K * dtype_size(dtype);
+    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16) && (M <= 4 || (operand < 100e6 && q.chunks >= 16))) {
         p.mt = 0;
         p.nt = q.row_tiles <= 512 ? 8 : q.row_tiles <= 2048 ? 4 : 2;
+        while (p.nt > 1 && p.nt * 2 > q.chunks) p.nt /= 2;
         p.waves = p.nt < 4 ? 4 : p.nt;
     } else {
-        p.mt = M <= 16 ? 1 : M <= 32 || dtype == NOVA_F32 ? 2 : 4;
+        // (taller tiles take more registers than there are: in binary32, and backward where the columns' scales come in two versions)
+        const int tallest = (dtype == NOVA_F32 ? 2 : 4) / (q.backward && q.group == 32 ? 2 : 1);
+        p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+        if (p.mt > tallest) p.mt = tallest;
         p.nt = q.backward && q.group < 128 ? 1 : 2;
         p.waves = 4;
-        const int64_t blocks = (int64_t)ceil_div(q.row_tiles, 4 * p.nt) * ceil_div(M, 16 * p.mt);
-        if (blocks < 256) p.splits = (int)(512 / blocks);
-        if (p.splits > ceil_div(q.chunks, 4)) p.splits = ceil_div(q.chunks, 4);
+        double least = q4_tile_time(M, q, dtype, p.mt, p.nt, 1);
+        const int narrow = p.nt;
+        for (int nt = narrow; nt <= (p.mt == 4 && !q.backward && q.group == 128 ? 4 : narrow); nt *= 2)
+            for (int splits = 1; splits <= 32 && splits <= q.chunks; ++splits) {
+                const double time = q4_tile_time(M, q, dtype, p.mt, nt, splits);
+                if (time < least) least = time, p.nt = nt, p.splits = splits;
+            }
     }
     p.split_chunks = ceil_div(q.chunks, p.splits);
     p.splits = ceil_div(q.chunks, p.split_chunks);
@@ -389,21 +436,24 @@ static int join(const Q4Call &a, hipStream_t s)
     return (int)hipGetLastError();
 }
 
-template <int DT, bool BACK, int GROUP, int MT, int NT, int AHEAD>
+template <int DT, bool BACK, int GROUP, typename Shape>
 static int run_tiles(const Q4Call &a, hipStream_t s)
 {
-    const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, 4 * NT) * a.splits;
-    int64_t tiles = ((int64_t)1 << 31) / 256 / columns;                      // rows in pieces that keep a launch below 2^31 threads
+    const auto kernel = q4_tile_kernel<DT, BACK, GROUP, Shape>;
+    constexpr unsigned lds = Shape::template lds_bytes<DT, BACK, GROUP>;
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    if (lds > 64 * 1024) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, Shape::PANELS) * a.splits;
+    int64_t tiles = ((int64_t)1 << 31) / Shape::THREADS / columns;           // rows in pieces that keep a launch below 2^31 threads
     if (tiles < 1) tiles = 1;
-    const int64_t M = a.M, step = tiles * 16 * MT;
-    constexpr unsigned lds = 2 * TileStage<DT, BACK, GROUP, MT, NT>::VERSIONS * kPieces<DT, BACK> * MT * 16 * 256;
+    const int64_t M = a.M, step = tiles * Shape::ROWS;
     for (int64_t m0 = 0; m0 < M; m0 += step) {
         Q4Call part = a;
         part.M = (int)(M - m0 < step ? M - m0 : step);
         part.x = (const Storage<DT> *)a.x + m0 * a.ldx;
         if (a.gate) part.gate = (const Storage<DT> *)a.gate + m0 * a.ldgate;
         part.out = (Storage<DT> *)a.out + m0 * a.ldout;
-        q4_tile_kernel<DT, BACK, GROUP, MT, NT, AHEAD><<<(unsigned)(columns * ceil_div(part.M, 16 * MT)), 256, lds, s>>>(part);
+        kernel<<<(unsigned)(columns * ceil_div(part.M, Shape::ROWS)), Shape::THREADS, lds, s>>>(part);
         NOVA_HIP_TRY(hipGetLastError());
         if (int err = join<DT>(part, s)) return err;
     }
@@ -432,15 +482,13 @@ static int run_group(const Q4Call &a, const Q4Shape &p, hipStream_t s)
         }
     }
     constexpr int NT = BACK && GROUP < 128 ? 1 : 2;
-#ifdef Q4_TUNE
-    if (p.waves == 2 && p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT, 2>(a, s);
-    if (p.waves == 2 && p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT, 2>(a, s);
-    if constexpr (DT != NOVA_F32) if (p.waves == 2) return run_tiles<DT, BACK, GROUP, 4, NT, 2>(a, s);
-#endif
-    if (p.mt == 1) return run_tiles<DT, BACK, GROUP, 1, NT, 4>(a, s);
-    if (p.mt == 2) return run_tiles<DT, BACK, GROUP, 2, NT, 4>(a, s);
-    if constexpr (DT != NOVA_F32) return run_tiles<DT, BACK, GROUP, 4, NT, 4>(a, s);
-    return (int)hipErrorInvalidValue;
+    if constexpr (DT != NOVA_F32 && !BACK && GROUP == 128)
+        if (p.nt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, 4, 1, 4, 2>>(a, s);
+    if constexpr (DT != NOVA_F32 && !(BACK && GROUP == 32))
+        if (p.mt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, NT, 1, 4, 2>>(a, s);
+    if constexpr (DT != NOVA_F32 || !(BACK && GROUP == 32))
+        if (p.mt == 2) return run_tiles<DT, BACK, GROUP, Tile<2, NT, 1, 4, DT == NOVA_F32 ? 2 : 4>>(a, s);
+    return run_tiles<DT, BACK, GROUP, Tile<1, NT, 1, 4, 2>>(a, s);
 }
 
 template <int DT, bool BACK>
