@@ -187,7 +187,9 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
     const int m0 = id % row_blocks * Shape::ROWS, block_tile = id / row_blocks % column_blocks * Shape::PANELS, split = id / row_blocks / column_blocks;
     const int tile0 = block_tile + wave % Shape::WN * NT;
-    const int first = split * a.split_chunks, count = min(q.chunks - first, a.split_chunks);
+    // whole panels, and the one that ends inside
+    const int whole = q.reduction / kQ4Chunk, first = split * a.split_chunks, count = min(whole - first, a.split_chunks);
+    const bool ragged = whole < q.chunks && split == a.splits - 1;
     const T *scales = (const T *)(a.Wq + q.code_bytes);
     const Codes<HALF> codes_to_operand;
 
@@ -204,26 +206,12 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     const char *panels[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) panels[n] = a.Wq + (size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks * kQ4PanelBytes;       // (as above)
-    auto load = [&](int i, Stage &s) {
-        const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
-        if (at + kQ4Chunk <= q.reduction) {
-#pragma unroll
-            for (int t = 0; t < PIECES; ++t) {
-                __builtin_memcpy(&s.x[t], x_row[t] + at, sizeof s.x[t]);
-                if (BACK && a.gate) __builtin_memcpy(&s.gate[t], gate_row[t] + at, sizeof s.x[t]);
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < PIECES; ++t) {
-                s.x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), c > 0);
-                if (BACK && a.gate) s.gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), c > 0);
-            }
-        }
+    auto load_panels = [&](int c, Stage &s) {
         if constexpr (BACK) {
             const int group = block_tile * 16 / GROUP;
 #pragma unroll
             for (int v = 0; v < VERSIONS; ++v)
-                __builtin_memcpy(&s.row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + at + my_pos, sizeof s.row_scale[v]);
+                __builtin_memcpy(&s.row_scale[v], scales + (size_t)min(group + v, q.groups - 1) * q.scale_pitch + c * kQ4Chunk + my_pos, sizeof s.row_scale[v]);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -231,6 +219,15 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
             if constexpr (!BACK)
                 s.scale[n] = ((const Several<T, SCALES> *)scales)[((size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks + c) * kQ4Rows + lane % 16u];
         }
+    };
+    auto load = [&](int i, Stage &s) {
+        const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) {
+            __builtin_memcpy(&s.x[t], x_row[t] + at, sizeof s.x[t]);
+            if (BACK && a.gate) __builtin_memcpy(&s.gate[t], gate_row[t] + at, sizeof s.x[t]);
+        }
+        load_panels(c, s);
     };
     auto fill = [&](char *stage, const Stage &s) {
 #pragma unroll
@@ -316,8 +313,21 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     };
 
     Stage stage[AHEAD];
-    static_for<AHEAD - 1>([&](auto I) { load(I, stage[I]); });
-    fill(lds, stage[0]);
+    if (count > 0) static_for<AHEAD - 1>([&](auto I) { load(I, stage[I]); });
+    if (ragged) {
+        Stage &s = stage[AHEAD - 1];
+        const int at = whole * kQ4Chunk;
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) {
+            s.x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), whole > 0);
+            if (BACK && a.gate) s.gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), whole > 0);
+        }
+        load_panels(whole, s);
+        fill(lds + LDS_STAGE, s);
+        __syncthreads();
+        multiply(lds + LDS_STAGE, s);
+    }
+    if (count > 0) fill(lds, stage[0]);
     for (int i = 0; i < count; i += AHEAD)
         static_for<AHEAD>([&](auto I) {
             if (i + I < count) {
