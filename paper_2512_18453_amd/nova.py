@@ -473,22 +473,23 @@ def _any_dtype_code(dtype):
 
 
 def _rows(t, shape, dtype, what):
-    """(pointer, elements from row to row) of a matrix on the device whose rows lie whole, anywhere apart."""
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape or (t.stride(1) != 1 and t.shape[1] > 1):
+    """(address, elements from row to row) of a matrix on the device whose rows lie whole, anywhere apart."""
+    step, unit = t.stride() if t.dim() == 2 else (0, 0)
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or (unit != 1 and shape[1] > 1):
         raise ValueError(f"{what}: expected a device tensor {shape} of {dtype} with elements of a row side by side")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+    return t.data_ptr(), step
 
 
 def _flat(t, count, dtype, what):
     if not t.is_cuda or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous device tensor of {count} {dtype}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _bytes(t, what):
     if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous device tensor of bytes")
-    return ctypes.c_void_p(t.data_ptr()), t.numel()
+    return t.data_ptr(), t.numel()
 
 
 def nova_q4_bytes(N, K, group, dtype, direction=NOVA_Q4_FORWARD):

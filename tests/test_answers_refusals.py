@@ -118,3 +118,10 @@ def test_no_rows_need_no_workspace(direction):
     for N, K in ((1, 1), (20, 40), (4096, 25088)):
         assert nova.lib().nova_q4_linear_workspace_bytes(0, N, K, 32, F16, direction) == 0
     assert nova.lib().nova_logprobs_workspace_bytes(0, 200000, 5, F16) == 0
+
+
+def test_binding_wants_matrices():
+    with pytest.raises(ValueError):
+        nova._rows(torch.zeros(40), (1, 40), torch.float32, "x")
+    with pytest.raises(ValueError):
+        nova._rows(torch.zeros((40, 2)).T, (2, 40), torch.float32, "x")
