@@ -415,7 +415,7 @@ int nova_q4_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t
 /*
  * Log probabilities of given tokens (classes), entropy and the most probable alternatives, one row of logits x [rows][V] at a time:
  *     M = max x_v,  L = ln sum_v exp(scale (x_v - M))  over the allowed entries,   ln p_v = scale (x_v - M) - L.
- * logits: device, dtype, `stride` elements from row to row (>= V); scale: finite and > 0 (the inverse of a temperature).
+ * logits: device, dtype, `stride` elements from row to row (>= V); scale: > 0, at most 1e38 (the inverse of a temperature).
  * mask: device bytes, nonzero = allowed, [rows][V] with mask_stride >= V, or one row for all with mask_stride 0; NULL: all allowed.  What a
  * masked entry holds does not matter (NaN and infinities included).
  * targets: device int64 [rows] or NULL.  Outputs (device; any but stats may be NULL; top_logprobs and top_ids only with top = 0):

@@ -1,6 +1,5 @@
 // The device-facing entry points of libnova: argument checks, tensor geometry, the slab loop of
 // nova_winograd_conv2d.  All device work is done by the launchers in the .hip files.
-#include <cmath>
 #include <cstring>
 
 #include "internal.hpp"
@@ -505,6 +504,9 @@ extern "C" int nova_q4_linear_backward(const void *dy, int64_t lddy, const void 
 
 // ---- log probabilities ----
 
+// scale times log2 e is formed in binary32
+static bool scale_ok(float scale) { return scale > 0.0f && scale <= 1e38f; }
+
 static bool logprobs_ok(int rows, int V, int top, int dtype) { return rows >= 0 && V >= 1 && top >= 0 && top <= 64 && any_dtype_ok(dtype); }
 
 extern "C" size_t nova_logprobs_workspace_bytes(int rows, int V, int top, int dtype)
@@ -517,7 +519,7 @@ extern "C" int nova_logprobs(const void *logits, int64_t stride, const int64_t *
                              float scale, int top, int dtype, float *logprob, float *entropy, float *stats, float *top_logprobs, int64_t *top_ids,
                              void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!logprobs_ok(rows, V, top, dtype) || !std::isfinite(scale) || !(scale > 0.0f) || (logprob && !targets)) return NOVA_EINVAL;
+    if (!logprobs_ok(rows, V, top, dtype) || !scale_ok(scale) || (logprob && !targets)) return NOVA_EINVAL;
     if (rows == 0) return NOVA_OK;
     if (!read_rows_ok(logits, stride, rows, V) || (mask && !read_rows_ok(mask, mask_stride, rows, V)) || !stats) return NOVA_EINVAL;
     if (top > 0 && (!top_logprobs || !top_ids)) return NOVA_EINVAL;
@@ -532,7 +534,7 @@ extern "C" int nova_logprobs_backward(const void *logits, int64_t stride, const 
                                       const float *entropy, const float *g_entropy, const uint8_t *mask, int64_t mask_stride, int rows, int V,
                                       float scale, int dtype, void *dlogits, int64_t dstride, void *stream)
 {
-    if (!logprobs_ok(rows, V, 0, dtype) || !std::isfinite(scale) || !(scale > 0.0f) || (g_logprob && !targets) || (g_entropy && !entropy))
+    if (!logprobs_ok(rows, V, 0, dtype) || !scale_ok(scale) || (g_logprob && !targets) || (g_entropy && !entropy))
         return NOVA_EINVAL;
     if (rows == 0) return NOVA_OK;
     if (!read_rows_ok(logits, stride, rows, V) || !stats || (mask && !read_rows_ok(mask, mask_stride, rows, V)) ||

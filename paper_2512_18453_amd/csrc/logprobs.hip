@@ -5,8 +5,8 @@
 // Rows are cut into slices where there are few of them; a second kernel joins the slices.
 //
 // Alternatives.  The pass leaves the largest logit of every lane and of every cell, the up to kCells parts that a lane's share is cut into.  If `least` is the
-// top-th largest of the lane maxima, the slice holds `top` logits that reach it, so only cells whose maximum does are read again: with 131072
-// logits and 8 alternatives some dozen cells of 4096.  What reaches `least` in them is sorted by one wave.  Where that is more than kCandidates (equal logits over all of a row) or a NaN stands in the row, the waves go over the slice once more, keeping sorted lists.
+// top-th largest of the lane maxima, the slice holds `top` logits that reach it, so only cells whose maximum does are read again (with 131072
+// logits and 8 alternatives some dozen of 4096; a slice of one step has its logits still in registers).  What reaches `least` in them is sorted by one wave.  Where that is more than kCandidates (equal logits over all of a row) or a NaN stands in the row, the waves go over the slice once more, keeping sorted lists.
 #include "q4_common.hpp"
 
 namespace nova {
@@ -34,6 +34,8 @@ __device__ __forceinline__ float value_of_rank(unsigned r)
 {
     return r == 0xff800001u ? __builtin_nanf("") : r == 0 ? -INFINITY : __uint_as_float(r & 0x80000000u ? r & 0x7fffffffu : ~r);
 }
+// The lowest bit that tells two values of a type apart
+template <int DT> constexpr int kRankBits = DT == NOVA_BF16 ? 16 : DT == NOVA_F16 ? 13 : 0;
 __device__ __forceinline__ rank_t rank_of(unsigned value, unsigned index) { return value ? (rank_t)value << 32 | (0xffffffffu - index) : 0; }
 
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -127,12 +129,12 @@ struct Best {
     }
 };
 
-// The largest rank (of BITS bits) that at least `count` of the lanes' N ranks reach, from the top bit down
-template <int BITS, typename R, int N>
+// The largest rank that at least `count` of the lanes' N ranks reach, from the top bit down to bit LOWEST
+template <int LOWEST, typename R, int N>
 __device__ __forceinline__ R reached_by(const R (&rank)[N], int count)
 {
     R t = 0;
-    for (int bit = BITS - 1; bit >= 0; --bit) {
+    for (int bit = (int)sizeof(R) * 8 - 1; bit >= LOWEST; --bit) {
         const R next = t | (R)1 << bit;
         int reaching = 0;
 #pragma unroll
@@ -151,7 +153,7 @@ __device__ __forceinline__ rank_t best_of(const rank_t *candidates, int count, i
     rank_t all[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) all[i] = i * 64 + lane < count ? candidates[i * 64 + lane] : 0;
-    const rank_t least = reached_by<64>(all, top);
+    const rank_t least = reached_by<0>(all, top);
     int kept = 0;
     scratch[lane] = 0;
 #pragma unroll
@@ -290,8 +292,8 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
     float in_cell = -INFINITY;
     if (TOP && threadIdx.x == 0) found_cells = found = 0;
     fetch(begin);
+    float v[kVectors * 8];
     for (unsigned chunk = 0, left = per_cell, cell = 0; chunk < chunks; ++chunk) {
-        float v[kVectors * 8];
 #pragma unroll
         for (int i = 0; i < kVectors * 8; ++i) v[i] = next[i / 8][i % 8];
         if (chunk + 1 < chunks) fetch(begin + (chunk + 1) * IN_HAND);
@@ -328,8 +330,20 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
         unsigned ranks[WAVES];
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) ranks[w] = lane_ranks[w * 64 + lane];
-        const float least = value_of_rank(reached_by<32>(ranks, a.top));
-        if (!again) {
+        const float least = value_of_rank(reached_by<kRankBits<DT>>(ranks, a.top));
+        // a lane's logits that reach `least`, of which bit i of `reaching` says that logit(i) does, to the candidates
+        auto note = [&](unsigned reaching, auto &&logit, auto &&index) {
+            int place = reaching ? atomicAdd(&found, __popc(reaching)) : 0;
+            static_for<kVectors * 8>([&](auto I) {
+                if ((reaching >> I & 1) && place < kCandidates) candidates[place++] = rank_of(value_rank(logit(I)), index(I));
+            });
+        };
+        if (WAVES > 1 && !again && chunks == 1) {  // they are still there (one wave is sooner through with reading a few again)
+            unsigned reaching = 0;
+#pragma unroll
+            for (int i = 0; i < kVectors * 8; ++i) reaching |= (unsigned)(v[i] >= least && v[i] != -INFINITY) << i;
+            note(reaching, [&](int i) { return v[i]; }, [&](int i) { return begin + i / 8 * STRIDE + threadIdx.x * 8 + i % 8; });
+        } else if (!again) {
             for (unsigned i = 0; i < used; ++i) {
                 const float largest = cell_largest[i][threadIdx.x];
                 if (largest >= least && largest != -INFINITY) {
@@ -339,10 +353,8 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
             }
             __syncthreads();
             again = found_cells > kCandidates;
-        }
-        if (!again) {
             const unsigned pieces = per_cell * kVectors;
-            const uint64_t items = (uint64_t)found_cells * pieces;
+            const uint64_t items = again ? 0 : (uint64_t)found_cells * pieces;
             for (uint64_t item = threadIdx.x; item < items; item += THREADS) {
                 const unsigned cell = cells[item / pieces], piece = (unsigned)(item % pieces);
                 const unsigned chunk = cell / THREADS * per_cell + piece / kVectors;
@@ -350,18 +362,14 @@ __global__ void __launch_bounds__(WAVES * 64) logprobs_kernel(const LogprobsArgs
                 if (chunk >= chunks || at >= end) continue;
                 Piece p;
                 load_piece(at, p);
+                unsigned reaching = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = p[e];
-                    if (v >= least && v != -INFINITY) {
-                        const int place = atomicAdd(&found, 1);
-                        if (place < kCandidates) candidates[place] = rank_of(value_rank(v), at + e);
-                    }
-                }
+                for (int e = 0; e < 8; ++e) reaching |= (unsigned)(p[e] >= least && p[e] != -INFINITY) << e;
+                note(reaching, [&](int e) { return p[e % 8]; }, [&](int e) { return at + e % 8; });
             }
-            __syncthreads();
-            again = found > kCandidates;
         }
+        __syncthreads();
+        again = again || found > kCandidates;
         if (!again) {
             if (wave == 0) best.mine = sorted_best(candidates, found, a.top, lists[0]);
         } else {

@@ -4,13 +4,6 @@
 
 namespace nova {
 
-// Row (of the layout) and position of the reduction -> output n and input k
-__device__ __forceinline__ void q4_element(const Q4Layout &q, int row, int pos, int &n, int &k)
-{
-    n = q.backward ? pos : row;
-    k = q.backward ? row : pos;
-}
-
 // Index of the scale of output n and group g
 __device__ __forceinline__ size_t q4_scale_index(const Q4Layout &q, int n, int g)
 {
@@ -19,37 +12,42 @@ __device__ __forceinline__ size_t q4_scale_index(const Q4Layout &q, int n, int g
     return ((size_t)(n / kQ4Rows) * q.scale_pitch + g / per_chunk * per_chunk) * kQ4Rows + n % kQ4Rows * per_chunk + g % per_chunk;
 }
 
-template <int DT, bool QUANTIZE>
+// Scale idx of the layout -> its output and group; false for padding
+__device__ __forceinline__ bool q4_scale_at(const Q4Layout &q, size_t idx, int &n, int &g)
+{
+    if (q.backward) {
+        n = (int)(idx % q.scale_pitch);
+        g = (int)(idx / q.scale_pitch);
+    } else {
+        const int per_chunk = kQ4Chunk / q.group;
+        const size_t chunk = idx / per_chunk / kQ4Rows;
+        n = (int)(chunk / q.chunks) * kQ4Rows + (int)(idx / per_chunk % kQ4Rows);
+        g = (int)(chunk % q.chunks) * per_chunk + (int)(idx % per_chunk);
+    }
+    return n < q.N && g < q.groups;
+}
+
+// Scales as given, or of weights: LANES = group / 8 lanes read a group, eight weights each
+template <int DT, int LANES>
 __global__ void __launch_bounds__(256) q4_scales_kernel(const Storage<DT> *__restrict__ src, Storage<DT> *__restrict__ scales, const Q4Layout q)
 {
-    for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < q.scale_count; idx += (size_t)gridDim.x * 256) {
+    const size_t step = (size_t)gridDim.x * (256 / LANES);
+    for (size_t idx = (size_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; idx < q.scale_count; idx += step) {
         int n, g;
-        if (q.backward) {
-            n = (int)(idx % q.scale_pitch);
-            g = (int)(idx / q.scale_pitch);
+        const bool real = q4_scale_at(q, idx, n, g);
+        if constexpr (LANES == 1) {
+            scales[idx] = real ? src[(size_t)n * q.groups + g] : (Storage<DT>)0.0f;
         } else {
-            const int per_chunk = kQ4Chunk / q.group;
-            const size_t chunk = idx / per_chunk / kQ4Rows;
-            n = (int)(chunk / q.chunks) * kQ4Rows + (int)(idx / per_chunk % kQ4Rows);
-            g = (int)(chunk % q.chunks) * per_chunk + (int)(idx % per_chunk);
+            const int lane = threadIdx.x % LANES, first = g * q.group + lane * 8;
+            const Eight<Storage<DT>> w = load_eight(src + (size_t)n * q.K + first, real ? q.K - first : 0, first >= 8);
+            unsigned largest = 0;                  // as bits: infinity is above every number, NaN above infinity
+#pragma unroll
+            for (int i = 0; i < 8; ++i) largest = max(largest, __float_as_uint((float)w.v[i]) & 0x7fffffffu);
+#pragma unroll
+            for (int across = LANES / 2; across; across /= 2) largest = max(largest, (unsigned)__shfl_xor((int)largest, across));
+            const float s = largest < 0x7f800000u ? __uint_as_float(largest) / 7.0f : __builtin_nanf("");
+            if (lane == 0) scales[idx] = (Storage<DT>)(real ? s : 0.0f);
         }
-        Storage<DT> s = (Storage<DT>)0.0f;
-        if (n < q.N && g < q.groups) {
-            if constexpr (QUANTIZE) {
-                const Storage<DT> *w = src + (size_t)n * q.K;
-                const int end = min(q.K, (g + 1) * q.group);
-                float largest = 0.0f;
-                for (int k = g * q.group; k < end; ++k) {
-                    const float a = fabsf((float)w[k]);
-                    largest = (a > largest || a != a) ? a : largest;
-                    if (largest != largest) break;
-                }
-                s = (Storage<DT>)(largest - largest == 0.0f ? largest / 7.0f : __builtin_nanf(""));     // an infinity makes NaN too
-            } else {
-                s = src[(size_t)n * q.groups + g];
-            }
-        }
-        scales[idx] = s;
     }
 }
 
@@ -59,26 +57,39 @@ __global__ void __launch_bounds__(256) q4_codes_kernel(const void *__restrict__ 
 {
     const size_t total = q.code_bytes / 4;
     for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (size_t)gridDim.x * 256) {
-        const int w = idx % 4, lane = idx / 4 % 64;
+        // the words of a panel in the order in which neighbouring threads read neighbouring weights: along a row forward, across the rows backward
+        const int in_panel = idx % 256;
+        const int w = q.backward ? in_panel / 64 : in_panel % 4, lane = q.backward ? in_panel % 64 : in_panel / 4;
         const size_t panel = idx / 256;
         const int row = (int)(panel / q.chunks) * kQ4Rows + lane % 16;
         const int first = (int)(panel % q.chunks) * kQ4Chunk + 32 * w + 8 * (lane / 16);
-        unsigned word = 0;
-        for (int v = 0; v < 8; ++v) {
-            if (row >= q.rows || first + v >= q.reduction) break;
-            int n, k, code;
-            q4_element(q, row, first + v, n, k);
-            const size_t at = (size_t)n * q.K + k;
-            if constexpr (QUANTIZE) {
-                const float s = (float)scales[q4_scale_index(q, n, k / q.group)];
-                const float c = s > 0.0f ? rintf((float)((const Storage<DT> *)src)[at] / s) : 0.0f;        // s NaN or 0: code 0
-                code = (int)fminf(fmaxf(c, -8.0f), 7.0f);
-            } else {
-                code = min(max((int)((const int8_t *)src)[at], -8), 7);
-            }
-            word |= ((unsigned)code & 15u) << (4 * (v / 2) + 16 * (v % 2));
+        const int count = row < q.rows ? min(q.reduction - first, 8) : 0;
+        typedef std::conditional_t<QUANTIZE, Storage<DT>, int8_t> S;
+        S v[8];
+        const size_t at = q.backward ? (size_t)first * q.K + row : (size_t)row * q.K + first, step = q.backward ? q.K : 1;
+        if (count == 8 && !q.backward) {
+            __builtin_memcpy(v, (const S *)src + at, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < count ? ((const S *)src)[at + i * step] : (S)0;
         }
-        words[idx] = word;
+        unsigned word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int code = 0;
+            if constexpr (QUANTIZE) {
+                if (i < count) {
+                    // (eight positions lie in one group forward; backward they are eight outputs of one input)
+                    const float s = (float)scales[q4_scale_index(q, q.backward ? first + i : row, (q.backward ? row : first) / q.group)];
+                    const float c = s > 0.0f ? rintf((float)v[i] / s) : 0.0f;                                  // s NaN or 0: code 0
+                    code = (int)fminf(fmaxf(c, -8.0f), 7.0f);
+                }
+            } else {
+                code = min(max((int)v[i], -8), 7);
+            }
+            word |= ((unsigned)code & 15u) << (4 * (i / 2) + 16 * (i % 2));
+        }
+        words[panel * 256 + lane * 4 + w] = word;
     }
 }
 
@@ -108,7 +119,11 @@ template <int DT, bool QUANTIZE>
 static int lay_out(const void *src, const void *scale_src, const Q4Layout &q, void *Wq, hipStream_t s)
 {
     Storage<DT> *scales = (Storage<DT> *)((char *)Wq + q.code_bytes);
-    q4_scales_kernel<DT, QUANTIZE><<<q4_blocks(q.scale_count), 256, 0, s>>>((const Storage<DT> *)scale_src, scales, q);
+    const Storage<DT> *from = (const Storage<DT> *)scale_src;
+    if (!QUANTIZE) q4_scales_kernel<DT, 1><<<q4_blocks(q.scale_count), 256, 0, s>>>(from, scales, q);
+    else if (q.group == 32) q4_scales_kernel<DT, 4><<<q4_blocks(q.scale_count * 4), 256, 0, s>>>(from, scales, q);
+    else if (q.group == 64) q4_scales_kernel<DT, 8><<<q4_blocks(q.scale_count * 8), 256, 0, s>>>(from, scales, q);
+    else q4_scales_kernel<DT, 16><<<q4_blocks(q.scale_count * 16), 256, 0, s>>>(from, scales, q);
     NOVA_HIP_TRY(hipGetLastError());
     q4_codes_kernel<DT, QUANTIZE><<<q4_blocks(q.code_bytes / 4), 256, 0, s>>>(src, scales, (unsigned *)Wq, q);
     return (int)hipGetLastError();

@@ -125,3 +125,11 @@ def test_binding_wants_matrices():
         nova._rows(torch.zeros(40), (1, 40), torch.float32, "x")
     with pytest.raises(ValueError):
         nova._rows(torch.zeros((40, 2)).T, (2, 40), torch.float32, "x")
+
+
+def test_largest_scale():
+    # (its product with log2 e has to be a number)
+    call = [AT, 10, None, None, 0, 2, 10, 1.1e38, 0, F16, None, None, AT, None, None, None, 0, None]
+    assert nova.lib().nova_logprobs(*call) == EINVAL
+    back = [AT, 10, AT, None, None, None, None, None, 0, 2, 10, 1.1e38, F16, AT, 10, None]
+    assert nova.lib().nova_logprobs_backward(*back) == EINVAL
