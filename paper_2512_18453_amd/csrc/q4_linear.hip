@@ -4,12 +4,8 @@
 // registers (q4_common.hpp).
 //   forward   a group's products are summed on the matrix unit with the codes as integers and the sum is scaled in binary32
 //   backward  the scales run along the reduction, so they go to the other operand: d * s in binary32, in two (three) bfloat16 pieces
-// Two kernels: up to 16 rows (q4_few_rows_kernel) the codes' bytes bind and nothing else; more rows (q4_tile_kernel) share the panels through LDS.
+// Two kernels: for up to 16 rows (q4_few_rows_kernel) the codes' bytes bind and nothing else; more rows (q4_tile_kernel) are shared by four waves through LDS.
 // Where the result's tiles give too few workgroups, the reduction is cut over workgroups too; a third kernel adds the pieces in order.
-#ifdef Q4_TUNE
-#include <cstdio>
-#include <cstdlib>
-#endif
 #include "q4_common.hpp"
 
 namespace nova {
@@ -48,9 +44,10 @@ __device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, 
 // ---- forward, up to 16 rows ----
 //
 // A wave makes 16 columns for all rows; `sharing` waves of a workgroup take the panels of the same columns in turn and add up through LDS in the order of their
-// numbers.  Bound by the codes' bytes: a wave has kAhead panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
-// along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it (read from memory as the
-// matrix unit takes it, 16 rows side by side, a load takes four times as long: each four lanes lie in four cache lines).
+// numbers.  Bound by the codes' bytes: a wave has AHEAD panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
+// along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it: read from memory as the
+// matrix unit takes it, 16 rows side by side, each four lanes lie in four cache lines, and one row of 25088 by 4096 took 16.5 us, 16 rows 27.  Now one row takes
+// 10.7 us (51 MB of codes, 5.1 TB/s), 8 rows 15.7: every 16 columns read all rows once more from L2.  The codes are streamed past it (12.2 us without).
 template <int DT, int GROUP, int QUADS>
 struct FewRowsStage {
     uint4v codes;
@@ -150,14 +147,19 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 
 // ---- more rows, and the gradient ----
 //
-// A workgroup of WM x WN waves makes 16 MT WM rows by 16 NT WN columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces,
-// backward with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), a wave reads its rows of it and multiplies its own NT
-// panels.  Two such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks
-// are stored at block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
-template <int MT_, int NT_, int WM_, int WN_, int AHEAD_>
+// A workgroup of four waves makes 16 MT rows by 64 NT columns: the rows' operand of 128 positions goes through LDS (as the matrix unit takes it: pieces, backward
+// with the scales multiplied in, once for each of the VERSIONS groups that the columns lie in), every wave reads it whole and multiplies its own NT panels. Two
+// such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks are stored at
+// block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
+//
+// Many rows: 1024 by 8192 x 8192 in bfloat16 150 us, 917 TFLOP/s where a large library product of that type reaches 1211.  A panel is made into operands once per 64 rows, three
+// vector instructions for each of its matrix instructions, so both units are busy (without making operands it took 124 us); 256 columns halve the LDS reads of 128 (162 us); eight waves
+// on 128 rows were slower (174 to 227), as all of them wait at one barrier.  Few tiles: 32 rows of the first layer behind the VGG stack (51 MB) 20.8 us, of which
+// the second launch and 8 MB of pieces take 6; four groups of waves per workgroup that shared a tile's stages instead of most of the cut gained nothing.
+// Gradient: twice the products, 512 rows by 4096 x 16384 152 us.
+template <int MT_, int NT_, int AHEAD_>
 struct Tile {
-    static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, AHEAD = AHEAD_, THREADS = 64 * WM * WN, ROWS = 16 * MT * WM, PANELS = NT * WN;
-    static constexpr int PIECES = ROWS * 16 / THREADS;                       // 8-element pieces of a stage that a thread loads
+    static constexpr int MT = MT_, NT = NT_, AHEAD = AHEAD_, ROWS = 16 * MT, PANELS = 4 * NT;
     template <bool BACK, int GROUP> static constexpr int versions = BACK && 16 * PANELS > GROUP ? 16 * PANELS / GROUP : 1;
     template <int DT, bool BACK, int GROUP> static constexpr unsigned lds_bytes = 2 * versions<BACK, GROUP> * kPieces<DT, BACK> * ROWS * 256;
     static_assert(AHEAD % 2 == 0, "two stages in LDS");
@@ -165,41 +167,40 @@ struct Tile {
 
 template <int DT, bool BACK, int GROUP, typename Shape>
 struct TileStage {
-    Eight<Storage<DT>> x[Shape::PIECES], gate[BACK ? Shape::PIECES : 1], row_scale[Shape::template versions<BACK, GROUP>];
+    Eight<Storage<DT>> x[Shape::MT], gate[BACK ? Shape::MT : 1], row_scale[Shape::template versions<BACK, GROUP>];
     uint4v codes[Shape::NT];
     Several<Storage<DT>, kQ4Chunk / GROUP> scale[BACK ? 1 : Shape::NT];
 };
 
 template <int DT, bool BACK, int GROUP, typename Shape>
-__global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call a)
+__global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 {
     typedef Storage<DT> T;
     typedef TileStage<DT, BACK, GROUP, Shape> Stage;
-    constexpr int MT = Shape::MT, NT = Shape::NT, AHEAD = Shape::AHEAD, PIECES = Shape::PIECES;
+    constexpr int MT = Shape::MT, NT = Shape::NT, AHEAD = Shape::AHEAD;
     constexpr bool HALF = DT == NOVA_F16 && !BACK;
     constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP, VERSIONS = Shape::template versions<BACK, GROUP>;
     static_assert(VERSIONS == 1 || NT * 16 <= GROUP, "a wave's columns lie in one group");
     constexpr int PLANE = Shape::ROWS * 256, LDS_STAGE = VERSIONS * P * PLANE;        // bytes
     extern __shared__ char lds[];
     const Q4Layout &q = a.q;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave_row = wave / Shape::WN * (16 * MT);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int column_blocks = (q.row_tiles + Shape::PANELS - 1) / Shape::PANELS, row_blocks = (a.M + Shape::ROWS - 1) / Shape::ROWS;
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
     const int m0 = id % row_blocks * Shape::ROWS, block_tile = id / row_blocks % column_blocks * Shape::PANELS, split = id / row_blocks / column_blocks;
-    const int tile0 = block_tile + wave % Shape::WN * NT;
+    const int tile0 = block_tile + wave * NT;
     // whole panels, and the one that ends inside
     const int whole = q.reduction / kQ4Chunk, first = split * a.split_chunks, count = min(whole - first, a.split_chunks);
     const bool ragged = whole < q.chunks && split == a.splits - 1;
     const T *scales = (const T *)(a.Wq + q.code_bytes);
     const Codes<HALF> codes_to_operand;
 
-    // thread t stages row t / 16 of every THREADS / 16, positions 8 (t % 16) ..
+    // thread t stages row t / 16 of every 16, positions 8 (t % 16) ..
     const int my_row = threadIdx.x / 16, my_pos = threadIdx.x % 16 * 8;
-    constexpr int STEP = Shape::THREADS / 16;
-    const T *x_row[PIECES], *gate_row[BACK ? PIECES : 1];
+    const T *x_row[MT], *gate_row[BACK ? MT : 1];
 #pragma unroll
-    for (int t = 0; t < PIECES; ++t) {
-        const int m = min(m0 + t * STEP + my_row, a.M - 1);                // (past the last: computed and not stored)
+    for (int t = 0; t < MT; ++t) {
+        const int m = min(m0 + t * 16 + my_row, a.M - 1);                // (past the last: computed and not stored)
         x_row[t] = (const T *)a.x + m * a.ldx + my_pos;
         if (BACK) gate_row[t] = (const T *)a.gate + m * a.ldgate + my_pos;
     }
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     auto load = [&](int i, Stage &s) {
         const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
 #pragma unroll
-        for (int t = 0; t < PIECES; ++t) {
+        for (int t = 0; t < MT; ++t) {
             __builtin_memcpy(&s.x[t], x_row[t] + at, sizeof s.x[t]);
             if (BACK && a.gate) __builtin_memcpy(&s.gate[t], gate_row[t] + at, sizeof s.x[t]);
         }
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
 #pragma unroll
         for (int v = 0; v < VERSIONS; ++v)
 #pragma unroll
-            for (int t = 0; t < PIECES; ++t) {
+            for (int t = 0; t < MT; ++t) {
                 Fragment f[P];
                 if constexpr (BACK) {
                     float d[8];
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    *(uint4v *)(stage + (v * P + p) * PLANE + (t * STEP + my_row) * 256 + ((my_pos / 8) ^ (my_row % 16)) * 16) = f[p].vec;
+                    *(uint4v *)(stage + (v * P + p) * PLANE + (t * 16 + my_row) * 256 + ((my_pos / 8) ^ my_row) * 16) = f[p].vec;
             }
     };
 
@@ -260,13 +261,13 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[t][n] = (float4v){0, 0, 0, 0};
-    const int version = VERSIONS > 1 ? wave % Shape::WN * NT * 16 / GROUP : 0;
+    const int version = VERSIONS > 1 ? wave * NT * 16 / GROUP : 0;
     auto read_rows = [&](const char *stage, int w, Fragment (&rows)[MT][P]) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (wave_row + t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
+                rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
     };
     auto multiply = [&](const char *stage, const Stage &s) {
         if constexpr (BACK) {
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
         Stage &s = stage[AHEAD - 1];
         const int at = whole * kQ4Chunk;
 #pragma unroll
-        for (int t = 0; t < PIECES; ++t) {
+        for (int t = 0; t < MT; ++t) {
             s.x[t] = load_eight(x_row[t] + at, q.reduction - (at + my_pos), whole > 0);
             if (BACK && a.gate) s.gate[t] = load_eight(gate_row[t] + at, q.reduction - (at + my_pos), whole > 0);
         }
@@ -342,7 +343,7 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) q4_tile_kernel(const Q4Call
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int m = m0 + wave_row + t * 16 + lane / 16 * 4 + i;
+            const int m = m0 + t * 16 + lane / 16 * 4 + i;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int column = (tile0 + n) * 16 + lane % 16;
@@ -418,15 +419,6 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
     }
     p.split_chunks = ceil_div(q.chunks, p.splits);
     p.splits = ceil_div(q.chunks, p.split_chunks);
-#ifdef Q4_TUNE
-    if (const char *e = getenv("Q4SHAPE")) {
-        int mt, nt, w, s;
-        if (sscanf(e, "%d,%d,%d,%d", &mt, &nt, &w, &s) == 4) p.mt = mt, p.nt = nt, p.waves = w, p.splits = s;
-        if (p.splits > q.chunks) p.splits = q.chunks;
-        p.split_chunks = ceil_div(q.chunks, p.splits);
-        p.splits = ceil_div(q.chunks, p.split_chunks);
-    }
-#endif
     return p;
 }
 
@@ -454,7 +446,7 @@ static int run_tiles(const Q4Call &a, hipStream_t s)
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     if (lds > 64 * 1024) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, Shape::PANELS) * a.splits;
-    int64_t tiles = ((int64_t)1 << 31) / Shape::THREADS / columns;           // rows in pieces that keep a launch below 2^31 threads
+    int64_t tiles = ((int64_t)1 << 31) / 256 / columns;           // rows in pieces that keep a launch below 2^31 threads
     if (tiles < 1) tiles = 1;
     const int64_t M = a.M, step = tiles * Shape::ROWS;
     for (int64_t m0 = 0; m0 < M; m0 += step) {
@@ -463,7 +455,7 @@ static int run_tiles(const Q4Call &a, hipStream_t s)
         part.x = (const Storage<DT> *)a.x + m0 * a.ldx;
         if (a.gate) part.gate = (const Storage<DT> *)a.gate + m0 * a.ldgate;
         part.out = (Storage<DT> *)a.out + m0 * a.ldout;
-        kernel<<<(unsigned)(columns * ceil_div(part.M, Shape::ROWS)), Shape::THREADS, lds, s>>>(part);
+        kernel<<<(unsigned)(columns * ceil_div(part.M, Shape::ROWS)), 256, lds, s>>>(part);
         NOVA_HIP_TRY(hipGetLastError());
         if (int err = join<DT>(part, s)) return err;
     }
@@ -493,12 +485,12 @@ static int run_group(const Q4Call &a, const Q4Shape &p, hipStream_t s)
     }
     constexpr int NT = BACK && GROUP < 128 ? 1 : 2;
     if constexpr (DT != NOVA_F32 && !BACK && GROUP == 128)
-        if (p.nt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, 4, 1, 4, 2>>(a, s);
+        if (p.nt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, 4, 2>>(a, s);
     if constexpr (DT != NOVA_F32 && !(BACK && GROUP == 32))
-        if (p.mt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, NT, 1, 4, 2>>(a, s);
+        if (p.mt == 4) return run_tiles<DT, BACK, GROUP, Tile<4, NT, 2>>(a, s);
     if constexpr (DT != NOVA_F32 || !(BACK && GROUP == 32))
-        if (p.mt == 2) return run_tiles<DT, BACK, GROUP, Tile<2, NT, 1, 4, DT == NOVA_F32 ? 2 : 4>>(a, s);
-    return run_tiles<DT, BACK, GROUP, Tile<1, NT, 1, 4, 2>>(a, s);
+        if (p.mt == 2) return run_tiles<DT, BACK, GROUP, Tile<2, NT, DT == NOVA_F32 ? 2 : 4>>(a, s);
+    return run_tiles<DT, BACK, GROUP, Tile<1, NT, 2>>(a, s);
 }
 
 template <int DT, bool BACK>

@@ -39,12 +39,12 @@ def test_few_rows(M, N, K, group, dtype, quads):
 
 
 @pytest.mark.parametrize("M,N,K,group,dtype,direction,tile", [
-    (12, 30000, 500, 128, F16, FWD, "1,2,1,4,2"), (7, 200, 600, 32, F32, FWD, "1,2,1,4,2"), (20, 300, 400, 64, BF16, FWD, "2,2,1,4,4"),
-    (50, 260, 390, 128, F32, FWD, "2,2,1,4,2"), (70, 500, 900, 32, F16, FWD, "4,2,1,4,2"), (2100, 4400, 400, 128, BF16, FWD, "4,4,1,4,2"),
-    (1030, 8200, 1300, 128, F16, FWD, "4,4,1,4,2"), (1100, 2300, 300, 64, F16, FWD, "4,2,1,4,2"),
-    (3, 300, 500, 128, F16, BWD, "1,2,1,4,2"), (16, 300, 500, 64, BF16, BWD, "1,1,1,4,2"), (30, 900, 2000, 128, BF16, BWD, "2,2,1,4,4"),
-    (40, 500, 700, 32, F16, BWD, "2,1,1,4,4"), (90, 500, 700, 128, F16, BWD, "4,2,1,4,2"), (90, 500, 700, 64, BF16, BWD, "4,1,1,4,2"),
-    (90, 500, 700, 32, F32, BWD, "1,1,1,4,2"), (90, 500, 700, 64, F32, BWD, "2,1,1,4,2")])
+    (12, 30000, 500, 128, F16, FWD, "1,2,2"), (7, 200, 600, 32, F32, FWD, "1,2,2"), (20, 300, 400, 64, BF16, FWD, "2,2,4"),
+    (50, 260, 390, 128, F32, FWD, "2,2,2"), (70, 500, 900, 32, F16, FWD, "4,2,2"), (2100, 4400, 400, 128, BF16, FWD, "4,4,2"),
+    (1030, 8200, 1300, 128, F16, FWD, "4,4,2"), (1100, 2300, 300, 64, F16, FWD, "4,2,2"),
+    (3, 300, 500, 128, F16, BWD, "1,2,2"), (16, 300, 500, 64, BF16, BWD, "1,1,2"), (30, 900, 2000, 128, BF16, BWD, "2,2,4"),
+    (40, 500, 700, 32, F16, BWD, "2,1,4"), (90, 500, 700, 128, F16, BWD, "4,2,2"), (90, 500, 700, 64, BF16, BWD, "4,1,2"),
+    (90, 500, 700, 32, F32, BWD, "1,1,2"), (90, 500, 700, 64, F32, BWD, "2,1,2")])
 def test_tiles(M, N, K, group, dtype, direction, tile):
     names, workspace = run(M, N, K, group, dtype, direction)
     assert names[0] == f"q4_tile_kernel<{CODE[dtype]},{direction},{group},Tile<{tile}>>"
