@@ -377,15 +377,17 @@ __global__ void __launch_bounds__(256) q4_join_kernel(const Q4Call a)
 // How a call is cut: few rows (mt 0; nt: waves that share a tile's panels) or tiles of 16 mt rows by 64 nt columns; waves of a workgroup; pieces of the reduction.
 struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
 
-// Time of a call with tiles, in us, as it measured on layers of 1000 to 30000 columns and 500 to 25088 positions at 24 to 512 rows (to some 15 %): 2 for the launch;
-// the stages of a workgroup one after the other, each `stage` long on a compute unit of its own and `load` times that where several workgroups share one;
-// and for a cut reduction a launch and the pieces written and read.
+// Time of a call with tiles, in us, as it measured on layers of 1000 to 25088 columns and positions at 12 to 512 rows (to some 15 %): 2 for the launch; the
+// stages of a workgroup one after the other, each `stage` long on a compute unit of its own and 0.71 times the workgroups there where several share one, as
+// many as the fullest unit has; and for a cut reduction a launch and the pieces written and read.
 static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, int splits)
 {
-    const double blocks = (double)ceil_div(q.row_tiles, 4 * nt) * ceil_div(M, 16 * mt) * splits, per_cu = blocks / 256;
-    const double stage = (nt == 4 ? 1.85 : mt == 4 ? 1.05 : mt == 2 ? 0.65 : 0.45) * (dtype == NOVA_F32 ? 2 : 1) * (q.backward ? 1.3 : 1);
-    double load = per_cu * (mt == 4 ? 0.6 : 0.7);
-    if (nt == 4) load = per_cu <= 1 ? 1 : 1.25 * (per_cu <= 2 ? 1 : per_cu / 2);
+    const int64_t blocks = (int64_t)ceil_div(q.row_tiles, 4 * nt) * ceil_div(M, 16 * mt) * splits, on_a_unit = (blocks + 255) / 256;
+    double stage = nt == 4 ? 1.6 : mt == 4 ? 0.83 : mt == 2 ? 0.58 : 0.45;
+    if (q.backward) stage = mt == 4 ? 1.62 : mt == 2 ? 1.0 : 0.7;
+    if (dtype == NOVA_F32) stage *= 2;
+    // (a unit holds two workgroups of the widest tile, three to five of the others)
+    double load = nt == 4 ? (on_a_unit <= 1 ? 1 : 1.43 * ((on_a_unit + 1) / 2)) : 0.71 * on_a_unit;
     if (load < 1) load = 1;
     return 2 + ceil_div(q.chunks, splits) * stage * load + (splits > 1 ? 2.5 + (double)splits * M * q.rows * 8 / 4e6 : 0);
 }
@@ -395,12 +397,14 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
     Q4Shape p;
     p.splits = 1;
     // Up to 16 rows without sharing them, where the rows' operand, read by every 16 columns, is little: 12 rows by 16384 x 4096 (100 MB of it) 12.3 us against 11.1
-    // in tiles, 8 rows 10.3 against 10.7; 16 rows by 4096 x 4096 6.0 against 8.0
-    const double operand = (double)q.row_tiles * M * q.K * dtype_size(dtype);
-    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16) && (M <= 4 || (operand < 100e6 && q.chunks >= 16))) {
+    // in tiles, 8 rows 10.3 against 10.7; 16 rows by 4096 x 4096 6.0 against 8.0.  Rows of an odd number of 16-bit elements begin between 32-bit words, which a
+    // 16-byte load takes some twelve times as long over: 8 rows by 5000 x 3001 9.9 against 8.1 in tiles, by 1000 x 4097 5.7 against 6.4.  Many columns with
+    // little to sum are sooner through in tiles: 6 rows by 30000 x 500 7.8 against 5.7, by 300 x 700 3.5 against 5.1.
+    const double operand = (double)q.row_tiles * M * q.K * dtype_size(dtype) * (q.K * dtype_size(dtype) % 4 ? 12 : 1);
+    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16) && (M <= 4 || (operand < 100e6 && (q.chunks >= 16 || q.row_tiles <= 256)))) {
         p.mt = 0;
         p.nt = q.row_tiles <= 512 ? 8 : q.row_tiles <= 2048 ? 4 : 2;
-        while (p.nt > 1 && p.nt * 2 > q.chunks) p.nt /= 2;
+        while (q.row_tiles > 512 && p.nt > 1 && p.nt * 2 > q.chunks) p.nt /= 2;
         p.waves = p.nt < 4 ? 4 : p.nt;
     } else {
         // (taller tiles take more registers than there are: in binary32, and backward where the columns' scales come in two versions)

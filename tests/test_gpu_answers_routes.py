@@ -32,7 +32,8 @@ def run(M, N, K, group, dtype, direction):
 
 
 @pytest.mark.parametrize("M,N,K,group,dtype,quads", [(1, 500, 1000, 128, F16, 1), (4, 700, 3000, 32, F32, 1), (5, 130, 2500, 64, BF16, 2), (8, 4096, 2048, 128, F16, 2),
-                                                     (9, 300, 2100, 32, F16, 4), (16, 1000, 4096, 64, BF16, 4), (3, 9000, 300, 128, BF16, 1), (2, 40000, 130, 64, F16, 1)])
+                                                     (9, 300, 2100, 32, F16, 4), (16, 1000, 4096, 64, BF16, 4), (3, 9000, 300, 128, BF16, 1), (2, 40000, 130, 64, F16, 1), (8, 1000, 4097, 128, F16, 2),
+                                                     (6, 300, 700, 32, BF16, 2)])
 def test_few_rows(M, N, K, group, dtype, quads):
     names, workspace = run(M, N, K, group, dtype, FWD)
     assert names == [f"q4_few_rows_kernel<{CODE[dtype]},{group},{quads}>"] and workspace == 0
@@ -40,8 +41,8 @@ def test_few_rows(M, N, K, group, dtype, quads):
 
 @pytest.mark.parametrize("M,N,K,group,dtype,direction,tile", [
     (12, 30000, 500, 128, F16, FWD, "1,2,2"), (7, 200, 600, 32, F32, FWD, "1,2,2"), (20, 300, 400, 64, BF16, FWD, "2,2,4"),
-    (50, 260, 390, 128, F32, FWD, "2,2,2"), (70, 500, 900, 32, F16, FWD, "4,2,2"), (2100, 4400, 400, 128, BF16, FWD, "4,4,2"),
-    (1030, 8200, 1300, 128, F16, FWD, "4,4,2"), (1100, 2300, 300, 64, F16, FWD, "4,2,2"),
+    (50, 260, 390, 128, F32, FWD, "2,2,2"), (70, 500, 900, 32, F16, FWD, "4,2,2"), (1010, 8150, 400, 128, BF16, FWD, "4,4,2"),
+    (1020, 8190, 1300, 128, F16, FWD, "4,4,2"), (8, 5000, 3001, 64, F16, FWD, "1,2,2"), (1100, 2300, 300, 64, F16, FWD, "4,2,2"),
     (3, 300, 500, 128, F16, BWD, "1,2,2"), (16, 300, 500, 64, BF16, BWD, "1,1,2"), (30, 900, 2000, 128, BF16, BWD, "2,2,4"),
     (40, 500, 700, 32, F16, BWD, "2,1,4"), (90, 500, 700, 128, F16, BWD, "4,2,2"), (90, 500, 700, 64, BF16, BWD, "4,1,2"),
     (90, 500, 700, 32, F32, BWD, "1,1,2"), (90, 500, 700, 64, F32, BWD, "2,1,2")])
