@@ -12,6 +12,9 @@
  * (r-1)/2 pixels) and each r x r filter g (r = 3 in the paper's experiments, r = 5 its stated
  * extension); stride 1, correlation (no kernel flip), no bias.
  *
+ * Further down, what comes behind a convolution stack: fully connected layers with 4-bit weights, log
+ * probabilities of classes or tokens, and the gradients of both.
+ *
  * Conventions for every call
  *   - "host" pointers are ordinary process memory, "device" pointers are HIP device memory
  *     of the current device; nothing is copied between the two behind the caller's back.
