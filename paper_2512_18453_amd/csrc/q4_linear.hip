@@ -28,6 +28,7 @@ struct alignas(sizeof(T) * COUNT) Several { T v[COUNT]; };
 template <int DT, bool BACK> constexpr int kPieces = DT == NOVA_F32 ? 3 : BACK ? 2 : 1;
 
 template <bool HALF> using Codes = std::conditional_t<HALF, F16Codes, Bf16Codes>;
+template <bool HALF> constexpr float kUnit = HALF ? 1.0f : kCodeUnit;        // what the sums over such codes are multiplied by, at the end
 
 template <typename T>
 __device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, int n, float sum)
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 #pragma unroll
             for (int p = 0; p < P; ++p) part = mfma<HALF>(rows[p], columns, part);
             if ((w + 1) * 32 % GROUP == 0) {
-                const float scale = (float)s.scale.v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
+                const float scale = (float)s.scale.v[w * 32 / GROUP];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] = fma32(scale, part[i], acc[i]);
             }
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
             if (i + I < count) multiply(stage[I]);
         });
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ((float *)own)[(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i];
+    for (int i = 0; i < 4; ++i) ((float *)own)[(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i] * kUnit<HALF>;
     __syncthreads();
     for (int e = threadIdx.x; e < tiles * 256; e += blockDim.x) {
         float sum = 0.0f;
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
                 if constexpr (BACK) {
                     float d[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = (float)s.x[t].v[i] * ((float)s.row_scale[v].v[i] * kCodeUnit);
+                    for (int i = 0; i < 8; ++i) d[i] = (float)s.x[t].v[i] * (float)s.row_scale[v].v[i];
                     if (a.gate) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) d[i] = (float)s.gate[t].v[i] > 0.0f ? d[i] : 0.0f;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
                 if ((w + 1) * 32 % GROUP == 0) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const float scale = (float)s.scale[n].v[w * 32 / GROUP] * (HALF ? 1.0f : kCodeUnit);
+                        const float scale = (float)s.scale[n].v[w * 32 / GROUP];
 #pragma unroll
                         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int column = (tile0 + n) * 16 + lane % 16;
-                if (m < a.M && column < q.rows) store_result<T>(a, split, m, column, acc[t][n][i]);
+                if (m < a.M && column < q.rows) store_result<T>(a, split, m, column, acc[t][n][i] * kUnit<HALF>);
             }
         }
 }
