@@ -10,6 +10,9 @@
 
 namespace nova {
 
+// (called from several places, a step that is a function of its own would keep its stage in memory)
+#define NOVA_INLINE __attribute__((always_inline))
+
 struct Q4Call {
     const void *x, *gate, *bias;                  // x: the rows' operand; gate: the layer's result (backward)
     const char *Wq;
@@ -81,11 +84,11 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
     char *own = lds + wave * OWN;
     const Codes<HALF> codes_to_operand;
 
-    auto load_panel = [&](int c, Stage &s) {
+    auto load_panel = [&](int c, Stage &s) NOVA_INLINE {
         s.codes = __builtin_nontemporal_load((const uint4v *)(codes + (size_t)c * kQ4PanelBytes + lane * 16u));
         s.scale = ((const Several<T, SCALES> *)scales)[(size_t)c * kQ4Rows + lane % 16u];
     };
-    auto load = [&](int i, Stage &s) {
+    auto load = [&](int i, Stage &s) NOVA_INLINE {
         const int c = first + min(i, count - 1) * sharing;                      // (past the last: the last once more, and not multiplied)
 #pragma unroll
         for (int r = 0; r < QUADS; ++r) __builtin_memcpy(&s.x[r], x[r] + c * kQ4Chunk, sizeof s.x[r]);
@@ -93,7 +96,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
     };
 
     float4v acc = {0, 0, 0, 0}, part = {0, 0, 0, 0};
-    auto multiply = [&](const Stage &s) {
+    auto multiply = [&](const Stage &s) NOVA_INLINE {
         // 16-byte block b of row r lies at block b ^ r % 8: the eight rows that are read at a time lie in different banks
 #pragma unroll
         for (int r = 0; r < QUADS; ++r) {
@@ -208,7 +211,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
     const char *panels[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) panels[n] = a.Wq + (size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks * kQ4PanelBytes;       // (as above)
-    auto load_panels = [&](int c, Stage &s) {
+    auto load_panels = [&](int c, Stage &s) NOVA_INLINE {
         if constexpr (BACK) {
             const int group = block_tile * 16 / GROUP;
 #pragma unroll
@@ -222,7 +225,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
                 s.scale[n] = ((const Several<T, SCALES> *)scales)[((size_t)min(tile0 + n, q.row_tiles - 1) * q.chunks + c) * kQ4Rows + lane % 16u];
         }
     };
-    auto load = [&](int i, Stage &s) {
+    auto load = [&](int i, Stage &s) NOVA_INLINE {
         const int c = first + min(i, count - 1), at = c * kQ4Chunk;             // (past the last: the last once more, and not multiplied)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
         }
         load_panels(c, s);
     };
-    auto fill = [&](char *stage, const Stage &s) {
+    auto fill = [&](char *stage, const Stage &s) NOVA_INLINE {
 #pragma unroll
         for (int v = 0; v < VERSIONS; ++v)
 #pragma unroll
@@ -263,14 +266,14 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[t][n] = (float4v){0, 0, 0, 0};
     const int version = VERSIONS > 1 ? wave * NT * 16 / GROUP : 0;
-    auto read_rows = [&](const char *stage, int w, Fragment (&rows)[MT][P]) {
+    auto read_rows = [&](const char *stage, int w, Fragment (&rows)[MT][P]) NOVA_INLINE {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int p = 0; p < P; ++p)
                 rows[t][p].vec = *(const uint4v *)(stage + (version * P + p) * PLANE + (t * 16 + lane % 16) * 256 + ((w * 4 + lane / 16) ^ (lane % 16)) * 16);
     };
-    auto multiply = [&](const char *stage, const Stage &s) {
+    auto multiply = [&](const char *stage, const Stage &s) NOVA_INLINE {
         if constexpr (BACK) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -408,7 +411,8 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
         while (q.row_tiles > 512 && p.nt > 1 && p.nt * 2 > q.chunks) p.nt /= 2;
         p.waves = p.nt < 4 ? 4 : p.nt;
     } else {
-        // (taller tiles take more registers than there are: in binary32, and backward where the columns' scales come in two versions)
+        // (taller tiles take more registers than there are in binary32, and wider ones where a panel holds several groups; where the columns' scales come in two
+        // versions, taller ones take so much LDS that a compute unit holds one workgroup: 700 rows by 4096 x 4096 backward 195 us against 148)
         const int tallest = (dtype == NOVA_F32 ? 2 : 4) / (q.backward && q.group == 32 ? 2 : 1);
         p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
         if (p.mt > tallest) p.mt = tallest;
