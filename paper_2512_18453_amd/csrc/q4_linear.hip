@@ -51,7 +51,8 @@ __device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, 
 // numbers.  Bound by the codes' bytes: a wave has AHEAD panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
 // along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it: read from memory as the
 // matrix unit takes it, 16 rows side by side, each four lanes lie in four cache lines, and one row of 25088 by 4096 took 16.5 us, 16 rows 27.  Now one row takes
-// 10.7 us (51 MB of codes, 5.1 TB/s), 8 rows 15.7: every 16 columns read all rows once more from L2.  The codes are streamed past it (12.2 us without).
+// 11.4 us (53 MB, 4.6 TB/s) with three sets of weights in turn and 12.8 with six, which the last-level cache cannot keep; 8 rows 16.5: every 16 columns read all
+// rows once more from L2.  The codes are streamed past it (1.5 us more without).
 template <int DT, int GROUP, int QUADS>
 struct FewRowsStage {
     uint4v codes;
@@ -156,11 +157,11 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 // such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks are stored at
 // block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
 //
-// Many rows: 1024 by 8192 x 8192 in bfloat16 150 us, 917 TFLOP/s where a large library product of that type reaches 1211.  A panel is made into operands once per 64 rows, three
-// vector instructions for each of its matrix instructions, so both units are busy (without making operands it took 124 us); 256 columns halve the LDS reads of 128 (162 us); eight waves
-// on 128 rows were slower (174 to 227), as all of them wait at one barrier.  Few tiles: 32 rows of the first layer behind the VGG stack (51 MB) 20.8 us, of which
-// the second launch and 8 MB of pieces take 6; four groups of waves per workgroup that shared a tile's stages instead of most of the cut gained nothing.
-// Gradient: twice the products, 512 rows by 4096 x 16384 152 us.
+// Many rows: 1024 by 8192 x 8192 in bfloat16 143 us, 961 TFLOP/s where a large library product of that type reaches 1211.  A panel is made into operands once per
+// 64 rows, three vector instructions for each of its matrix instructions, so both units are busy (without making operands it took 124 us); 256 columns halve the
+// LDS reads of 128 (162 us); eight waves on 128 rows were slower (174 to 227), as all of them wait at one barrier, and so were matrix instructions of 32 by 32
+// (151).  Few tiles: 32 rows of the first layer behind the VGG stack (53 MB) 19.4 us, of which the second launch and 8 MB of pieces take 6; four groups of waves
+// per workgroup that shared a tile's stages instead of most of the cut gained nothing.  Gradient: twice the products, 512 rows by 4096 x 16384 146 us.
 template <int MT_, int NT_, int AHEAD_>
 struct Tile {
     static constexpr int MT = MT_, NT = NT_, AHEAD = AHEAD_, ROWS = 16 * MT, PANELS = 4 * NT;
