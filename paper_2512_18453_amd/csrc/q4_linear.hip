@@ -34,15 +34,11 @@ template <bool HALF> using Codes = std::conditional_t<HALF, F16Codes, Bf16Codes>
 template <bool HALF> constexpr float kUnit = HALF ? 1.0f : kCodeUnit;        // what the sums over such codes are multiplied by, at the end
 
 template <typename T>
-__device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, int n, float sum)
+__device__ __forceinline__ void write_result(const Q4Call &a, int m, int n, float sum)
 {
-    if (a.splits > 1) {
-        a.partial[((size_t)split * a.M + m) * a.q.rows + n] = sum;
-    } else {
-        if (a.bias) sum += load_f32((const T *)a.bias + n);
-        if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
-        store_from_f32((T *)a.out + m * a.ldout + n, sum);
-    }
+    if (a.bias) sum += load_f32((const T *)a.bias + n);
+    if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
+    store_from_f32((T *)a.out + m * a.ldout + n, sum);
 }
 
 // ---- forward, up to 16 rows ----
@@ -51,7 +47,7 @@ __device__ __forceinline__ void store_result(const Q4Call &a, int split, int m, 
 // numbers.  Bound by the codes' bytes: a wave has AHEAD panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
 // along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it: read from memory as the
 // matrix unit takes it, 16 rows side by side, each four lanes lie in four cache lines, and one row of 25088 by 4096 took 16.5 us, 16 rows 27.  Now one row takes
-// 11.4 us (53 MB, 4.6 TB/s) with three sets of weights in turn and 12.8 with six, which the last-level cache cannot keep; 8 rows 16.5: every 16 columns read all
+// 11.4 us (53 MB, 4.6 TB/s) with three sets of weights in turn and 12.8 with six, which the last-level cache cannot keep; 8 rows by 8192 x 4096 6.6: every 16 columns read all
 // rows once more from L2.  The codes are streamed past it (1.5 us more without).
 template <int DT, int GROUP, int QUADS>
 struct FewRowsStage {
@@ -71,12 +67,11 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
     extern __shared__ char lds[];
     const Q4Layout &q = a.q;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), tiles = blockDim.x / 64 / sharing;
-    const int blocks = (q.row_tiles + tiles - 1) / tiles, split = blockIdx.x / blocks, tile0 = blockIdx.x % blocks * tiles;
+    const int tile0 = blockIdx.x * tiles;
     const int tile = min(tile0 + wave / sharing, q.row_tiles - 1);           // (past the last: computed and not stored)
     // whole panels of this wave, and the one that ends inside
-    const int whole = q.reduction / kQ4Chunk, first = split * a.split_chunks + wave % sharing, end = min(whole, (split + 1) * a.split_chunks);
-    const int count = end > first ? (end - first + sharing - 1) / sharing : 0;
-    const bool ragged = whole < q.chunks && split == a.splits - 1 && wave % sharing == (whole - split * a.split_chunks) % sharing;
+    const int whole = q.reduction / kQ4Chunk, first = wave % sharing, count = whole > first ? (whole - first + sharing - 1) / sharing : 0;
+    const bool ragged = whole < q.chunks && first == whole % sharing;
     const T *scales = (const T *)(a.Wq + q.code_bytes) + (size_t)tile * q.scale_pitch * kQ4Rows;
     const char *codes = a.Wq + (size_t)tile * q.chunks * kQ4PanelBytes;
     const T *x[QUADS];
@@ -90,7 +85,8 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
         s.scale = ((const Several<T, SCALES> *)scales)[(size_t)c * kQ4Rows + lane % 16u];
     };
     auto load = [&](int i, Stage &s) NOVA_INLINE {
-        const int c = first + min(i, count - 1) * sharing;                      // (past the last: the last once more, and not multiplied)
+        // (past the last: the last once more, and not multiplied; with the load in a branch every step waits for all of them, one row 16.1 us against 11.4)
+        const int c = first + min(i, count - 1) * sharing;
 #pragma unroll
         for (int r = 0; r < QUADS; ++r) __builtin_memcpy(&s.x[r], x[r] + c * kQ4Chunk, sizeof s.x[r]);
         load_panel(c, s);
@@ -146,7 +142,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
         float sum = 0.0f;
         for (int w = 0; w < sharing; ++w) sum += ((const float *)(lds + (e / 256 * sharing + w) * OWN))[e % 256];
         const int m = e % 256 / 16, n = (tile0 + e / 256) * 16 + e % 16;
-        if (m < a.M && n < q.rows) store_result<T>(a, split, m, n, sum);
+        if (m < a.M && n < q.rows) write_result<T>(a, m, n, sum);
     }
 }
 
@@ -352,7 +348,10 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int column = (tile0 + n) * 16 + lane % 16;
-                if (m < a.M && column < q.rows) store_result<T>(a, split, m, column, acc[t][n][i] * kUnit<HALF>);
+                if (m >= a.M || column >= q.rows) continue;
+                const float sum = acc[t][n][i] * kUnit<HALF>;
+                if (a.splits > 1) a.partial[((size_t)split * a.M + m) * q.rows + column] = sum;
+                else write_result<T>(a, m, column, sum);
             }
         }
 }
@@ -372,10 +371,7 @@ __global__ void __launch_bounds__(256) q4_join_kernel(const Q4Call a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += v[i];
         }
-        const int m = (int)(at / a.q.rows), n = (int)(at % a.q.rows);
-        if (a.bias) sum += load_f32((const T *)a.bias + n);
-        if (a.relu) sum = sum < 0.0f ? 0.0f : sum;
-        store_from_f32((T *)a.out + m * a.ldout + n, sum);
+        write_result<T>(a, (int)(at / a.q.rows), (int)(at % a.q.rows), sum);
     }
 }
 
@@ -384,7 +380,7 @@ struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
 
 // Time of a call with tiles, in us, as it measured on layers of 1000 to 25088 columns and positions at 12 to 512 rows (to some 15 %): 2 for the launch; the
 // stages of a workgroup one after the other, each `stage` long on a compute unit of its own and 0.71 times the workgroups there where several share one, as
-// many as the fullest unit has; and for a cut reduction a launch and the pieces written and read.
+// many as the fullest unit has; and for a cut reduction a launch and the pieces, added one behind the other, written and read.
 static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, int splits)
 {
     const int64_t blocks = (int64_t)ceil_div(q.row_tiles, 4 * nt) * ceil_div(M, 16 * mt) * splits, on_a_unit = (blocks + 255) / 256;
@@ -394,7 +390,7 @@ static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, 
     // (a unit holds two workgroups of the widest tile, three to five of the others)
     double load = nt == 4 ? (on_a_unit <= 1 ? 1 : 1.43 * ((on_a_unit + 1) / 2)) : 0.71 * on_a_unit;
     if (load < 1) load = 1;
-    return 2 + ceil_div(q.chunks, splits) * stage * load + (splits > 1 ? 2.5 + (double)splits * M * q.rows * 8 / 4e6 : 0);
+    return 2 + ceil_div(q.chunks, splits) * stage * load + (splits > 1 ? 2.4 + 0.04 * splits + (double)splits * M * q.rows * 8 / 4e6 : 0);
 }
 
 static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
@@ -406,7 +402,11 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
     // 16-byte load takes some twelve times as long over: 8 rows by 5000 x 3001 9.9 against 8.1 in tiles, by 1000 x 4097 5.7 against 6.4.  Many columns with
     // little to sum are sooner through in tiles: 6 rows by 30000 x 500 7.8 against 5.7, by 300 x 700 3.5 against 5.1.
     const double operand = (double)q.row_tiles * M * q.K * dtype_size(dtype) * (q.K * dtype_size(dtype) % 4 ? 12 : 1);
-    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16) && (M <= 4 || (operand < 100e6 && (q.chunks >= 16 || q.row_tiles <= 256)))) {
+    // A long sum is left to few waves here and can be cut in tiles, where the columns are few enough that the pieces are: 16 rows by 25088 x 1000 in binary16
+    // 19.9 us against 9.7, by 8192 x 1000 8.3 against 7.2, by 4096 x 1000 5.3 against 6.1; 8 rows 13.3 against 9.8, 6.1 against 6.9; 1 row 9.0 against 9.1.
+    // Binary32, of three pieces: 1 row by 25088 x 10 20.2 against 8.9, by 8192 x 10 8.0 against 6.0, by 4096 x 1000 5.9 against 6.2; by 25088 x 4096 the same.
+    const bool long_sums = q.row_tiles <= 128 && ((dtype == NOVA_F32 || M > 8) ? q.chunks >= 64 : M > 4 && q.chunks > 128);
+    if (!q.backward && M <= (dtype == NOVA_F32 ? 4 : 16) && !long_sums && (M <= 4 || (operand < 100e6 && (q.chunks >= 16 || q.row_tiles <= 256)))) {
         p.mt = 0;
         p.nt = q.row_tiles <= 512 ? 8 : q.row_tiles <= 2048 ? 4 : 2;
         while (q.row_tiles > 512 && p.nt > 1 && p.nt * 2 > q.chunks) p.nt /= 2;
@@ -422,7 +422,7 @@ static Q4Shape q4_shape(int M, const Q4Layout &q, int dtype)
         double least = q4_tile_time(M, q, dtype, p.mt, p.nt, 1);
         const int narrow = p.nt;
         for (int nt = narrow; nt <= (p.mt == 4 && !q.backward && q.group == 128 ? 4 : narrow); nt *= 2)
-            for (int splits = 1; splits <= 32 && splits <= q.chunks; ++splits) {
+            for (int splits = 1; splits <= 64 && splits <= q.chunks; ++splits) {
                 const double time = q4_tile_time(M, q, dtype, p.mt, nt, splits);
                 if (time < least) least = time, p.nt = nt, p.splits = splits;
             }
@@ -453,8 +453,7 @@ static int run_tiles(const Q4Call &a, hipStream_t s)
 {
     const auto kernel = q4_tile_kernel<DT, BACK, GROUP, Shape>;
     constexpr unsigned lds = Shape::template lds_bytes<DT, BACK, GROUP>;
-    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
-    if (lds > 64 * 1024) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    static_assert(lds <= 64 * 1024, "LDS of a workgroup");
     const int64_t columns = (int64_t)ceil_div(a.q.row_tiles, Shape::PANELS) * a.splits;
     int64_t tiles = ((int64_t)1 << 31) / 256 / columns;           // rows in pieces that keep a launch below 2^31 threads
     if (tiles < 1) tiles = 1;
@@ -476,7 +475,7 @@ template <int DT, int GROUP, int QUADS>
 static void run_few_rows(const Q4Call &a, const Q4Shape &p, hipStream_t s)
 {
     constexpr unsigned operand = kPieces<DT, false> * QUADS * 4 * 256, own = operand > 1024 ? operand : 1024;
-    q4_few_rows_kernel<DT, GROUP, QUADS><<<ceil_div(a.q.row_tiles, p.waves / p.nt) * a.splits, p.waves * 64, p.waves * own, s>>>(a, p.nt);
+    q4_few_rows_kernel<DT, GROUP, QUADS><<<ceil_div(a.q.row_tiles, p.waves / p.nt), p.waves * 64, p.waves * own, s>>>(a, p.nt);
 }
 
 template <int DT, bool BACK, int GROUP>
@@ -489,8 +488,7 @@ static int run_group(const Q4Call &a, const Q4Shape &p, hipStream_t s)
                 if (a.M <= 8) run_few_rows<DT, GROUP, 2>(a, p, s);
                 else run_few_rows<DT, GROUP, 4>(a, p, s);
             }
-            NOVA_HIP_TRY(hipGetLastError());
-            return join<DT>(a, s);
+            return (int)hipGetLastError();
         }
     }
     constexpr int NT = BACK && GROUP < 128 ? 1 : 2;

@@ -140,6 +140,23 @@ def test_backward(M, N, K, group, dtype):
     close(nova.nova_q4_linear_backward(dy, Wq, K, group, y=y), d @ W, d.abs() @ W.abs(), N, extra)
 
 
+# few outputs of a long sum, on both sides of where a sum is cut into more pieces than a unit has waves
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("M,N,K,group", [(1, 10, 8192, 64), (4, 33, 25088, 128), (9, 70, 8193, 32), (16, 515, 12544, 128), (8, 17, 16385, 64),
+                                         (6, 16, 60000, 128), (12, 2049, 8200, 64), (5, 2048, 16500, 128)])
+def test_long_sums(M, N, K, group, dtype):
+    print(f"[case] long sums {M} x {N} x {K}, group {group}, {dtype}", flush=True)
+    gen, codes, scales, W = make(N, K, group, dtype)
+    x = torch.randn((M, K), device=DEV, generator=gen).to(dtype)
+    y = nova.nova_q4_linear(x, nova.nova_q4_pack(codes, scales, group), N, group)
+    close(y, x.double() @ W.T, x.double().abs() @ W.abs().T, K)
+    del W
+    gen, codes, scales, W = make(K, N, group, dtype)            # the gradient's sum runs over the outputs
+    dx = nova.nova_q4_linear_backward(x, nova.nova_q4_pack(codes, scales, group, BWD), N, group)
+    extra = 0.0 if dtype == F32 else 2.0 ** -15
+    close(dx, x.double() @ W, x.double().abs() @ W.abs(), K, extra)
+
+
 def test_gradient_against_differences():
     # (the forward call itself, in binary32, in small steps: it is linear in x, so a central difference is exact up to the rounding of its two results)
     M, N, K, group = 3, 40, 150, 64
