@@ -506,7 +506,7 @@ static LogprobsShape logprobs_shape(int rows, int V)
     p.threads = V <= 64 * kVectors * 8 ? 64 : kMaxWaves * 64;
     const int in_hand = p.threads * kVectors * 8;
     int64_t slices = ((int64_t)V + in_hand - 1) / in_hand;
-    const int64_t wanted = (1024 + rows - 1) / (rows > 0 ? rows : 1);
+    const int64_t wanted = rows > 0 ? (1023 + (int64_t)rows) / rows : 1024;
     if (slices > wanted) slices = wanted;
     if (slices > kMaxSlices) slices = kMaxSlices;
     const int64_t each = (((int64_t)V + slices - 1) / slices + in_hand - 1) / in_hand * in_hand;
