@@ -383,7 +383,7 @@ struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
 // many as the fullest unit has; and for a cut reduction a launch and the pieces, added one behind the other, written and read.
 static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, int splits)
 {
-    const int64_t blocks = (int64_t)ceil_div(q.row_tiles, 4 * nt) * ceil_div(M, 16 * mt) * splits, on_a_unit = (blocks + 255) / 256;
+    const int64_t row_blocks = ((int64_t)M + 16 * mt - 1) / (16 * mt), blocks = ceil_div(q.row_tiles, 4 * nt) * row_blocks * splits, on_a_unit = (blocks + 255) / 256;
     double stage = nt == 4 ? 1.6 : mt == 4 ? 0.83 : mt == 2 ? 0.58 : 0.45;
     if (q.backward) stage = mt == 4 ? 1.62 : mt == 2 ? 1.0 : 0.7;
     if (dtype == NOVA_F32) stage *= 2;
