@@ -240,11 +240,14 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
                 if constexpr (BACK) {
                     float d[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = (float)s.x[t].v[i] * (float)s.row_scale[v].v[i];
+                    for (int i = 0; i < 8; ++i) d[i] = (float)s.x[t].v[i];
                     if (a.gate) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) d[i] = (float)s.gate[t].v[i] > 0.0f ? d[i] : 0.0f;
                     }
+                    // (behind the gate: zero times a scale that is no number is NaN)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] *= (float)s.row_scale[v].v[i];
                     split_fragment<P>(d, f);
                 } else if constexpr (DT == NOVA_F32) {
                     split_fragment<P>(s.x[t].v, f);
