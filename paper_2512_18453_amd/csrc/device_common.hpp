@@ -167,6 +167,15 @@ __device__ __forceinline__ void wait_vmcnt_at_most(int n)
     }
 }
 
+// What the lanes of a wave stored to LDS before is seen by its other lanes behind, and what they read before is read before it is overwritten.  The LDS accesses of
+// a wave are done in their order, so nothing is waited for; it is the compiler that is told: a thread by itself may read ahead of its own store elsewhere.
+__device__ __forceinline__ void exchange_in_wave()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // blockIdx.x -> logical block id such that consecutive logical ids run on the same XCD
 // (hardware deals consecutive workgroup ids round-robin over the 8 XCDs, each with its own L2).
 __device__ __forceinline__ unsigned xcd_local_block_id(unsigned id, unsigned total)

@@ -156,15 +156,16 @@ __device__ __forceinline__ rank_t best_of(const rank_t *candidates, int count, i
     const rank_t least = reached_by<0>(all, top);
     int kept = 0;
     scratch[lane] = 0;
+    exchange_in_wave();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const unsigned long long keep = __ballot(all[i] >= least);
         if (keep >> lane & 1) scratch[kept + __popcll(keep & ((1ull << lane) - 1))] = all[i];
         kept += __popcll(keep);
     }
-    __builtin_amdgcn_wave_barrier();
+    exchange_in_wave();
     const rank_t mine = scratch[lane];
-    __builtin_amdgcn_wave_barrier();
+    exchange_in_wave();
     return mine;
 }
 
@@ -181,9 +182,9 @@ __device__ __forceinline__ rank_t sorted_best(const rank_t *candidates, int coun
     int place = 0;
     for (int i = 0; i < count; ++i) place += read_lane(mine, i) > mine;
     scratch[lane] = 0;
-    __builtin_amdgcn_wave_barrier();
+    exchange_in_wave();
     if (lane < count) scratch[place] = mine;
-    __builtin_amdgcn_wave_barrier();
+    exchange_in_wave();
     return scratch[lane];
 }
 
@@ -432,9 +433,9 @@ __global__ void __launch_bounds__(kJoinWaves * 64) logprobs_join_kernel(const Lo
                 best.mine = r;
             } else {
                 lists[wave][lane] = r;
-                __builtin_amdgcn_wave_barrier();
+                exchange_in_wave();
                 best.merge(lists[wave]);
-                __builtin_amdgcn_wave_barrier();
+                exchange_in_wave();
             }
         }
     }

@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 #pragma unroll
             for (int p = 0; p < P; ++p) *(uint4v *)(own + p * PLANE + row * 256 + ((lane % 16) ^ (row % 8)) * 16) = f[p].vec;
         }
+        exchange_in_wave();
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const int row = lane % (4 * QUADS);
@@ -120,6 +121,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
                 for (int i = 0; i < 4; ++i) acc[i] = fma32(scale, part[i], acc[i]);
             }
         }
+        exchange_in_wave();
     };
 
     Stage stage[AHEAD];
