@@ -526,7 +526,7 @@ extern "C" int nova_logprobs(const void *logits, int64_t stride, const int64_t *
     const size_t need = logprobs_workspace(rows, V, top, dtype);
     if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
     if (workspace_bytes < need) return NOVA_ENOSPC;
-    const LogprobsArgs a = {logits, stride, targets, mask, mask_stride, rows, V, scale, top, logprob, entropy, stats, top_logprobs, top_ids};
+    const LogprobsArgs a = {logits, stride, targets, mask, mask_stride, rows, V, scale, top, logprob, entropy, stats, top_logprobs, top_ids, 0.0f, 0.0f};
     return hip_result(launch_logprobs(a, dtype, workspace, stream));
 }
 

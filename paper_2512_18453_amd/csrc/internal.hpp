@@ -200,6 +200,7 @@ struct LogprobsArgs {
     const void *logits; int64_t stride; const int64_t *targets; const uint8_t *mask; int64_t mask_stride;
     int rows, V; float scale; int top;
     float *logprob, *entropy, *stats, *top_logprobs; int64_t *top_ids;
+    float exponent, exponent_rest;             // their sum is scale log2 e; set by launch_logprobs
 };
 int launch_logprobs(const LogprobsArgs &a, int dtype, void *workspace, void *stream);
 struct LogprobsBackwardArgs {
