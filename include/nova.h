@@ -397,6 +397,7 @@ int nova_q4_unpack(const void *Wq, size_t Wq_bytes, int N, int K, int group, int
  * bias: device [N] or NULL.  Wq: NOVA_Q4_FORWARD layout of dtype.
  * Products and sums in binary32: the codes are exact on the matrix unit, a group's sum is scaled in binary32, and y is rounded once.  Sums are formed in a
  * fixed order: equal calls give equal bits.
+ * (A group's sum that passes binary32's range before its scale comes to it is formed again from smaller rows: y is infinite where the scaled sums are.)
  *
  * nova_q4_linear_backward: dx[m][k] = sum_n d[m][n] W[n][k], d = dy, or with y (the layer's result after its ReLU) d = y > 0 ? dy : 0; y may
  * be NULL.  The weights of a stored layer are constants: there is no gradient of codes, scales or bias.  dy: [M][N], y: [M][N], dx: [M][K] with

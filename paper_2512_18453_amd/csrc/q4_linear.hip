@@ -33,6 +33,43 @@ template <int DT, bool BACK> constexpr int kPieces = DT == NOVA_F32 ? 3 : BACK ?
 template <bool HALF> using Codes = std::conditional_t<HALF, F16Codes, Bf16Codes>;
 template <bool HALF> constexpr float kUnit = HALF ? 1.0f : kCodeUnit;        // what the sums over such codes are multiplied by, at the end
 
+// Forward, a group's sum is formed before its scale comes to it, and with rows of binary32 or bfloat16 such a sum can pass binary32's range (|x| adding up to 7e38) where the result does not.  A
+// workgroup whose results are not all finite makes them again, from rows that are a 256th, in which no group's sum passes it, and writes those that were not: what holds infinities
+// or NaN takes twice as long, anything else the check: 1 x 4096 x 1000 in binary32 6.83 -> 7.06 us, 32 x 4096 x 4096 in bfloat16 10.8 -> 11.2, 1024 x 8192 x 8192 148.6 -> 149.7.
+template <int DT, bool BACK> constexpr int kPasses = BACK || DT == NOVA_F16 ? 1 : 2;
+constexpr float kShrunk = 1.0f / 256;
+template <int DT, int PASS>
+__device__ __forceinline__ void row_fragment(const Eight<Storage<DT>> &x, Fragment (&f)[kPieces<DT, false>])
+{
+    Eight<Storage<DT>> row = x;
+    if constexpr (PASS > 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row.v[i] = (Storage<DT>)((float)x.v[i] * kShrunk);
+    }
+    if constexpr (DT == NOVA_F32) split_fragment<kPieces<DT, false>>(row.v, f);
+    else __builtin_memcpy(&f[0], &row, 16);
+}
+// What the sums of a pass are multiplied by
+template <bool HALF, int PASS> constexpr float kSumUnit = PASS > 0 ? kUnit<HALF> / kShrunk : kUnit<HALF>;
+// The thread's number; in a second pass one that the compiler does not know from the first, so that it keeps nothing in registers from there
+template <int PASS>
+__device__ __forceinline__ int thread_of_pass()
+{
+    int t = threadIdx.x;
+    if constexpr (PASS > 0) asm volatile("" : "+v"(t));
+    return t;
+}
+// Whether a thread of the workgroup has results left; flag: 0 since a barrier
+__device__ __forceinline__ bool left_in_workgroup(bool mine, int &flag)
+{
+    exchange_in_wave();                           // (the wave has read what it reads of LDS, here and behind)
+    if (mine) flag = 1;
+    __syncthreads();
+    const bool any = flag != 0;
+    exchange_in_wave();
+    return any;
+}
+
 template <typename T>
 __device__ __forceinline__ void write_result(const Q4Call &a, int m, int n, float sum)
 {
@@ -56,17 +93,18 @@ struct FewRowsStage {
     Several<Storage<DT>, kQ4Chunk / GROUP> scale;
 };
 
-template <int DT, int GROUP, int QUADS>
-__global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int sharing)
+// `open`: in, which of the thread's results to write (bit i: the i-th); out, which were not written because they are not finite
+template <int DT, int GROUP, int QUADS, int PASS>
+__device__ __forceinline__ unsigned q4_few_rows_pass(const Q4Call &a, int sharing, unsigned open)
 {
     typedef Storage<DT> T;
     typedef FewRowsStage<DT, GROUP, QUADS> Stage;
     constexpr bool HALF = DT == NOVA_F16;
     constexpr int P = kPieces<DT, false>, SCALES = kQ4Chunk / GROUP, AHEAD = 4;
     constexpr int PLANE = QUADS * 4 * 256, OWN = P * PLANE > 1024 ? P * PLANE : 1024;        // bytes of a wave: the operand, later its sums
-    extern __shared__ char lds[];
+    extern __shared__ __align__(16) char lds[];
     const Q4Layout &q = a.q;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), tiles = blockDim.x / 64 / sharing;
+    const int thread = thread_of_pass<PASS>(), lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64), tiles = blockDim.x / 64 / sharing;
     const int tile0 = blockIdx.x * tiles;
     const int tile = min(tile0 + wave / sharing, q.row_tiles - 1);           // (past the last: computed and not stored)
     // whole panels of this wave, and the one that ends inside
@@ -99,8 +137,7 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
         for (int r = 0; r < QUADS; ++r) {
             const int row = 4 * r + lane / 16;
             Fragment f[P];
-            if constexpr (DT == NOVA_F32) split_fragment<P>(s.x[r].v, f);
-            else __builtin_memcpy(&f[0], &s.x[r], 16);
+            row_fragment<DT, PASS>(s.x[r], f);
 #pragma unroll
             for (int p = 0; p < P; ++p) *(uint4v *)(own + p * PLANE + row * 256 + ((lane % 16) ^ (row % 8)) * 16) = f[p].vec;
         }
@@ -138,14 +175,29 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
             if (i + I < count) multiply(stage[I]);
         });
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ((float *)own)[(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i] * kUnit<HALF>;
+    for (int i = 0; i < 4; ++i) ((float *)own)[(lane / 16 * 4 + i) * 16 + lane % 16] = acc[i];
     __syncthreads();
-    for (int e = threadIdx.x; e < tiles * 256; e += blockDim.x) {
+    unsigned left = 0;
+    for (int e = thread, bit = 1; e < tiles * 256; e += blockDim.x, bit *= 2) {
         float sum = 0.0f;
         for (int w = 0; w < sharing; ++w) sum += ((const float *)(lds + (e / 256 * sharing + w) * OWN))[e % 256];
+        sum *= kSumUnit<HALF, PASS>;
         const int m = e % 256 / 16, n = (tile0 + e / 256) * 16 + e % 16;
-        if (m < a.M && n < q.rows) write_result<T>(a, m, n, sum);
+        if (m >= a.M || n >= q.rows || (PASS > 0 && !(open & bit))) continue;
+        if (PASS < kPasses<DT, false> - 1 && !__builtin_isfinite(sum)) left |= bit;
+        else write_result<T>(a, m, n, sum);
     }
+    return left;
+}
+
+template <int DT, int GROUP, int QUADS>
+__global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int sharing)
+{
+    __shared__ int flag;
+    if (kPasses<DT, false> > 1 && threadIdx.x == 0) flag = 0;
+    const unsigned open = q4_few_rows_pass<DT, GROUP, QUADS, 0>(a, sharing, ~0u);
+    if constexpr (kPasses<DT, false> > 1)
+        if (left_in_workgroup(open != 0, flag)) q4_few_rows_pass<DT, GROUP, QUADS, 1>(a, sharing, open);
 }
 
 // ---- more rows, and the gradient ----
@@ -175,8 +227,9 @@ struct TileStage {
     Several<Storage<DT>, kQ4Chunk / GROUP> scale[BACK ? 1 : Shape::NT];
 };
 
-template <int DT, bool BACK, int GROUP, typename Shape>
-__global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
+// `open` as above, bit (4 t + i) NT + n
+template <int DT, bool BACK, int GROUP, typename Shape, int PASS>
+__device__ __forceinline__ uint64_t q4_tile_pass(const Q4Call &a, uint64_t open)
 {
     typedef Storage<DT> T;
     typedef TileStage<DT, BACK, GROUP, Shape> Stage;
@@ -185,9 +238,9 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
     constexpr int P = kPieces<DT, BACK>, SCALES = kQ4Chunk / GROUP, VERSIONS = Shape::template versions<BACK, GROUP>;
     static_assert(VERSIONS == 1 || NT * 16 <= GROUP, "a wave's columns lie in one group");
     constexpr int PLANE = Shape::ROWS * 256, LDS_STAGE = VERSIONS * P * PLANE;        // bytes
-    extern __shared__ char lds[];
+    extern __shared__ __align__(16) char lds[];
     const Q4Layout &q = a.q;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int thread = thread_of_pass<PASS>(), lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64);
     const int column_blocks = (q.row_tiles + Shape::PANELS - 1) / Shape::PANELS, row_blocks = (a.M + Shape::ROWS - 1) / Shape::ROWS;
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x);
     const int m0 = id % row_blocks * Shape::ROWS, block_tile = id / row_blocks % column_blocks * Shape::PANELS, split = id / row_blocks / column_blocks;
@@ -199,7 +252,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
     const Codes<HALF> codes_to_operand;
 
     // thread t stages row t / 16 of every 16, positions 8 (t % 16) ..
-    const int my_row = threadIdx.x / 16, my_pos = threadIdx.x % 16 * 8;
+    const int my_row = thread / 16, my_pos = thread % 16 * 8;
     const T *x_row[MT], *gate_row[BACK ? MT : 1];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -251,10 +304,8 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) d[i] *= (float)s.row_scale[v].v[i];
                     split_fragment<P>(d, f);
-                } else if constexpr (DT == NOVA_F32) {
-                    split_fragment<P>(s.x[t].v, f);
                 } else {
-                    __builtin_memcpy(&f[0], &s.x[t], 16);
+                    row_fragment<DT, PASS>(s.x[t], f);
                 }
 #pragma unroll
                 for (int p = 0; p < P; ++p)
@@ -345,6 +396,7 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
             }
         });
 
+    uint64_t left = 0;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -353,12 +405,25 @@ __global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int column = (tile0 + n) * 16 + lane % 16;
-                if (m >= a.M || column >= q.rows) continue;
-                const float sum = acc[t][n][i] * kUnit<HALF>;
-                if (a.splits > 1) a.partial[((size_t)split * a.M + m) * q.rows + column] = sum;
+                const uint64_t bit = (uint64_t)1 << ((t * 4 + i) * NT + n);
+                if (m >= a.M || column >= q.rows || (PASS > 0 && !(open & bit))) continue;
+                const float sum = acc[t][n][i] * kSumUnit<HALF, PASS>;
+                if (PASS < kPasses<DT, BACK> - 1 && !__builtin_isfinite(sum)) left |= bit;
+                else if (a.splits > 1) a.partial[((size_t)split * a.M + m) * q.rows + column] = sum;
                 else write_result<T>(a, m, column, sum);
             }
         }
+    return left;
+}
+
+template <int DT, bool BACK, int GROUP, typename Shape>
+__global__ void __launch_bounds__(256, 2) q4_tile_kernel(const Q4Call a)
+{
+    __shared__ int flag;
+    if (kPasses<DT, BACK> > 1 && threadIdx.x == 0) flag = 0;
+    const uint64_t open = q4_tile_pass<DT, BACK, GROUP, Shape, 0>(a, ~(uint64_t)0);
+    if constexpr (kPasses<DT, BACK> > 1)
+        if (left_in_workgroup(open != 0, flag)) q4_tile_pass<DT, BACK, GROUP, Shape, 1>(a, open);
 }
 
 // The pieces of a cut reduction, in order

@@ -24,3 +24,48 @@ def test_closed_places_meet_weights_that_are_no_numbers(M, group, dtype):
     bad = torch.zeros(K, dtype=torch.bool, device=DEV)
     bad[group:3 * group] = True
     assert bool(torch.isnan(got[:, bad]).all()) and torch.equal(got[:, ~bad], clean[:, ~bad])
+
+
+# every kernel and height of tile, sums in one piece and cut, K that ends inside a panel, a panel that holds one group and several
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N,K,group", [(1, 130, 300, 128), (2, 40000, 130, 64), (4, 700, 2999, 32), (7, 300, 1000, 128), (16, 500, 2048, 64), (16, 60, 30000, 128), (30, 77, 515, 32), (33, 300, 5000, 128),
+                                         (100, 200, 640, 64), (1010, 8150, 400, 128)])
+def test_large_rows_under_small_scales(M, N, K, group, dtype):
+    # the sum of a group over its codes is beyond binary32, the scaled one is not
+    gen, codes, scales, W = make(N, K, group, dtype)
+    scales *= 2.0 ** -30                                     # (exact)
+    W *= 2.0 ** -30
+    Wq = nova.nova_q4_pack(codes, scales, group)
+    x = torch.randn((M, K), device=DEV, generator=gen).to(dtype)
+    bias = torch.randn((N,), device=DEV, generator=gen).to(dtype)
+    clean = nova.nova_q4_linear(x, Wq, N, group, bias=bias)
+    rows = sorted({0, M // 2, M - 1})
+    for r in rows:
+        x[r] = (torch.sign(x[r].float()) * 2.0 ** 126 * (1 + torch.rand((K,), device=DEV, generator=gen))).clamp(-2.0 ** 127, 2.0 ** 127).to(dtype)
+    x[M - 1, K // 2:] = 2.0 ** 126                           # (sums of one sign)
+    codes[5, :] = 7
+    W[5] = 7 * scales[5].double().repeat_interleave(group)[:K]
+    Wq = nova.nova_q4_pack(codes, scales, group)
+    ws = torch.full((nova.nova_q4_linear_workspace_bytes(M, N, K, group, dtype),), 0xFF, dtype=torch.uint8, device=DEV)
+    got = nova.nova_q4_linear(x, Wq, N, group, bias=bias, workspace=ws)
+    want, S = x[rows].double() @ W.T + bias.double(), x[rows].double().abs() @ W.abs().T + bias.double().abs()
+    close(got[rows], want, S, K + 1)
+    others = [r for r in range(M) if r not in rows]
+    columns = torch.arange(N, device=DEV) != 5
+    assert torch.equal(got[others][:, columns], clean[others][:, columns])      # rows beside them keep their bits
+    relu = nova.nova_q4_linear(x, Wq, N, group, bias=bias, flags=nova.NOVA_FLAG_RELU)
+    assert torch.equal(relu, torch.where(got < 0, 0.0, got))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M", [1, 9, 40, 150])
+def test_results_beyond_the_type_are_infinite(M, dtype):
+    N, K, group = 48, 400, 32
+    gen, codes, scales, W = make(N, K, group, dtype)
+    codes = codes.abs().clamp(min=1, max=7)
+    codes[1::2] *= -1
+    x = (2.0 ** 126 * (1 + torch.rand((M, K), device=DEV, generator=gen))).clamp(max=2.0 ** 127).to(dtype)
+    got = nova.nova_q4_linear(x, nova.nova_q4_pack(codes, torch.ones_like(scales), group), N, group)
+    want = torch.full((M, N), float("inf"), device=DEV)
+    want[:, 1::2] *= -1
+    assert torch.equal(got.float(), want)
