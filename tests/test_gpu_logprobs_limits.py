@@ -1,11 +1,11 @@
-"""Log probabilities: what rounding of the scale costs."""
+"""Log probabilities: what rounding of the scale costs, rows of logits and of masks at different strides, more rows than one launch takes."""
 import math
 
 import pytest
 import torch
 
 from paper_2512_18453_amd import nova
-from test_gpu_logprobs import DEV, F32, definition
+from test_gpu_logprobs import BF16, DEV, F16, F32, TINY, UNIT, check, definition, error, gradient, make, within
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,45 @@ def test_scale_is_not_rounded_twice(V, scale):
     print(f"  L {L:.3f} off {off_L * 2 ** 24:.2f} units, H {H:.3f} off {off_H * 2 ** 24:.2f}, E {E:.2f}, W {W:.2f}", flush=True)
     assert abs(off_L) <= 1.5 * 2.0 ** -24 * (1 + L) + E * 2.0 ** -27
     assert abs(off_H) <= 2 * 2.0 ** -24 * (1 + H) + W * 2.0 ** -28
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("R,V", [(4, 301), (2, 30001), (400, 2049), (1500, 70)])
+def test_rows_of_logits_and_of_masks_at_different_strides(R, V, dtype):
+    # what a row gives does not depend on where it and its mask begin
+    gen, _, targets = make(R, V, dtype)
+    a, h = torch.randn((R,), device=DEV, generator=gen), torch.randn((R,), device=DEV, generator=gen)
+    for offset, mask_offset in ((0, 5), (1, 0), (3, 2), (7, 7)):
+        x = torch.randn((R, V + 13), device=DEV, generator=gen).to(dtype)[:, offset:offset + V]
+        mask = (torch.rand((R, V + 30), device=DEV, generator=gen) < 0.7)[:, mask_offset:mask_offset + V]
+        got = nova.nova_logprobs(x, targets, mask=mask, scale=0.8, top=9)
+        want = nova.nova_logprobs(x.contiguous(), targets, mask=mask.contiguous(), scale=0.8, top=9)
+        for p, q in zip(got, want, strict=True):
+            assert torch.equal(p, q)
+        grid = torch.full((R, V + 17), 7.0, dtype=dtype, device=DEV)
+        nova.nova_logprobs_backward(x, want.stats, targets, g_logprob=a, entropy=want.entropy, g_entropy=h, mask=mask, scale=0.8, dlogits=grid[:, 2:2 + V])
+        back = nova.nova_logprobs_backward(x.contiguous(), want.stats, targets, g_logprob=a, entropy=want.entropy, g_entropy=h, mask=mask.contiguous(), scale=0.8)
+        assert torch.equal(grid[:, 2:2 + V], back) and bool((grid[:, :2] == 7).all()) and bool((grid[:, 2 + V:] == 7).all())
+
+
+@pytest.mark.parametrize("masks", ["none", "rows", "shared"])
+@pytest.mark.parametrize("V", [1, 3])
+def test_more_rows_than_one_launch(V, masks):
+    # a launch takes 2^22 rows
+    R = (1 << 22) + 3
+    print(f"[case] {R} x {V}, masks: {masks}", flush=True)
+    gen, x, targets = make(R, V, F16)
+    mask = None
+    if masks != "none":
+        mask = torch.rand((R if masks == "rows" else 1, V), device=DEV, generator=gen) < 0.7
+        mask[:, 0] = True
+        if masks == "shared":
+            targets[:] = 0
+        else:
+            mask.scatter_(1, targets.unsqueeze(1), True)
+    f, want = check(x, targets, mask, 0.8, 2)
+    a, h = torch.randn((R,), device=DEV, generator=gen), torch.randn((R,), device=DEV, generator=gen)
+    got = nova.nova_logprobs_backward(x, f.stats, targets, g_logprob=a, entropy=f.entropy, g_entropy=h, mask=mask, scale=0.8)
+    g, size = gradient(x, targets, mask, 0.8, a, h, want)
+    bound = size * 2 * error(V, torch.where(want["lp"] > -60, want["lp"], 60.0), want["L"].unsqueeze(1)) + UNIT[F16] * g.abs() + TINY[F16]
+    within(got, g, bound, "gradient")

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from launches import launches
 from paper_2512_18453_amd import nova
 from test_gpu_q4 import BF16, BWD, DEV, F16, F32, close, make
 
@@ -69,3 +70,21 @@ def test_results_beyond_the_type_are_infinite(M, dtype):
     want = torch.full((M, N), float("inf"), device=DEV)
     want[:, 1::2] *= -1
     assert torch.equal(got.float(), want)
+
+
+@pytest.mark.parametrize("M,dtype", [(1027, F16), (515, F32)])
+def test_more_rows_than_one_launch(M, dtype):
+    # the gradient of 2^24 inputs, the widest there is: 1024 (512) rows are 2^23 workgroups, all that a launch takes
+    N, K, group = 3, 1 << 24, 32
+    print(f"[case] backward {M} x {N} x {K}, {dtype}", flush=True)
+    gen, codes, scales, W = make(N, K, group, dtype)
+    Wb = nova.nova_q4_pack(codes, scales, group, BWD)
+    dy, y = (torch.randn((M, N), device=DEV, generator=gen).to(dtype) for _ in range(2))
+    dx = torch.empty((M, K), dtype=dtype, device=DEV)
+    ws = torch.empty(nova.nova_q4_linear_workspace_bytes(M, N, K, group, dtype, BWD), dtype=torch.uint8, device=DEV)
+    found = launches(lambda: nova.nova_q4_linear_backward(dy, Wb, K, group, y=y, dx=dx, workspace=ws))
+    assert [blocks for _, blocks, _ in found] == [1 << 23, 1 << 18]
+    nova.nova_q4_linear_backward(dy, Wb, K, group, y=y, dx=dx, workspace=ws)
+    for r in (0, M - 4, M - 3, M - 2, M - 1):                # (the launch's last row, and the next one's)
+        d = (dy[r:r + 1] * (y[r:r + 1] > 0)).double()
+        close(dx[r:r + 1], d @ W, d.abs() @ W.abs(), N, 0.0 if dtype == F32 else 2.0 ** -15)
