@@ -223,7 +223,7 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p
             if (t >= 0 && t < a.V) {
                 const bool allowed = !MASK || a.mask[row * a.mask_stride + t];
                 const float x = allowed ? load_f32((const Storage<DT> *)a.logits + row * a.stride + t) : -INFINITY;
-                lp = bad ? nan : empty ? -INFINITY : (x - p.m) * a.scale - log_sum;
+                lp = bad ? nan : empty ? -INFINITY : fma32(x - p.m, a.scale, -log_sum);
             }
             a.logprob[row] = lp;
         }
@@ -231,7 +231,7 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p
     if (lane < a.top) {
         const int64_t at = (int64_t)row * a.top + lane;
         a.top_ids[at] = best ? (int64_t)(0xffffffffu - (unsigned)best) : -1;
-        a.top_logprobs[at] = bad ? nan : best ? (value_of_rank((unsigned)(best >> 32)) - p.m) * a.scale - log_sum : -INFINITY;
+        a.top_logprobs[at] = bad ? nan : best ? fma32(value_of_rank((unsigned)(best >> 32)) - p.m, a.scale, -log_sum) : -INFINITY;
     }
 }
 

@@ -73,3 +73,13 @@ def test_more_rows_than_one_launch(V, masks):
     g, size = gradient(x, targets, mask, 0.8, a, h, want)
     bound = size * 2 * error(V, torch.where(want["lp"] > -60, want["lp"], 60.0), want["L"].unsqueeze(1)) + UNIT[F16] * g.abs() + TINY[F16]
     within(got, g, bound, "gradient")
+
+
+@pytest.mark.parametrize("V", [100, 2049, 30001])
+def test_small_scales_of_large_logits(V):
+    # d = scale (x - M) has two roundings and ln p = d - L a third: two units of 2^-24 of |d| are what `error` has for them, so d is not rounded on the way
+    for scale in (1e-3, 2.3e-4, 7e-3):
+        gen = torch.Generator(device=DEV).manual_seed(V)
+        x = 6e4 * torch.randn((400, V), device=DEV, generator=gen)
+        targets = torch.randint(0, V, (400,), device=DEV, generator=gen)
+        check(x, targets, None, torch.tensor(scale, dtype=F32).item(), 9)
