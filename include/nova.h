@@ -382,7 +382,8 @@ int nova_relu_maxpool2x2(const void *in, void *out, int N, int C, int H, int W, 
  *   codes 0; a group that holds an infinity or a NaN comes back as NaN.
  * nova_q4_pack: from codes [N][K] (device, one byte each; kept within [-8, 7]) and scales [N][ceil(K/group)] (device, dtype).
  * nova_q4_unpack: the inverse, from a layout of either direction; scales may be NULL.
- * Wq: device, 16-byte aligned, at least nova_q4_bytes; fully overwritten by the first two (padding included).
+ * Wq: device, 16-byte aligned, at least nova_q4_bytes; fully overwritten by the first two (padding included).  Like a transformed filter it holds no
+ * record of what it was made for: layouts of other sizes, groups, dtypes or directions can have as many bytes, and the caller keeps them apart.
  * Errors: NOVA_EINVAL; NOVA_ENOSPC if Wq_bytes is less than the layout's size; NOVA_EHIP.
  */
 enum { NOVA_Q4_FORWARD = 0, NOVA_Q4_BACKWARD = 1 };
@@ -402,7 +403,8 @@ int nova_q4_unpack(const void *Wq, size_t Wq_bytes, int N, int K, int group, int
  * nova_q4_linear_backward: dx[m][k] = sum_n d[m][n] W[n][k], d = dy, or with y (the layer's result after its ReLU) d = y > 0 ? dy : 0; y may
  * be NULL.  The weights of a stored layer are constants: there is no gradient of codes, scales or bias.  dy: [M][N], y: [M][N], dx: [M][K] with
  * their row lengths; Wq: NOVA_Q4_BACKWARD layout.  d * s is formed in binary32 and enters the matrix unit in two pieces of 8 bits of mantissa
- * (three for NOVA_F32), so it is rounded to 16 (24) bits; sums in binary32.
+ * (three for NOVA_F32), so it is rounded to 16 (24) bits; sums in binary32.  A product d * s beyond binary32's range is an infinity, with a code of 0 NaN.
+ * Pieces end at 2^-133, where what is smaller than 2^-118 (2^-109) is rounded; so are NOVA_F32 rows of nova_q4_linear, which enter in three pieces.
  *
  * workspace: device, 16-byte aligned, at least nova_q4_linear_workspace_bytes(.. direction) bytes (it may be 0, and the pointer then NULL);
  * nothing in it has to be zero and nothing survives.  Outputs must not overlap any input or the workspace.

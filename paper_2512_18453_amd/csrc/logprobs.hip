@@ -85,9 +85,9 @@ __device__ __forceinline__ rank_t read_lane(rank_t v, int lane)
 struct Sums {
     float m, s, u;
 };
-// Exponents of 2, scale log2 e times t: that factor is c + rest.  c alone is off by up to 1.2 units of 2^-24, alike for all entries of a row: at a scale of 0.9 L and H of rows of
-// 131071 logits were off by 4 and 28 such units where 32 bits throughout leave 1 and 2.  One more multiply per logit: 1024 rows of 131072 bfloat16 logits 55.6 -> 57.5 us.
-// rest is above 0, so that what is infinite in t is so, with its sign, in both products.
+// Exponents of 2, scale log2 e times t: that factor is c + rest.  c alone is off by up to 1.2 units of 2^-24, alike for all entries of a row: at a scale of 0.9
+// L and H of rows of 131071 logits were off by 4 and 28 such units where 32 bits throughout leave 1 and 2.  One more multiply per logit: 1024 rows of 131072
+// bfloat16 logits 55.6 -> 57.5 us.  rest is above 0, so that what is infinite in t is so, with its sign, in both products.
 struct Exponent {
     float c, rest;
 
@@ -235,8 +235,9 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int row, Sums p
     }
 }
 
-// 16 bytes that are used once, from and to any element's address: past the caches.  1024 rows of 131072 bfloat16 logits forward 68 -> 51 us, 256 rows (which the
-// last-level cache could keep) 27 -> 22; written so the gradient 131 -> 92, 34 -> 25 us.  The gradient reads logits as usual: 256 rows 24.7 us against 26.6.
+// 16 bytes that are used once, from and to any element's address: past the caches.  1024 rows of 131072 bfloat16 logits forward 68 -> 51 us (52 with the
+// exponents' second part), 256 rows (which the last-level cache could keep) 27 -> 22; written so the gradient 131 -> 92, 34 -> 25 us.  The gradient reads
+// logits as usual: 256 rows 24.7 us against 26.6.
 typedef unsigned loose16 __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T>
 __device__ __forceinline__ void load_streamed(Eight<T> &e, const T *p)

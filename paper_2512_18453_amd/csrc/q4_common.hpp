@@ -83,7 +83,8 @@ struct Bf16Codes {
 };
 
 // Eight binary32 values as PIECES operands of bfloat16 whose sum they are: each piece but the last is the value cut off behind 8 bits of mantissa, so the
-// rest is exact (and an infinity is all in the first piece); the last is the rest rounded.  Two pieces: within 2^-15 of the value; three: all of it.
+// rest is exact (and an infinity is all in the first piece); the last is the rest rounded.  Two pieces: within 2^-15 of the value; three: all of it, where it
+// is 2^-109 or more (the last place of a piece is 2^-133 at the lowest).
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef bf16 bhalf2 __attribute__((ext_vector_type(2)));
 template <int PIECES>

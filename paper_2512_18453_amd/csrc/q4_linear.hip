@@ -3,7 +3,9 @@
 // Codes are read as panels of 16 columns by 128 positions of the reduction (1 KB, one 16-byte load per lane) and become operands of the matrix unit in
 // registers (q4_common.hpp).
 //   forward   a group's products are summed on the matrix unit with the codes as integers and the sum is scaled in binary32
-//   backward  the scales run along the reduction, so they go to the other operand: d * s in binary32, in two (three) bfloat16 pieces
+//   backward  the scales run along the reduction, so they go to the other operand: d * s in binary32, in two (three) bfloat16 pieces.  Two hold a
+//             product of two bfloat16 numbers; one of binary16 numbers has 22 bits and loses 6, to 2^-5 of what rounding the result does: a third
+//             piece is half as much matrix work again, and pieces of binary16 lack its range
 // Two kernels: for up to 16 rows (q4_few_rows_kernel) the codes' bytes bind and nothing else; more rows (q4_tile_kernel) are shared by four waves through LDS.
 // Where the result's tiles give too few workgroups, the reduction is cut over workgroups too; a third kernel adds the pieces in order.
 #include "q4_common.hpp"
@@ -33,9 +35,10 @@ template <int DT, bool BACK> constexpr int kPieces = DT == NOVA_F32 ? 3 : BACK ?
 template <bool HALF> using Codes = std::conditional_t<HALF, F16Codes, Bf16Codes>;
 template <bool HALF> constexpr float kUnit = HALF ? 1.0f : kCodeUnit;        // what the sums over such codes are multiplied by, at the end
 
-// Forward, a group's sum is formed before its scale comes to it, and with rows of binary32 or bfloat16 such a sum can pass binary32's range (|x| adding up to 7e38) where the result does not.  A
-// workgroup whose results are not all finite makes them again, from rows that are a 256th, in which no group's sum passes it, and writes those that were not: what holds infinities
-// or NaN takes twice as long, anything else the check: 1 x 4096 x 1000 in binary32 6.83 -> 7.06 us, 32 x 4096 x 4096 in bfloat16 10.8 -> 11.2, 1024 x 8192 x 8192 148.6 -> 149.7.
+// Forward, a group's sum is formed before its scale comes to it, and with rows of binary32 or bfloat16 such a sum can pass binary32's range (|x| adding up to
+// 7e38) where the result does not.  A workgroup whose results are not all finite makes them again, from rows that are a 256th, in which no group's sum passes
+// it, and writes those that were not: what holds infinities or NaN takes twice as long, anything else the check: 1 x 4096 x 1000 in binary32 6.83 -> 7.06 us,
+// 32 x 4096 x 4096 in bfloat16 10.8 -> 11.2, 1024 x 8192 x 8192 148.6 -> 149.7.
 template <int DT, bool BACK> constexpr int kPasses = BACK || DT == NOVA_F16 ? 1 : 2;
 constexpr float kShrunk = 1.0f / 256;
 template <int DT, int PASS>
@@ -83,9 +86,9 @@ __device__ __forceinline__ void write_result(const Q4Call &a, int m, int n, floa
 // A wave makes 16 columns for all rows; `sharing` waves of a workgroup take the panels of the same columns in turn and add up through LDS in the order of their
 // numbers.  Bound by the codes' bytes: a wave has AHEAD panels on their way in registers, with the rows' operand that belongs to them.  That is loaded
 // along the rows, 256 bytes of four rows at a time, and goes through a piece of LDS that is the wave's own to the lanes that need it: read from memory as the
-// matrix unit takes it, 16 rows side by side, each four lanes lie in four cache lines, and one row of 25088 by 4096 took 16.5 us, 16 rows 27.  Now one row takes
-// 11.4 us (53 MB, 4.6 TB/s) with three sets of weights in turn and 12.8 with six, which the last-level cache cannot keep; 8 rows by 8192 x 4096 6.6: every 16 columns read all
-// rows once more from L2.  The codes are streamed past it (1.5 us more without).
+// matrix unit takes it, 16 rows side by side, each four lanes lie in four cache lines, and one row of 25088 by 4096 took 16.5 us, 16 rows 27.  Now one row
+// takes 11.4 us (53 MB, 4.6 TB/s) with three sets of weights in turn and 12.8 with six, which the last-level cache cannot keep; 8 rows by 8192 x 4096 7.2:
+// every 16 columns read all rows once more from L2.  The codes are streamed past it (1.5 us more without).
 template <int DT, int GROUP, int QUADS>
 struct FewRowsStage {
     uint4v codes;
@@ -132,7 +135,8 @@ __device__ __forceinline__ unsigned q4_few_rows_pass(const Q4Call &a, int sharin
 
     float4v acc = {0, 0, 0, 0}, part = {0, 0, 0, 0};
     auto multiply = [&](const Stage &s) NOVA_INLINE {
-        // 16-byte block b of row r lies at block b ^ r % 8: the eight rows that are read at a time lie in different banks
+        // 16-byte block b of row r lies at block b ^ r % 8: eight rows that are read at a time lie in different banks.  (Four rows are each read by four lanes:
+        // 3 cycles of conflicts per LDS instruction are counted there, some 400 of a wave's 24000.)
 #pragma unroll
         for (int r = 0; r < QUADS; ++r) {
             const int row = 4 * r + lane / 16;
@@ -207,11 +211,12 @@ __global__ void __launch_bounds__(1024) q4_few_rows_kernel(const Q4Call a, int s
 // such stages: one is filled while the other is multiplied; what fills them is loaded AHEAD - 1 stages before.  A row's 16-byte blocks are stored at
 // block ^ row % 16, so the 16 rows that a fragment's load touches lie in different banks.
 //
-// Many rows: 1024 by 8192 x 8192 in bfloat16 143 us, 961 TFLOP/s where a large library product of that type reaches 1211.  A panel is made into operands once per
+// Many rows: 1024 by 8192 x 8192 in bfloat16 146 us, 941 TFLOP/s where a large library product of that type reaches 1211.  A panel is made into operands once per
 // 64 rows, three vector instructions for each of its matrix instructions, so both units are busy (without making operands it took 124 us); 256 columns halve the
 // LDS reads of 128 (162 us); eight waves on 128 rows were slower (174 to 227), as all of them wait at one barrier, and so were matrix instructions of 32 by 32
-// (151).  Few tiles: 32 rows of the first layer behind the VGG stack (53 MB) 19.4 us, of which the second launch and 8 MB of pieces take 6; four groups of waves
-// per workgroup that shared a tile's stages instead of most of the cut gained nothing.  Gradient: twice the products, 512 rows by 4096 x 16384 146 us.
+// (151).  Few tiles: 32 rows of the first layer behind the VGG stack (53 MB) 18.9 us, of which the second launch and 8 MB of pieces take 6; four groups of waves
+// per workgroup that shared a tile's stages instead of most of the cut gained nothing.  Gradient: twice the products, 512 rows by 4096 x 16384 148 us; the versions
+// of smaller groups and the narrower tiles that go with them 215 us (64) and 378 (32).
 template <int MT_, int NT_, int AHEAD_>
 struct Tile {
     static constexpr int MT = MT_, NT = NT_, AHEAD = AHEAD_, ROWS = 16 * MT, PANELS = 4 * NT;
@@ -453,7 +458,8 @@ struct Q4Shape { int mt, nt, waves, splits, split_chunks; };
 // many as the fullest unit has; and for a cut reduction a launch and the pieces, added one behind the other, written and read.
 static double q4_tile_time(int M, const Q4Layout &q, int dtype, int mt, int nt, int splits)
 {
-    const int64_t row_blocks = ((int64_t)M + 16 * mt - 1) / (16 * mt), blocks = ceil_div(q.row_tiles, 4 * nt) * row_blocks * splits, on_a_unit = (blocks + 255) / 256;
+    const int64_t row_blocks = ((int64_t)M + 16 * mt - 1) / (16 * mt), blocks = ceil_div(q.row_tiles, 4 * nt) * row_blocks * splits;
+    const int64_t on_a_unit = (blocks + 255) / 256;
     double stage = nt == 4 ? 1.6 : mt == 4 ? 0.83 : mt == 2 ? 0.58 : 0.45;
     if (q.backward) stage = mt == 4 ? 1.62 : mt == 2 ? 1.0 : 0.7;
     if (dtype == NOVA_F32) stage *= 2;
