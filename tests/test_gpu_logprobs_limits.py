@@ -84,3 +84,33 @@ def test_small_scales_of_large_logits(V):
         x = 6e4 * torch.randn((400, V), device=DEV, generator=gen)
         targets = torch.randint(0, V, (400,), device=DEV, generator=gen)
         check(x, targets, None, torch.tensor(scale, dtype=F32).item(), 9)
+
+
+def test_longest_row():
+    # V = 2^31 - 1, as long as a row can be: 64 slices forward, 262144 workgroups a row backward
+    V, step = 2 ** 31 - 1, 1 << 27
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.empty((1, V), dtype=BF16, device=DEV)
+    for lo in range(0, V, step):
+        x[0, lo:lo + step] = torch.randn((min(step, V - lo),), device=DEV, generator=gen)
+    at = [0, V - 1, 1 << 30, (1 << 31) - 9, 77777777]
+    x[0, at] = torch.tensor([30.0, 29.0, 28.0, 27.0, 26.0], device=DEV).to(BF16)
+    targets = torch.tensor([V - 1], device=DEV)
+    got = nova.nova_logprobs(x, targets, top=5)
+    sums = torch.zeros(2, dtype=torch.float64, device=DEV)
+    for lo in range(0, V, step):
+        d = x[0, lo:lo + step].double() - 30.0
+        sums += torch.stack([d.exp().sum(), (d.exp() * d).sum()])
+    L, E = sums[0].log().item(), (sums[1] / sums[0]).item()
+    assert got.top_ids[0].tolist() == at and got.stats[0, 0].item() == 30.0
+    assert abs(got.stats[0, 1].item() - L) <= error(V, torch.zeros(()), torch.tensor(L)).item()
+    assert abs(got.logprob.item() - (-1.0 - L)) <= error(V, torch.ones(()), torch.tensor(L)).item()
+    assert abs(got.entropy.item() - (L - E)) <= error(V, torch.tensor(60.0), torch.tensor(L)).item() * (1 + L - E)
+    a = torch.ones(1, device=DEV)
+    dx = nova.nova_logprobs_backward(x, got.stats, targets, g_logprob=a, dlogits=x.clone())
+    for lo in range(0, V, step):
+        p = (x[0, lo:lo + step].double() - 30.0 - L).exp()
+        want = -p
+        if lo + step >= V:
+            want[-1] += 1.0
+        within(dx[0, lo:lo + step], want, UNIT[BF16] * want.abs() + 2.0 ** -17 * p + TINY[BF16], "gradient")

@@ -88,3 +88,28 @@ def test_more_rows_than_one_launch(M, dtype):
     for r in (0, M - 4, M - 3, M - 2, M - 1):                # (the launch's last row, and the next one's)
         d = (dy[r:r + 1] * (y[r:r + 1] > 0)).double()
         close(dx[r:r + 1], d @ W, d.abs() @ W.abs(), N, 0.0 if dtype == F32 else 2.0 ** -15)
+
+
+@pytest.mark.parametrize("M", [3, 40])
+def test_weights_beyond_32_bits(M):
+    # 9.4e9 weights: codes and layouts of more than 2^32 bytes
+    N, K, group, dtype = (1 << 20) + 5, 9001, 128, F16
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    codes = torch.randint(-8, 8, (N, K), dtype=torch.int8, device=DEV, generator=gen)
+    scales = (torch.rand((N, -(-K // group)), device=DEV, generator=gen) * 0.1 + 0.002).to(dtype)
+
+    def weights(rows, columns):
+        return codes[rows][:, columns].double() * scales[rows][:, columns // group].double()
+    every, some = slice(None), torch.tensor([0, 1, 524287, 524288, N - 2, N - 1], device=DEV)
+    x = torch.randn((M, K), device=DEV, generator=gen).to(dtype)
+    Wq = nova.nova_q4_pack(codes, scales, group)
+    W = weights(some, torch.arange(K, device=DEV))
+    close(nova.nova_q4_linear(x, Wq, N, group)[:, some], x.double() @ W.T, x.double().abs() @ W.abs().T, K)
+    back = nova.nova_q4_unpack(Wq, N, K, group, dtype)
+    assert torch.equal(back[0], codes) and torch.equal(back[1], scales)
+    del Wq, back
+    Wb = nova.nova_q4_pack(codes, scales, group, BWD)
+    dy = torch.randn((M, N), device=DEV, generator=gen).to(dtype)
+    some = torch.tensor([0, 127, 128, 4500, K - 1], device=DEV)
+    W = weights(every, some)
+    close(nova.nova_q4_linear_backward(dy, Wb, K, group)[:, some], dy.double() @ W, dy.double().abs() @ W.abs(), N, 2.0 ** -15)
