@@ -33,8 +33,8 @@ def _linear(name, M, N, K, dtype, bias=False, relu=False):
     return dict(name=name, kind="linear", M=M, N=N, K=K, dtype=dtype, bias=bias, relu=relu)
 
 
-def _backward(name, M, N, K, dtype, format, relu=False):
-    return dict(name=name, kind="linear_backward", M=M, N=N, K=K, dtype=dtype, format=format, relu=relu)
+def _backward(name, M, N, K, dtype, format, dw, relu=False):
+    return dict(name=name, kind="linear_backward", M=M, N=N, K=K, dtype=dtype, format=format, dw=dw, relu=relu)
 
 
 def _matmul(name, M, N, K, dtype, formats, block_b):
@@ -63,10 +63,10 @@ def listed():
         _matmul("odd_sizes_f32", 517, 5001, 2055, "f32", ("e5m2", "e4m3"), 1),
         # tokens laid out once for several projections, weights with a scale per 128 x 128: the matrix units bind; the largest call
         _matmul("square_bf16", 8192, 8192, 8192, "bf16", ("e4m3", "e4m3"), 128),
-        # the backward pass through the second fully connected layer and its ReLU at batch 32
-        _backward("fc2_backward_f16", 32, 4096, 4096, "f16", "e5m2", relu=True),
-        # ... and through a wide projection of many tokens
-        _backward("many_rows_backward_bf16", 4096, 4096, 16384, "bf16", "e4m3"),
+        # the backward pass through the second fully connected layer and its ReLU at batch 32, the weights' gradient in binary32 for an optimizer's own copy
+        _backward("fc2_backward_f16", 32, 4096, 4096, "f16", "e5m2", "f32", relu=True),
+        # ... and through a wide projection of many tokens, the weights' gradient in the layer's type
+        _backward("many_rows_backward_bf16", 4096, 4096, 16384, "bf16", "e4m3", "bf16"),
         # what a training step does to the first layer's weights after their update
         _quantize("fc1_weights_f16", 4096, 25088, "f16", "e4m3", 128, False),
         # a batch's activations for the product that gives the weights' gradient, sizes that are whole numbers of nothing
@@ -112,7 +112,7 @@ def draw(rng):
     if kind == "matmul":
         return dict(kind=kind, M=M, N=N, K=K, dtype=dtype, format_a=rng.choice(["e4m3", "e5m2"]), format_b=rng.choice(["e4m3", "e4m3", "e5m2"]),
                     block_b=rng.choice([1, 128]))
-    return dict(kind=kind, M=M, N=N, K=K, dtype=dtype, format=rng.choice(["e4m3", "e5m2"]), relu=rng.random() < 0.4)
+    return dict(kind=kind, M=M, N=N, K=K, dtype=dtype, format=rng.choice(["e4m3", "e5m2"]), dw=rng.choice(["f32", dtype]), relu=rng.random() < 0.4)
 
 
 # ---- blocks of 128 (the plain form of the quantisation) ----
@@ -215,7 +215,7 @@ def prepare(case, seed):
                 need = nova.nova_f8_linear_workspace_bytes(M, N, K, dtype)
             else:
                 s["dx"] = torch.empty((M, K), dtype=dtype, device=DEV)
-                s["dw"], s["dbias"] = torch.empty((N, K), device=DEV), torch.empty((N,), device=DEV)
+                s["dw"], s["dbias"] = torch.empty((N, K), dtype=DTYPES[case["dw"]], device=DEV), torch.empty((N,), device=DEV)
                 need = nova.nova_f8_linear_backward_workspace_bytes(M, N, K, dtype)
             s["workspace"] = torch.empty(need, dtype=torch.uint8, device=DEV)
         elif kind == "matmul":
@@ -251,7 +251,7 @@ def _plain_linear_backward(s):
     dx = _values(*_quantized(d, case["format"], 1), 1) @ _values(s["w"], s["sw"], 128)
     # the weights' gradient sums over the rows, so there the blocks run along them
     dw = _values(*_quantized(d.T, case["format"], 1), 1) @ _values(*_quantized(s["x"].T, "e4m3", 1), 1).T
-    return dict(dx=dx.to(s["dy"].dtype), dw=dw, dbias=d.sum(0, dtype=torch.float64).float())
+    return dict(dx=dx.to(s["dy"].dtype), dw=dw.to(DTYPES[case["dw"]]), dbias=d.sum(0, dtype=torch.float64).float())
 
 
 def _plain_matmul(s):
@@ -320,7 +320,7 @@ def work(case):
         return {"bytes": N * K + scales(N, K, 128) + (M * K + M * N) * es + N * es * case["bias"], "flops": 2.0 * M * N * K}
     if case["kind"] == "matmul":
         return {"bytes": M * K + N * K + scales(M, K, 1) + scales(N, K, case["block_b"]) + M * N * es, "flops": 2.0 * M * N * K}
-    return {"bytes": N * K + scales(N, K, 128) + (M * N * (1 + case["relu"]) + 2 * M * K) * es + 4.0 * (N * K + N), "flops": 4.0 * M * N * K}
+    return {"bytes": N * K + scales(N, K, 128) + (M * N * (1 + case["relu"]) + 2 * M * K) * es + N * K * SIZES[case["dw"]] + 4 * N, "flops": 4.0 * M * N * K}
 
 
 # ---- the definition in 64 bits ----
