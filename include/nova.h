@@ -13,7 +13,8 @@
  * extension); stride 1, correlation (no kernel flip), no bias.
  *
  * Further down, what comes behind a convolution stack: fully connected layers with 4-bit weights, log
- * probabilities of classes or tokens, and the gradients of both.
+ * probabilities of classes or tokens, and the gradients of both; fully connected layers that train in 8-bit
+ * floating point, and dropout between them.
  *
  * Conventions for every call
  *   - "host" pointers are ordinary process memory, "device" pointers are HIP device memory
@@ -24,7 +25,7 @@
  *     HIP error code (thread-local).
  *   - Return value: NOVA_OK (0) or a negative NOVA_E* code; nothing throws or aborts.
  *   - dtype selects the storage format of x, w, U, V, y: NOVA_F16 (IEEE binary16) or
- *     NOVA_F32; the calls behind a convolution stack (4-bit layers, log probabilities) take NOVA_BF16 too.  Arithmetic: transforms in binary32 (filter transform in binary64),
+ *     NOVA_F32; the calls behind a convolution stack (4-bit and 8-bit layers, log probabilities, dropout) take NOVA_BF16 too.  Arithmetic: transforms in binary32 (filter transform in binary64),
  *     channel contraction on the matrix cores with binary32 accumulation.
  */
 #ifndef NOVA_H
@@ -53,7 +54,7 @@ enum {
     NOVA_ENOMEM = -8        /* host allocation failed */
 };
 
-enum { NOVA_F32 = 0, NOVA_F16 = 1, NOVA_BF16 = 2 };   /* NOVA_BF16 (bfloat16): the nova_q4_* and nova_logprobs* calls only */
+enum { NOVA_F32 = 0, NOVA_F16 = 1, NOVA_BF16 = 2 };   /* NOVA_BF16 (bfloat16): the nova_q4_*, nova_logprobs*, nova_f8_* and nova_dropout* calls only */
 enum { NOVA_MATRIX_A = 0, NOVA_MATRIX_BT = 1, NOVA_MATRIX_G = 2 };
 
 /* flags of nova_winograd_conv2d / nova_output_transform / nova_contract */
@@ -65,6 +66,8 @@ enum {
                                a NaN in a window makes that output NaN.  The step between the blocks of a
                                VGG-style stack, without writing and re-reading the unpooled layer */
 };
+/* ... of nova_f8_matmul and nova_f8_linear_backward */
+enum { NOVA_FLAG_ADD = 8 };  /* the result is added to what the output holds */
 
 /* ------------------------------------------------------------------ transforms (host) */
 
@@ -450,6 +453,84 @@ int nova_logprobs(const void *logits, int64_t stride, const int64_t *targets, co
 int nova_logprobs_backward(const void *logits, int64_t stride, const float *stats, const int64_t *targets, const float *g_logprob,
                            const float *entropy, const float *g_entropy, const uint8_t *mask, int64_t mask_stride, int rows, int V, float scale,
                            int dtype, void *dlogits, int64_t dstride, void *stream);
+
+/* ------------------------------------------------------------------ layers in 8-bit floating point */
+
+/*
+ * Matrices of 8-bit floating-point codes with a scale per block of 128, their products, and the fully connected layer that trains on them.
+ *     X[r][k] = code[r][k] * s[r / block][k / 128],   block 1 (a scale per row and 128 columns) or 128 (per 128 x 128),
+ * codes in NOVA_F8_E4M3 (largest 448) or NOVA_F8_E5M2 (largest 57344), the OCP formats without and with infinities; scales binary32.
+ * A matrix is laid out for products that sum along its rows ("columns" is the length of the sum): panels [ceil(rows/16)][ceil(columns/128)] of 2048 bytes,
+ * byte 1024 h + 256 b + 16 i + v holding row 16 r + i at column 128 c + 32 b + 16 h + v (h < 2, b < 4, i < 16, v < 16); then the scales
+ * [ceil(columns/128)][pitch], pitch = rows rounded up to 16 (block 1) or ceil(rows/128); padding is zero.
+ *
+ * nova_f8_bytes: size of a layout (0 for invalid arguments).
+ * nova_f8_quantize: from x [rows][columns] (device, dtype, ldx elements from row to row; 0: one row that stands for all): s = max|x| / largest code, divided in
+ *   binary32; code = x / s, divided in binary32, rounded to nearest, ties to even, and kept within the largest code.  A block of zeros (or whose scale rounds to zero) has scale
+ *   0 and codes 0; a block that holds an infinity or a NaN has scale NaN and codes 0, and what is formed of it is NaN.  transposed = 1: the layout of x^T (columns rows
+ *   of `rows` columns, blocks along x's columns).
+ * nova_f8_pack: from codes [rows][columns] and scales [ceil(rows/block)][ceil(columns/128)] (device, both without gaps); transposed = 1 (block 128 only): the layout of
+ *   the transpose of what they stand for, with the same values, as nova_f8_linear_backward takes the weights.
+ * nova_f8_unpack: the inverse, rows and columns being the layout's; scales may be NULL.
+ * Xq: device, 16-byte aligned; written whole by the first two.  A layout holds no record of what it was made for.
+ * rows, columns: 1 .. 2^31 - 1.  Errors: NOVA_EINVAL; NOVA_ENOSPC if Xq_bytes is less than the layout's size; NOVA_EHIP.
+ */
+enum { NOVA_F8_E4M3 = 0, NOVA_F8_E5M2 = 1 };
+size_t nova_f8_bytes(int rows, int columns, int block);
+int nova_f8_quantize(const void *x, int64_t ldx, int rows, int columns, int dtype, int format, int block, int transposed, void *Xq, size_t Xq_bytes, void *stream);
+int nova_f8_pack(const uint8_t *codes, const float *scales, int rows, int columns, int block, int transposed, void *Xq, size_t Xq_bytes, void *stream);
+int nova_f8_unpack(const void *Xq, size_t Xq_bytes, int rows, int columns, int block, uint8_t *codes, float *scales, void *stream);
+
+/*
+ * nova_f8_matmul: out[m][n] = sum_k A[m][k] B[n][k] + bias[n], of two layouts [M][K] and [N][K]; then with NOVA_FLAG_RELU max(., 0) (NaN stays NaN), or with
+ * NOVA_FLAG_ADD added to what out holds.  out: device [M][N] of dtype, ldout >= N; bias: device [N] of dtype or NULL.
+ * nova_f8_linear: the layer y = Q(x) W^T + bias (ReLU as above), Q the quantisation to NOVA_F8_E4M3 with block 1 on the way; x [M][K], y [M][N] of dtype;
+ *   Wq: layout of W [N][K], NOVA_F8_E4M3, block 128.
+ * nova_f8_linear_backward: with d = dy, or with y (the layer's result after its ReLU) d = y > 0 ? dy : 0 (y may be NULL),
+ *     dx = Q(d) W,   dw = Q(d^T) Q(x^T)^T,   dbias = sum_m d[m][.]
+ *   Q(d) and Q(d^T) in `format`, Q(x^T) in NOVA_F8_E4M3, all of block 1.  dx [M][K] of dtype, dw [N][K] of dw_dtype (NOVA_F32 or dtype), dbias [N] in binary32; with NOVA_FLAG_ADD
+ *   the latter two are added to what is there.  Each of the three may be NULL; dx needs Wq, the layout of W^T [K][N] (pack or quantise with transposed = 1; block 128, NOVA_F8_E4M3),
+ *   dw needs x.  With M = 0 dw and dbias are sums over nothing: zero, or left as they are.
+ * dtype: NOVA_F32, NOVA_F16, NOVA_BF16.  Rows are given with elements from row to row (inputs: at least the row's length, or 0 for one row that stands for all; with
+ * one row it does not matter) and need no alignment beyond the element's.
+ * Sums of the 128 products of a chunk are formed on the matrix unit, scaled by the product of the two scales (in binary32: beyond its range infinite, and NaN where the
+ * sum is 0) and added up in binary32; results are rounded once.  For results in NOVA_F32 a chunk's sum is as exact as binary32; for the two others it is formed at twice that
+ * rate, where the products of eight neighbouring columns are cut off below 2^-13 of the power of two of the largest of them (1.5e-5 of the sum on normal data).  Sums are formed in a fixed order: equal calls give equal bits.
+ * M 0 .. 2^31 - 1; N, K 1 .. 2^24.  workspace: device, 16-byte aligned, at least the _workspace_bytes of the same sizes (for nova_f8_matmul it may be 0, and the
+ * pointer then NULL); nothing in it has to be zero and nothing survives.  Outputs must not overlap any input or the workspace.
+ * Errors: NOVA_EINVAL, NOVA_ENOSPC (a layout's bytes or workspace_bytes too small), NOVA_EHIP.
+ */
+size_t nova_f8_matmul_workspace_bytes(int M, int N, int K, int block_a, int block_b, int dtype);
+int nova_f8_matmul(const void *Aq, size_t Aq_bytes, int block_a, int format_a, const void *Bq, size_t Bq_bytes, int block_b, int format_b, const void *bias,
+                   void *out, int64_t ldout, int M, int N, int K, int dtype, int flags, void *workspace, size_t workspace_bytes, void *stream);
+size_t nova_f8_linear_workspace_bytes(int M, int N, int K, int dtype);
+int nova_f8_linear(const void *x, int64_t ldx, const void *Wq, size_t Wq_bytes, const void *bias, void *y, int64_t ldy, int M, int N, int K, int dtype, int flags,
+                   void *workspace, size_t workspace_bytes, void *stream);
+size_t nova_f8_linear_backward_workspace_bytes(int M, int N, int K, int dtype);
+int nova_f8_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, int format, const void *Wq, size_t Wq_bytes, void *dx, int64_t lddx,
+                            const void *x, int64_t ldx, void *dw, int64_t lddw, int dw_dtype, float *dbias, int M, int N, int K, int dtype, int flags,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------ dropout */
+
+/*
+ * Dropout whose mask is a function of (seed, offset, row, column) and is never stored:
+ *     y = f(x) / (1 - p) where an element is kept, else 0 (whatever x holds);   f(x) = x, or max(x, 0) with NOVA_FLAG_RELU (NaN stays NaN);   + residual, if given
+ * nova_dropout_backward: dx = dy / (1 - p) where kept (the same seed, offset and p) and, with gate, where gate > 0; else 0.  Behind NOVA_FLAG_RELU gate is x, or y if no
+ *   residual was added.  The residual's gradient is dy itself.
+ * An element is kept if its 32 random bits u are at least round(p 2^32): u = 65536 h + l, where h is the 16 bits number column % 8 (the lower half of a word first) of the
+ * four words of Philox 4x32-10 with key = seed (lower word first) and counter = (column / 8, row, o's lower word, o's upper word), and l the same of counter
+ * (column / 8, row + 2^31, ..); o = offset + *device_offset (device, one 64-bit number; NULL: 0), read when the kernel runs, so that the replays of a captured graph can
+ * draw new masks.  The mask does not depend on the number of rows and columns, on dtype or strides.
+ * p: 0 .. 1; p = 1 keeps nothing.  x, residual, gate, dy: device, dtype (NOVA_F32, NOVA_F16, NOVA_BF16), given with elements from row to row as above.  The factor 1 / (1 - p) is
+ * binary32, x times it is rounded to binary32 before the residual comes to it, and the result is rounded once more.  y (dx) may be any of the inputs (same pointer and
+ * row length); otherwise it must not overlap them.
+ * rows, columns: 0 .. 2^31 - 1.  Errors: NOVA_EINVAL, NOVA_EHIP.
+ */
+int nova_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldresidual, void *y, int64_t ldy, int rows, int columns, int dtype, double p,
+                 uint64_t seed, uint64_t offset, const uint64_t *device_offset, int flags, void *stream);
+int nova_dropout_backward(const void *dy, int64_t lddy, const void *gate, int64_t ldgate, void *dx, int64_t lddx, int rows, int columns, int dtype, double p,
+                          uint64_t seed, uint64_t offset, const uint64_t *device_offset, void *stream);
 
 /* ------------------------------------------------------------------ misc */
 const char *nova_strerror(int code);

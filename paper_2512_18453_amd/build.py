@@ -20,7 +20,8 @@ LIB = os.path.join(HERE, "libnova.so")
 
 SOURCES = ["transforms.cpp", "discovery.cpp", "api.cpp", "filter_transform.hip", "input_transform.hip",
            "contract.hip", "output_transform.hip", "pool.hip", "static_workspace.hip", "int8.hip", "fused_output.hip", "contract_output.hip", "layer.hip", "contract_columns.hip",
-           "few_channels.hip", "q4_layout.hip", "q4_linear.hip", "logprobs.hip"]
+           "few_channels.hip", "q4_layout.hip", "q4_linear.hip", "logprobs.hip",
+           "f8_layout.hip", "f8_matmul.hip", "dropout.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wno-unused-function"]
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # Up to 56 bytes of a kernel's arguments -- pointers and sizes, 14 of the 16 scalar registers that a launch can fill; two hold the argument pointer --

@@ -544,6 +544,201 @@ extern "C" int nova_logprobs_backward(const void *logits, int64_t stride, const 
     return hip_result(launch_logprobs_backward(a, dtype, stream));
 }
 
+// ---- layers in 8-bit floating point ----
+
+static bool f8_block_ok(int block) { return block == 1 || block == 128; }
+static bool f8_format_ok(int format) { return format == NOVA_F8_E4M3 || format == NOVA_F8_E5M2; }
+static bool f8_size_ok(int n) { return n >= 1 && n <= (1 << 24); }
+static size_t padded(const F8Layout &q) { return align256(q.bytes()); }
+
+extern "C" size_t nova_f8_bytes(int rows, int columns, int block)
+{
+    if (rows < 1 || columns < 1 || !f8_block_ok(block)) return 0;
+    return make_f8_layout(rows, columns, block).bytes();
+}
+
+extern "C" int nova_f8_quantize(const void *x, int64_t ldx, int rows, int columns, int dtype, int format, int block, int transposed, void *Xq, size_t Xq_bytes,
+                                void *stream)
+{
+    if (rows < 1 || columns < 1 || !any_dtype_ok(dtype) || !f8_format_ok(format) || !f8_block_ok(block) || (transposed & ~1) || !Xq || !aligned16(Xq) ||
+        !read_rows_ok(x, ldx, rows, columns))
+        return NOVA_EINVAL;
+    const F8Layout q = transposed ? make_f8_layout(columns, rows, block) : make_f8_layout(rows, columns, block);
+    if (Xq_bytes < q.bytes()) return NOVA_ENOSPC;
+    const F8Source src = {x, ldx, nullptr, 0, rows, columns, dtype};
+    return hip_result(launch_f8_quantize(src, q, format, transposed, Xq, stream));
+}
+
+extern "C" int nova_f8_pack(const uint8_t *codes, const float *scales, int rows, int columns, int block, int transposed, void *Xq, size_t Xq_bytes, void *stream)
+{
+    if (!codes || !scales || rows < 1 || columns < 1 || !f8_block_ok(block) || (transposed & ~1) || (transposed && block == 1) || !Xq || !aligned16(Xq))
+        return NOVA_EINVAL;
+    const F8Layout q = transposed ? make_f8_layout(columns, rows, block) : make_f8_layout(rows, columns, block);
+    if (Xq_bytes < q.bytes()) return NOVA_ENOSPC;
+    return hip_result(launch_f8_pack(codes, scales, q, transposed, Xq, stream));
+}
+
+extern "C" int nova_f8_unpack(const void *Xq, size_t Xq_bytes, int rows, int columns, int block, uint8_t *codes, float *scales, void *stream)
+{
+    if (!Xq || !aligned16(Xq) || !codes || rows < 1 || columns < 1 || !f8_block_ok(block)) return NOVA_EINVAL;
+    const F8Layout q = make_f8_layout(rows, columns, block);
+    if (Xq_bytes < q.bytes()) return NOVA_ENOSPC;
+    return hip_result(launch_f8_unpack(Xq, q, codes, scales, stream));
+}
+
+static bool f8_product_ok(int M, int N, int K, int dtype) { return M >= 0 && f8_size_ok(N) && f8_size_ok(K) && any_dtype_ok(dtype); }
+
+// ReLU alone, or a sum that is added to what is there
+static bool f8_flags_ok(int flags) { return flags == 0 || flags == NOVA_FLAG_RELU || flags == NOVA_FLAG_ADD; }
+
+extern "C" size_t nova_f8_matmul_workspace_bytes(int M, int N, int K, int block_a, int block_b, int dtype)
+{
+    if (!f8_product_ok(M, N, K, dtype) || !f8_block_ok(block_a) || !f8_block_ok(block_b) || M == 0) return 0;
+    return f8_matmul_workspace(M, N, K);
+}
+
+extern "C" int nova_f8_matmul(const void *Aq, size_t Aq_bytes, int block_a, int format_a, const void *Bq, size_t Bq_bytes, int block_b, int format_b,
+                              const void *bias, void *out, int64_t ldout, int M, int N, int K, int dtype, int flags, void *workspace, size_t workspace_bytes,
+                              void *stream)
+{
+    if (!f8_product_ok(M, N, K, dtype) || !f8_flags_ok(flags) || !f8_block_ok(block_a) || !f8_block_ok(block_b) || !f8_format_ok(format_a) ||
+        !f8_format_ok(format_b) || !Bq || !aligned16(Bq))
+        return NOVA_EINVAL;
+    const F8Operand b = {Bq, make_f8_layout(N, K, block_b), format_b};
+    if (Bq_bytes < b.layout.bytes()) return NOVA_ENOSPC;
+    if (M == 0) return NOVA_OK;
+    if (!Aq || !aligned16(Aq) || !write_rows_ok(out, ldout, M, N)) return NOVA_EINVAL;
+    const F8Operand a = {Aq, make_f8_layout(M, K, block_a), format_a};
+    const size_t need = f8_matmul_workspace(M, N, K);
+    if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
+    if (Aq_bytes < a.layout.bytes() || workspace_bytes < need) return NOVA_ENOSPC;
+    return hip_result(launch_f8_matmul(a, b, bias, out, ldout, dtype, flags, workspace, stream));
+}
+
+extern "C" size_t nova_f8_linear_workspace_bytes(int M, int N, int K, int dtype)
+{
+    if (!f8_product_ok(M, N, K, dtype) || M == 0) return 0;
+    return padded(make_f8_layout(M, K, 1)) + f8_matmul_workspace(M, N, K);
+}
+
+extern "C" int nova_f8_linear(const void *x, int64_t ldx, const void *Wq, size_t Wq_bytes, const void *bias, void *y, int64_t ldy, int M, int N, int K,
+                              int dtype, int flags, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!f8_product_ok(M, N, K, dtype) || (flags & ~NOVA_FLAG_RELU) || !Wq || !aligned16(Wq)) return NOVA_EINVAL;
+    const F8Operand w = {Wq, make_f8_layout(N, K, 128), NOVA_F8_E4M3};
+    if (Wq_bytes < w.layout.bytes()) return NOVA_ENOSPC;
+    if (M == 0) return NOVA_OK;
+    if (!read_rows_ok(x, ldx, M, K) || !write_rows_ok(y, ldy, M, N) || !workspace || !aligned16(workspace)) return NOVA_EINVAL;
+    if (workspace_bytes < nova_f8_linear_workspace_bytes(M, N, K, dtype)) return NOVA_ENOSPC;
+    const F8Source src = {x, ldx, nullptr, 0, M, K, dtype};
+    const F8Operand a = {workspace, make_f8_layout(M, K, 1), NOVA_F8_E4M3};
+    if (int err = launch_f8_quantize(src, a.layout, a.format, 0, workspace, stream)) return hip_result(err);
+    return hip_result(launch_f8_matmul(a, w, bias, y, ldy, dtype, flags, (char *)workspace + padded(a.layout), stream));
+}
+
+// The parts of a backward call's workspace, in their order
+struct F8BackwardParts {
+    F8Layout d, d_transposed, x_transposed;
+    size_t d_at, d_transposed_at, x_at, sums_at, products_at, bytes;
+};
+static F8BackwardParts f8_backward_parts(int M, int N, int K)
+{
+    F8BackwardParts p;
+    p.d = make_f8_layout(M, N, 1);
+    p.d_transposed = make_f8_layout(N, M, 1);
+    p.x_transposed = make_f8_layout(K, M, 1);
+    p.d_at = 0;
+    p.d_transposed_at = padded(p.d);
+    p.x_at = p.d_transposed_at + padded(p.d_transposed);
+    p.sums_at = p.x_at + padded(p.x_transposed);
+    p.products_at = p.sums_at + align256((size_t)p.d_transposed.chunks * N * 4);
+    const size_t dx = f8_matmul_workspace(M, K, N), dw = f8_matmul_workspace(N, K, M);
+    p.bytes = p.products_at + (dx > dw ? dx : dw);
+    return p;
+}
+
+extern "C" size_t nova_f8_linear_backward_workspace_bytes(int M, int N, int K, int dtype)
+{
+    if (!f8_product_ok(M, N, K, dtype) || M == 0) return 0;
+    return f8_backward_parts(M, N, K).bytes;
+}
+
+extern "C" int nova_f8_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, int format, const void *Wq, size_t Wq_bytes, void *dx,
+                                       int64_t lddx, const void *x, int64_t ldx, void *dw, int64_t lddw, int dw_dtype, float *dbias, int M, int N, int K,
+                                       int dtype, int flags, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!f8_product_ok(M, N, K, dtype) || (flags & ~NOVA_FLAG_ADD) || !f8_format_ok(format) || (!dx && !dw && !dbias) ||
+        (dw && dw_dtype != NOVA_F32 && dw_dtype != dtype))
+        return NOVA_EINVAL;
+    const F8Operand w = {Wq, make_f8_layout(K, N, 128), NOVA_F8_E4M3};
+    if (dx && (!Wq || !aligned16(Wq))) return NOVA_EINVAL;
+    if (dx && Wq_bytes < w.layout.bytes()) return NOVA_ENOSPC;
+    if (dw && !write_rows_ok(dw, lddw, N, K)) return NOVA_EINVAL;
+    if (M == 0) {
+        // a sum over no rows
+        if (flags & NOVA_FLAG_ADD) return NOVA_OK;
+        if (dw)
+            if (int err = launch_f8_zero(dw, lddw, N, K, dw_dtype, stream)) return hip_result(err);
+        return dbias ? hip_result(launch_f8_zero(dbias, N, 1, N, NOVA_F32, stream)) : NOVA_OK;
+    }
+    if (!read_rows_ok(dy, lddy, M, N) || (y && !read_rows_ok(y, ldy, M, N)) || (dx && !write_rows_ok(dx, lddx, M, K)) || (dw && !read_rows_ok(x, ldx, M, K)) ||
+        !workspace || !aligned16(workspace))
+        return NOVA_EINVAL;
+    const F8BackwardParts p = f8_backward_parts(M, N, K);
+    if (workspace_bytes < p.bytes) return NOVA_ENOSPC;
+    char *const ws = (char *)workspace;
+    const F8Source d = {dy, lddy, y, ldy, M, N, dtype};
+    if (int err = launch_f8_quantize_both(d, format, dx ? ws + p.d_at : nullptr, dw ? ws + p.d_transposed_at : nullptr, dbias, (float *)(ws + p.sums_at),
+                                          (flags & NOVA_FLAG_ADD) != 0, stream))
+        return hip_result(err);
+    if (dx) {
+        const F8Operand a = {ws + p.d_at, p.d, format};
+        if (int err = launch_f8_matmul(a, w, nullptr, dx, lddx, dtype, 0, ws + p.products_at, stream)) return hip_result(err);
+    }
+    if (dw) {
+        const F8Source xs = {x, ldx, nullptr, 0, M, K, dtype};
+        if (int err = launch_f8_quantize(xs, p.x_transposed, NOVA_F8_E4M3, 1, ws + p.x_at, stream)) return hip_result(err);
+        const F8Operand a = {ws + p.d_transposed_at, p.d_transposed, format}, b = {ws + p.x_at, p.x_transposed, NOVA_F8_E4M3};
+        if (int err = launch_f8_matmul(a, b, nullptr, dw, lddw, dw_dtype, flags & NOVA_FLAG_ADD, ws + p.products_at, stream)) return hip_result(err);
+    }
+    return NOVA_OK;
+}
+
+// ---- dropout ----
+
+static bool dropout_ok(int rows, int columns, int dtype, double p)
+{
+    return rows >= 0 && columns >= 0 && any_dtype_ok(dtype) && p >= 0.0 && p <= 1.0;
+}
+
+static int dropout(DropoutArgs a, int dtype, double p, void *stream)
+{
+    a.threshold = (uint64_t)(p * 4294967296.0 + 0.5);
+    a.factor = a.threshold < ((uint64_t)1 << 32) ? (float)(1.0 / (1.0 - p)) : 0.0f;
+    return hip_result(launch_dropout(a, dtype, stream));
+}
+
+extern "C" int nova_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldresidual, void *y, int64_t ldy, int rows, int columns, int dtype, double p,
+                            uint64_t seed, uint64_t offset, const uint64_t *device_offset, int flags, void *stream)
+{
+    if (!dropout_ok(rows, columns, dtype, p) || (flags & ~NOVA_FLAG_RELU)) return NOVA_EINVAL;
+    if (rows == 0 || columns == 0) return NOVA_OK;
+    if (!read_rows_ok(x, ldx, rows, columns) || (residual && !read_rows_ok(residual, ldresidual, rows, columns)) || !write_rows_ok(y, ldy, rows, columns))
+        return NOVA_EINVAL;
+    return dropout({x, ldx, residual, ldresidual, nullptr, 0, y, ldy, rows, columns, (flags & NOVA_FLAG_RELU) != 0, 0, seed, offset, device_offset, 0.0f}, dtype, p,
+                   stream);
+}
+
+extern "C" int nova_dropout_backward(const void *dy, int64_t lddy, const void *gate, int64_t ldgate, void *dx, int64_t lddx, int rows, int columns, int dtype,
+                                     double p, uint64_t seed, uint64_t offset, const uint64_t *device_offset, void *stream)
+{
+    if (!dropout_ok(rows, columns, dtype, p)) return NOVA_EINVAL;
+    if (rows == 0 || columns == 0) return NOVA_OK;
+    if (!read_rows_ok(dy, lddy, rows, columns) || (gate && !read_rows_ok(gate, ldgate, rows, columns)) || !write_rows_ok(dx, lddx, rows, columns))
+        return NOVA_EINVAL;
+    return dropout({dy, lddy, nullptr, 0, gate, ldgate, dx, lddx, rows, columns, 0, 0, seed, offset, device_offset, 0.0f}, dtype, p, stream);
+}
+
 extern "C" const char *nova_strerror(int code)
 {
     switch (code) {

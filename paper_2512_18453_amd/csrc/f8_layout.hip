@@ -1,0 +1,295 @@
+// Matrices in 8-bit floating point: from rows of numbers to the layout that the products read (nova_f8_quantize in nova.h), from codes, and back.
+//
+// A workgroup takes 128 x 128 elements of the source, a thread 8 x 8 of them, and holds them in registers: what is largest in a row, a column or all of them
+// is known before any is divided, and one read serves the layout of the rows, of the columns, and the columns' sums.  Codes go through LDS, where they are put
+// in the panels' order, so that memory sees whole 16-byte pieces side by side.
+#include "f8_common.hpp"
+
+namespace nova {
+
+constexpr int kTile = 128;
+
+struct F8Quantize {
+    F8Source src;
+    char *rows_q, *columns_q;                     // layouts of the source and of its transpose; either may be null
+    float *partial;                               // sums of the columns over 128 rows, or null
+    F8Layout rows_layout, columns_layout;
+    int tiles_across;
+    int64_t tiles;
+};
+
+__device__ __forceinline__ float *f8_scales(char *q, const F8Layout &layout) { return (float *)(q + layout.code_bytes); }
+
+// Largest magnitude as bits (infinity is above every number, NaN above infinity) -> scale; a block that holds one of them has scale NaN
+template <int FORMAT>
+__device__ __forceinline__ float scale_of(unsigned bits)
+{
+    return bits < 0x7f800000u ? __uint_as_float(bits) / kLargestCode<FORMAT> : __builtin_nanf("");
+}
+
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Quotients as nova.h defines them: divided in binary32, kept within the largest code (a scale that is subnormal can be too small by half); 0 for scales of 0 and NaN
+template <int FORMAT>
+__device__ __forceinline__ float quotient(float v, float scale)
+{
+    constexpr float L = kLargestCode<FORMAT>;
+    return scale > 0.0f ? __builtin_amdgcn_fmed3f(v / scale, -L, L) : 0.0f;
+}
+
+// The largest value over the 16 lanes of a row of the wave
+__device__ __forceinline__ unsigned largest_of_16(unsigned v)
+{
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false));      // rotations by 8, 4, 2, 1
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
+    return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
+}
+
+// A tile's codes from LDS to the panels row_tile .. of a chunk
+__device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
+{
+    for (int piece = threadIdx.x; piece < kTile * kTile / 16; piece += 256) {
+        const int r = row_tile + piece / 128;
+        if (r < layout.row_tiles) *(uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16) = staged[piece];
+    }
+}
+
+// BLOCK: 1 or 128, of whichever layouts there are
+template <int DT, int FORMAT, int BLOCK>
+__global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
+{
+    typedef Storage<DT> T;
+    __shared__ uint4v staged[kTile * kTile / 16];
+    __shared__ unsigned largest[4][kTile];
+    __shared__ float sums[4][kTile];
+    const int t = threadIdx.x, j = t % 16, g = t / 16, wave = t / 64;
+    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const int tile_row = (int)(tile / a.tiles_across), tile_column = (int)(tile % a.tiles_across);
+        const int64_t row = (int64_t)tile_row * kTile + 8 * g, column = (int64_t)tile_column * kTile + 8 * j;
+        const int count = (int)min((int64_t)8, max((int64_t)0, a.src.columns - column));
+        float v[8][8];
+        Eight<T> x[8], gate[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int here = row + k < a.src.rows ? count : 0;
+            x[k] = load_eight((const T *)a.src.x + (row + k) * a.src.ld + column, here, here > 0 && column >= 8);
+            if (a.src.gate) gate[k] = load_eight((const T *)a.src.gate + (row + k) * a.src.ldgate + column, here, here > 0 && column >= 8);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = a.src.gate && !((float)gate[k].v[e] > 0.0f) ? 0.0f : (float)x[k].v[e];
+
+        // the largest of each column, and with them of the tile
+        __syncthreads();
+        if (BLOCK > 1 || a.columns_q) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                unsigned m = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) m = max(m, magnitude(v[k][e]));
+                m = max(m, (unsigned)__shfl_xor((int)m, 16));
+                m = max(m, (unsigned)__shfl_xor((int)m, 32));
+                if (t % 64 < 16) largest[wave][8 * j + e] = m;
+            }
+        }
+        if (a.partial) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += v[k][e];
+                s += __shfl_xor(s, 16);
+                s += __shfl_xor(s, 32);
+                if (t % 64 < 16) sums[wave][8 * j + e] = s;
+            }
+        }
+        __syncthreads();
+        if (a.partial && t < kTile && tile_column * (int64_t)kTile + t < a.src.columns)
+            a.partial[(size_t)tile_row * a.src.columns + tile_column * kTile + t] = (sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]);
+        float whole = 0.0f;
+        if constexpr (BLOCK > 1) {
+            unsigned m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) m = max(m, largest[w][8 * j + e]);
+            whole = scale_of<FORMAT>(largest_of_16(m));
+        }
+
+        if (a.rows_q) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float s = whole;
+                if constexpr (BLOCK == 1) {
+                    unsigned m = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[k][e]));
+                    s = scale_of<FORMAT>(largest_of_16(m));
+                    if (j == 0 && row + k < a.rows_layout.scale_pitch)
+                        f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + row + k] = s;
+                }
+                float q[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[e] = quotient<FORMAT>(v[k][e], s);
+                unsigned *at = (unsigned *)staged + (g / 2 * kF8PanelBytes + j / 2 % 2 * 1024 + (j / 4 * 16 + g % 2 * 8 + k) * 16 + j % 2 * 8) / 4;
+                at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
+                at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);
+            }
+            if (BLOCK > 1 && t == 0) f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + tile_row] = whole;
+            __syncthreads();
+            write_panels(staged, a.rows_q, a.rows_layout, tile_row * (kTile / kF8Rows), tile_column);
+            __syncthreads();
+        }
+        if (a.columns_q) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float s = whole;
+                if constexpr (BLOCK == 1) {
+                    const int n = 8 * j + e;
+                    s = scale_of<FORMAT>(max(max(largest[0][n], largest[1][n]), max(largest[2][n], largest[3][n])));
+                    if (g == 0 && column + e < a.columns_layout.scale_pitch)
+                        f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + column + e] = s;
+                }
+                float q[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) q[k] = quotient<FORMAT>(v[k][e], s);
+                unsigned *at = (unsigned *)staged + (j / 2 * kF8PanelBytes + g / 2 % 2 * 1024 + (g / 4 * 16 + j % 2 * 8 + e) * 16 + g % 2 * 8) / 4;
+                at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
+                at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);
+            }
+            if (BLOCK > 1 && t == 0) f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + tile_column] = whole;
+            __syncthreads();
+            write_panels(staged, a.columns_q, a.columns_layout, tile_column * (kTile / kF8Rows), tile_row);
+        }
+    }
+}
+
+// out (+)= the pieces' sums, in their order
+__global__ void __launch_bounds__(256) f8_sums_kernel(const float *__restrict__ partial, float *__restrict__ out, int pieces, int columns, int add)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= columns) return;
+    double s = add ? out[n] : 0.0;
+    for (int p = 0; p < pieces; ++p) s += partial[(size_t)p * columns + n];
+    out[n] = (float)s;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) f8_zero_kernel(T *__restrict__ out, int64_t ld, int rows, int columns)
+{
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < (int64_t)rows * columns; i += (int64_t)gridDim.x * 256) out[i / columns * ld + i % columns] = (T)0;
+}
+
+// A thread per 16-byte piece of the layout, and per scale
+__global__ void __launch_bounds__(256) f8_pack_kernel(const uint8_t *__restrict__ codes, const float *__restrict__ scales, char *__restrict__ q, const F8Layout layout,
+                                                      int transposed)
+{
+    const size_t stride = (size_t)gridDim.x * 256, first = (size_t)blockIdx.x * 256 + threadIdx.x;
+    for (size_t idx = first; idx < layout.code_bytes / 16; idx += stride) {
+        const int piece = idx % 128, lane = piece % 64;
+        const size_t panel = idx / 128;
+        const int64_t row = (int64_t)(panel / layout.chunks) * kF8Rows + lane % 16;
+        const int64_t column = (int64_t)(panel % layout.chunks) * kF8Chunk + lane / 16 * 32 + piece / 64 * 16;
+        uint8_t v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool real = row < layout.rows && column + i < layout.columns;
+            v[i] = real ? codes[transposed ? (column + i) * layout.rows + row : row * layout.columns + column + i] : (uint8_t)0;
+        }
+        __builtin_memcpy(q + idx * 16, v, 16);
+    }
+    const int bands = (int)(((int64_t)layout.rows + layout.block - 1) / layout.block);
+    for (size_t idx = first; idx < layout.scale_count; idx += stride) {
+        const size_t band = idx % layout.scale_pitch, chunk = idx / layout.scale_pitch;
+        f8_scales(q, layout)[idx] = band < (size_t)bands ? scales[transposed ? chunk * bands + band : band * layout.chunks + chunk] : 0.0f;
+    }
+}
+
+__global__ void __launch_bounds__(256) f8_unpack_kernel(const char *__restrict__ q, const F8Layout layout, uint8_t *__restrict__ codes, float *__restrict__ scales)
+{
+    // a workgroup's threads read whole panels, neighbours write neighbouring pieces of a row
+    const size_t stride = (size_t)gridDim.x * 256, first = (size_t)blockIdx.x * 256 + threadIdx.x;
+    for (size_t idx = first; idx < layout.code_bytes / 16; idx += stride) {
+        const int piece = idx % 8, row_in = idx / 8 % 16;
+        const size_t panel = idx / 128;
+        const int64_t row = (int64_t)(panel / layout.chunks) * kF8Rows + row_in, column = (int64_t)(panel % layout.chunks) * kF8Chunk + piece * 16;
+        if (row >= layout.rows || column >= layout.columns) continue;
+        uint8_t v[16];
+        __builtin_memcpy(v, q + panel * kF8PanelBytes + piece % 2 * 1024 + (piece / 2 * 16 + row_in) * 16, 16);
+        uint8_t *to = codes + row * layout.columns + column;
+        if (column + 16 <= layout.columns) {
+            __builtin_memcpy(to, v, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 15; ++i)
+                if (column + i < layout.columns) to[i] = v[i];
+        }
+    }
+    if (!scales) return;
+    const int64_t bands = ((int64_t)layout.rows + layout.block - 1) / layout.block;
+    for (size_t idx = first; idx < (size_t)bands * layout.chunks; idx += stride)
+        scales[idx] = ((const float *)(q + layout.code_bytes))[idx % layout.chunks * layout.scale_pitch + idx / layout.chunks];
+}
+
+static unsigned blocks_for(size_t threads) { return (unsigned)(threads > ((size_t)1 << 30) ? (1 << 22) : (threads + 255) / 256); }
+
+template <int DT, int FORMAT>
+static void run_quantize(const F8Quantize &a, int block, hipStream_t s)
+{
+    const unsigned blocks = (unsigned)(a.tiles < (1 << 22) ? a.tiles : 1 << 22);
+    if (block == 1) f8_quantize_kernel<DT, FORMAT, 1><<<blocks, 256, 0, s>>>(a);
+    else f8_quantize_kernel<DT, FORMAT, 128><<<blocks, 256, 0, s>>>(a);
+}
+
+static int quantize(F8Quantize a, int format, int block, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    a.tiles_across = (int)(((int64_t)a.src.columns + kTile - 1) / kTile);
+    a.tiles = (int64_t)a.tiles_across * (((int64_t)a.src.rows + kTile - 1) / kTile);
+    const bool e4m3 = format == NOVA_F8_E4M3;
+    if (a.src.dtype == NOVA_F32) e4m3 ? run_quantize<NOVA_F32, NOVA_F8_E4M3>(a, block, s) : run_quantize<NOVA_F32, NOVA_F8_E5M2>(a, block, s);
+    else if (a.src.dtype == NOVA_F16) e4m3 ? run_quantize<NOVA_F16, NOVA_F8_E4M3>(a, block, s) : run_quantize<NOVA_F16, NOVA_F8_E5M2>(a, block, s);
+    else e4m3 ? run_quantize<NOVA_BF16, NOVA_F8_E4M3>(a, block, s) : run_quantize<NOVA_BF16, NOVA_F8_E5M2>(a, block, s);
+    return (int)hipGetLastError();
+}
+
+int launch_f8_quantize(const F8Source &x, const F8Layout &q, int format, int transposed, void *Xq, void *stream)
+{
+    F8Quantize a = {x, nullptr, nullptr, nullptr, q, q, 0, 0};
+    (transposed ? a.columns_q : a.rows_q) = (char *)Xq;
+    return quantize(a, format, q.block, stream);
+}
+
+int launch_f8_quantize_both(const F8Source &x, int format, void *Xq, void *Xq_transposed, float *sums, float *partial, int add, void *stream)
+{
+    const F8Quantize a = {x, (char *)Xq, (char *)Xq_transposed, sums ? partial : nullptr, make_f8_layout(x.rows, x.columns, 1), make_f8_layout(x.columns, x.rows, 1),
+                          0, 0};
+    if (int err = quantize(a, format, 1, stream)) return err;
+    if (!sums) return 0;
+    f8_sums_kernel<<<(x.columns + 255) / 256, 256, 0, (hipStream_t)stream>>>(partial, sums, a.columns_layout.chunks, x.columns, add);
+    return (int)hipGetLastError();
+}
+
+int launch_f8_pack(const uint8_t *codes, const float *scales, const F8Layout &q, int transposed, void *Xq, void *stream)
+{
+    f8_pack_kernel<<<blocks_for(q.code_bytes / 16), 256, 0, (hipStream_t)stream>>>(codes, scales, (char *)Xq, q, transposed);
+    return (int)hipGetLastError();
+}
+
+int launch_f8_unpack(const void *Xq, const F8Layout &q, uint8_t *codes, float *scales, void *stream)
+{
+    f8_unpack_kernel<<<blocks_for(q.code_bytes / 16), 256, 0, (hipStream_t)stream>>>((const char *)Xq, q, codes, scales);
+    return (int)hipGetLastError();
+}
+
+int launch_f8_zero(void *out, int64_t ld, int rows, int columns, int dtype, void *stream)
+{
+    const unsigned blocks = blocks_for((size_t)rows * columns);
+    if (dtype == NOVA_F32) f8_zero_kernel<<<blocks, 256, 0, (hipStream_t)stream>>>((unsigned *)out, ld, rows, columns);
+    else f8_zero_kernel<<<blocks, 256, 0, (hipStream_t)stream>>>((unsigned short *)out, ld, rows, columns);
+    return (int)hipGetLastError();
+}
+
+}  // namespace nova

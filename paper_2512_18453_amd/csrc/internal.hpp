@@ -102,6 +102,28 @@ inline Q4Layout make_q4_layout(int N, int K, int group, int direction)
     return q;
 }
 
+// A matrix in 8-bit floating point as it is laid out for a product that sums along its rows (nova_f8_pack in nova.h): panels of codes, then scales.
+constexpr int kF8Rows = 16, kF8Chunk = 128, kF8PanelBytes = 2048;
+struct F8Layout {
+    int rows, columns, block;                  // block: rows that share the scale of a chunk (1 or 128)
+    int row_tiles, chunks;                     // panels
+    int scale_pitch;                           // scales of a chunk: rows padded to whole panels, or bands of 128
+    size_t code_bytes, scale_count;
+    size_t bytes() const { return code_bytes + scale_count * 4; }
+};
+
+inline F8Layout make_f8_layout(int rows, int columns, int block)
+{
+    F8Layout q;
+    q.rows = rows; q.columns = columns; q.block = block;
+    q.row_tiles = rows / kF8Rows + (rows % kF8Rows != 0);
+    q.chunks = columns / kF8Chunk + (columns % kF8Chunk != 0);
+    q.scale_pitch = block == 1 ? q.row_tiles * kF8Rows : rows / block + (rows % block != 0);
+    q.code_bytes = (size_t)q.row_tiles * q.chunks * kF8PanelBytes;
+    q.scale_count = (size_t)q.chunks * q.scale_pitch;
+    return q;
+}
+
 }  // namespace nova
 
 struct nova_transforms {
@@ -208,6 +230,26 @@ struct LogprobsBackwardArgs {
     const uint8_t *mask; int64_t mask_stride; int rows, V; float scale; void *dlogits; int64_t dstride;
 };
 int launch_logprobs_backward(const LogprobsBackwardArgs &a, int dtype, void *stream);
+// Matrices in 8-bit floating point (F8Layout): quantise, lay out codes, read back; products
+struct F8Source {
+    const void *x; int64_t ld; const void *gate; int64_t ldgate;   // gate: elements count where it is > 0
+    int rows, columns, dtype;
+};
+int launch_f8_quantize(const F8Source &x, const F8Layout &q, int format, int transposed, void *Xq, void *stream);
+int launch_f8_quantize_both(const F8Source &x, int format, void *Xq, void *Xq_transposed, float *sums, float *partial, int add, void *stream);
+int launch_f8_pack(const uint8_t *codes, const float *scales, const F8Layout &q, int transposed, void *Xq, void *stream);
+int launch_f8_unpack(const void *Xq, const F8Layout &q, uint8_t *codes, float *scales, void *stream);
+int launch_f8_zero(void *out, int64_t ld, int rows, int columns, int dtype, void *stream);
+struct F8Operand { const void *q; F8Layout layout; int format; };
+size_t f8_matmul_workspace(int M, int N, int K);
+int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream);
+// Dropout: the forward call and its gradient
+struct DropoutArgs {
+    const void *x; int64_t ldx; const void *residual; int64_t ldresidual; const void *gate; int64_t ldgate; void *y; int64_t ldy;
+    int rows, columns, relu;
+    uint64_t threshold, seed, offset; const uint64_t *device_offset; float factor;
+};
+int launch_dropout(const DropoutArgs &a, int dtype, void *stream);
 int launch_relu_maxpool2x2(const void *in, void *out, int N, int C, int H, int W, int dtype,
                            void *stream);
 }  // namespace nova

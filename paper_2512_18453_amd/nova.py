@@ -16,9 +16,10 @@ NOVA_F32, NOVA_F16, NOVA_BF16 = 0, 1, 2
 NOVA_MATRIX_A, NOVA_MATRIX_BT, NOVA_MATRIX_G = 0, 1, 2
 NOVA_ROWS_PLAIN, NOVA_ROWS_BALANCED, NOVA_ROWS_GIVEN = 0, 1, 2
 NOVA_MATRIX_F32, NOVA_MATRIX_F16, NOVA_MATRIX_INT8 = 0, 1, 2
-NOVA_FLAG_RELU, NOVA_FLAG_M_F16, NOVA_FLAG_POOL2 = 1, 2, 4
+NOVA_FLAG_RELU, NOVA_FLAG_M_F16, NOVA_FLAG_POOL2, NOVA_FLAG_ADD = 1, 2, 4, 8
 NOVA_INT8_PER_TENSOR, NOVA_INT8_PER_CHANNEL, NOVA_INT8_PER_POSITION = 0, 1, 2
 NOVA_Q4_FORWARD, NOVA_Q4_BACKWARD = 0, 1
+NOVA_F8_E4M3, NOVA_F8_E5M2 = 0, 1
 NOVA_PATH_STAGES, NOVA_PATH_FEW_CHANNELS, NOVA_PATH_FUSED_OUTPUT = 0, 1, 2
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libnova.so")
@@ -35,6 +36,9 @@ EXPORTS = [
     "nova_input_transform", "nova_contract", "nova_output_transform", "nova_relu_maxpool2x2",
     "nova_q4_bytes", "nova_q4_quantize", "nova_q4_pack", "nova_q4_unpack", "nova_q4_linear_workspace_bytes", "nova_q4_linear", "nova_q4_linear_backward",
     "nova_logprobs_workspace_bytes", "nova_logprobs", "nova_logprobs_backward",
+    "nova_f8_bytes", "nova_f8_quantize", "nova_f8_pack", "nova_f8_unpack", "nova_f8_matmul_workspace_bytes", "nova_f8_matmul",
+    "nova_f8_linear_workspace_bytes", "nova_f8_linear", "nova_f8_linear_backward_workspace_bytes", "nova_f8_linear_backward",
+    "nova_dropout", "nova_dropout_backward",
     "nova_strerror", "nova_last_hip_error", "nova_version",
 ]
 
@@ -123,6 +127,23 @@ def lib():
         L.nova_logprobs_workspace_bytes.restype = sz
         L.nova_logprobs.argtypes = [vp, i64, vp, vp, i64, i, i, f, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
         L.nova_logprobs_backward.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i, i, f, i, vp, i64, vp]
+        L.nova_f8_bytes.argtypes = [i] * 3
+        L.nova_f8_bytes.restype = sz
+        L.nova_f8_quantize.argtypes = [vp, i64, i, i, i, i, i, i, vp, sz, vp]
+        L.nova_f8_pack.argtypes = [vp, vp, i, i, i, i, vp, sz, vp]
+        L.nova_f8_unpack.argtypes = [vp, sz, i, i, i, vp, vp, vp]
+        L.nova_f8_matmul_workspace_bytes.argtypes = [i] * 6
+        L.nova_f8_matmul_workspace_bytes.restype = sz
+        L.nova_f8_matmul.argtypes = [vp, sz, i, i, vp, sz, i, i, vp, vp, i64, i, i, i, i, i, vp, sz, vp]
+        L.nova_f8_linear_workspace_bytes.argtypes = [i] * 4
+        L.nova_f8_linear_workspace_bytes.restype = sz
+        L.nova_f8_linear.argtypes = [vp, i64, vp, sz, vp, vp, i64, i, i, i, i, i, vp, sz, vp]
+        L.nova_f8_linear_backward_workspace_bytes.argtypes = [i] * 4
+        L.nova_f8_linear_backward_workspace_bytes.restype = sz
+        L.nova_f8_linear_backward.argtypes = [vp, i64, vp, i64, i, vp, sz, vp, i64, vp, i64, vp, i64, i, vp, i, i, i, i, i, vp, sz, vp]
+        u64, d = ctypes.c_uint64, ctypes.c_double
+        L.nova_dropout.argtypes = [vp, i64, vp, i64, vp, i64, i, i, i, d, u64, u64, vp, i, vp]
+        L.nova_dropout_backward.argtypes = [vp, i64, vp, i64, vp, i64, i, i, i, d, u64, u64, vp, vp]
         L.nova_strerror.argtypes = [i]
         L.nova_strerror.restype = ctypes.c_char_p
         L.nova_last_hip_error.restype = i
@@ -601,6 +622,166 @@ def nova_logprobs_backward(logits, stats, targets=None, g_logprob=None, entropy=
                                         row_values(entropy, "entropy"), row_values(g_entropy, "g_entropy"), *_mask(mask, R, V), R, V, scale, dt,
                                         *_rows(dlogits, (R, V), logits.dtype, "dlogits"), _stream()), "nova_logprobs_backward")
     return dlogits
+
+
+# ---- layers in 8-bit floating point, dropout ----
+
+_F8_DTYPE = {NOVA_F8_E4M3: torch.float8_e4m3fn, NOVA_F8_E5M2: torch.float8_e5m2}
+
+
+def _f8_dtype(format):
+    if format not in _F8_DTYPE:
+        raise ValueError(f"unsupported format {format}")
+    return _F8_DTYPE[format]
+
+
+def _here(*tensors):
+    """The library works on the current device."""
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != at:
+            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{at}")
+
+
+def _workspace(workspace, need, device):
+    return torch.empty(need, dtype=torch.uint8, device=device) if workspace is None else workspace
+
+
+def nova_f8_bytes(rows, columns, block):
+    return lib().nova_f8_bytes(rows, columns, block)
+
+
+def nova_f8_quantize(x, block, format=NOVA_F8_E4M3, transposed=False, Xq=None):
+    """x [rows,columns] -> the 8-bit layout of x (of x^T with transposed), flat uint8, with a scale per `block` (1 or 128) x 128."""
+    (R, C), dt = x.shape, _any_dtype_code(x.dtype)
+    _here(x, Xq)
+    if Xq is None:
+        Xq = torch.empty(lib().nova_f8_bytes(*((C, R) if transposed else (R, C)), block), dtype=torch.uint8, device=x.device)
+    _check(lib().nova_f8_quantize(*_rows(x, (R, C), x.dtype, "x"), R, C, dt, format, block, int(transposed), *_bytes(Xq, "Xq"), _stream()), "nova_f8_quantize")
+    return Xq
+
+
+def nova_f8_pack(codes, scales, block, transposed=False, Xq=None):
+    """codes [rows,columns] (float8_e4m3fn, float8_e5m2 or their bytes), scales float32 [ceil(rows / block), ceil(columns / 128)] -> the 8-bit layout of the
+    matrix (of its transpose with transposed, block 128), flat uint8."""
+    R, C = codes.shape
+    if codes.dtype not in (torch.uint8, *_F8_DTYPE.values()):
+        raise TypeError(f"codes: unsupported dtype {codes.dtype}")
+    _here(codes, scales, Xq)
+    if Xq is None:
+        Xq = torch.empty(lib().nova_f8_bytes(*((C, R) if transposed else (R, C)), block), dtype=torch.uint8, device=codes.device)
+    _check(lib().nova_f8_pack(_flat(codes, R * C, codes.dtype, "codes"), _flat(scales, -(-R // max(block, 1)) * -(-C // 128), torch.float32, "scales"), R, C, block,
+                              int(transposed), *_bytes(Xq, "Xq"), _stream()), "nova_f8_pack")
+    return Xq
+
+
+def nova_f8_unpack(Xq, rows, columns, block, format=NOVA_F8_E4M3):
+    """(codes float8 [rows,columns], scales float32 [ceil(rows / block), ceil(columns / 128)]) of a layout."""
+    _here(Xq)
+    codes = torch.empty((rows, columns), dtype=_f8_dtype(format), device=Xq.device)
+    scales = torch.empty((-(-rows // max(block, 1)), -(-columns // 128)), dtype=torch.float32, device=Xq.device)
+    _check(lib().nova_f8_unpack(*_bytes(Xq, "Xq"), rows, columns, block, codes.data_ptr(), scales.data_ptr(), _stream()), "nova_f8_unpack")
+    return codes, scales
+
+
+def nova_f8_matmul_workspace_bytes(M, N, K, block_a, block_b, dtype):
+    return lib().nova_f8_matmul_workspace_bytes(M, N, K, block_a, block_b, _any_dtype_code(dtype))
+
+
+def nova_f8_matmul(Aq, Bq, M, N, K, block_a=1, block_b=128, format_a=NOVA_F8_E4M3, format_b=NOVA_F8_E4M3, bias=None, out=None, dtype=torch.bfloat16, flags=0,
+                   workspace=None):
+    """Layouts Aq [M,K] and Bq [N,K] -> A B^T + bias [M,N] of dtype (out's, if it is given)."""
+    _here(Aq, Bq, bias, out, workspace)
+    if out is None:
+        if flags & NOVA_FLAG_ADD:
+            raise ValueError("NOVA_FLAG_ADD needs out")
+        out = torch.empty((M, N), dtype=dtype, device=Aq.device)
+    dt = _any_dtype_code(out.dtype)
+    workspace = _workspace(workspace, lib().nova_f8_matmul_workspace_bytes(M, N, K, block_a, block_b, dt), Aq.device)
+    _check(lib().nova_f8_matmul(*_bytes(Aq, "Aq"), block_a, format_a, *_bytes(Bq, "Bq"), block_b, format_b,
+                                None if bias is None else _flat(bias, N, out.dtype, "bias"), *_rows(out, (M, N), out.dtype, "out"), M, N, K, dt, flags,
+                                *_bytes(workspace, "workspace"), _stream()), "nova_f8_matmul")
+    return out
+
+
+def nova_f8_linear_workspace_bytes(M, N, K, dtype):
+    return lib().nova_f8_linear_workspace_bytes(M, N, K, _any_dtype_code(dtype))
+
+
+def nova_f8_linear(x, Wq, N, bias=None, y=None, flags=0, workspace=None):
+    """x [M,K] -> y [M,N] through the weights' layout Wq ([N,K], E4M3, block 128)."""
+    (M, K), dt = x.shape, _any_dtype_code(x.dtype)
+    _here(x, Wq, bias, y, workspace)
+    if y is None:
+        y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    workspace = _workspace(workspace, lib().nova_f8_linear_workspace_bytes(M, N, K, dt), x.device)
+    _check(lib().nova_f8_linear(*_rows(x, (M, K), x.dtype, "x"), *_bytes(Wq, "Wq"), None if bias is None else _flat(bias, N, x.dtype, "bias"),
+                                *_rows(y, (M, N), x.dtype, "y"), M, N, K, dt, flags, *_bytes(workspace, "workspace"), _stream()), "nova_f8_linear")
+    return y
+
+
+def nova_f8_linear_backward_workspace_bytes(M, N, K, dtype):
+    return lib().nova_f8_linear_backward_workspace_bytes(M, N, K, _any_dtype_code(dtype))
+
+
+def nova_f8_linear_backward(dy, Wq, x, y=None, format=NOVA_F8_E5M2, dx=None, dw=None, dbias=None, flags=0, need_dbias=True, K=None, dw_dtype=torch.float32, workspace=None):
+    """dy [M,N] -> (dx [M,K], dw [N,K] of dw_dtype (dw's, if it is given; float32 or dy's dtype), dbias float32 [N]) of a layer with input x [M,K] and the transposed weights' layout Wq ([K,N], E4M3, block 128).  Wq
+    None: no dx; x None (K must then be given): no dw; need_dbias False and no dbias: no dbias.  y: the layer's result if a ReLU made it.  With
+    NOVA_FLAG_ADD dw and dbias are added to (and must be given)."""
+    (M, N), dt = dy.shape, _any_dtype_code(dy.dtype)
+    if x is not None:
+        K = x.shape[1]
+    if K is None:
+        raise ValueError("K: needed where x is not given")
+    _here(dy, Wq, x, y, dx, dw, dbias, workspace)
+    need_dbias = need_dbias or dbias is not None
+    if flags & NOVA_FLAG_ADD and ((x is not None and dw is None) or (need_dbias and dbias is None)):
+        raise ValueError("NOVA_FLAG_ADD needs dw and dbias")
+    if (Wq is None and dx is not None) or (x is None and dw is not None):
+        raise ValueError("dx needs Wq, dw needs x")
+    if dx is None and Wq is not None:
+        dx = torch.empty((M, K), dtype=dy.dtype, device=dy.device)
+    if dw is None and x is not None:
+        dw = torch.empty((N, K), dtype=dw_dtype, device=dy.device)
+    if dbias is None and need_dbias:
+        dbias = torch.empty((N,), dtype=torch.float32, device=dy.device)
+    workspace = _workspace(workspace, lib().nova_f8_linear_backward_workspace_bytes(M, N, K, dt), dy.device)
+
+    def rows_or_none(t, shape, dtype, what):
+        return (None, 0) if t is None else _rows(t, shape, dtype, what)
+    _check(lib().nova_f8_linear_backward(*_rows(dy, (M, N), dy.dtype, "dy"), *rows_or_none(y, (M, N), dy.dtype, "y"), format,
+                                         *((None, 0) if Wq is None else _bytes(Wq, "Wq")), *rows_or_none(dx, (M, K), dy.dtype, "dx"),
+                                         *rows_or_none(x, (M, K), dy.dtype, "x"), *((None, 0, dt) if dw is None else (*_rows(dw, (N, K), dw.dtype, "dw"), _any_dtype_code(dw.dtype))),
+                                         None if dbias is None else _flat(dbias, N, torch.float32, "dbias"), M, N, K, dt, flags,
+                                         *_bytes(workspace, "workspace"), _stream()), "nova_f8_linear_backward")
+    return dx, dw, dbias
+
+
+def _draw(seed, offset, device_offset):
+    """The arguments that choose a mask: numbers modulo 2^64, and one on the device."""
+    return seed % 2 ** 64, offset % 2 ** 64, None if device_offset is None else _flat(device_offset, 1, torch.int64, "device_offset")
+
+
+def nova_dropout(x, p, seed, offset=0, device_offset=None, residual=None, flags=0, y=None):
+    """x [rows,columns] -> dropout of x (of its ReLU with NOVA_FLAG_RELU) plus residual; device_offset: int64 [1] on the device, added to offset when the kernel runs."""
+    (R, C), dt = x.shape, _any_dtype_code(x.dtype)
+    _here(x, device_offset, residual, y)
+    if y is None:
+        y = torch.empty((R, C), dtype=x.dtype, device=x.device)
+    _check(lib().nova_dropout(*_rows(x, (R, C), x.dtype, "x"), *((None, 0) if residual is None else _rows(residual, (R, C), x.dtype, "residual")),
+                              *_rows(y, (R, C), x.dtype, "y"), R, C, dt, p, *_draw(seed, offset, device_offset), flags, _stream()), "nova_dropout")
+    return y
+
+
+def nova_dropout_backward(dy, p, seed, offset=0, device_offset=None, gate=None, dx=None):
+    """dy [rows,columns] -> the gradient of nova_dropout's x; gate: what its ReLU saw (or made, without a residual)."""
+    (R, C), dt = dy.shape, _any_dtype_code(dy.dtype)
+    _here(dy, device_offset, gate, dx)
+    if dx is None:
+        dx = torch.empty((R, C), dtype=dy.dtype, device=dy.device)
+    _check(lib().nova_dropout_backward(*_rows(dy, (R, C), dy.dtype, "dy"), *((None, 0) if gate is None else _rows(gate, (R, C), dy.dtype, "gate")),
+                                       *_rows(dx, (R, C), dy.dtype, "dx"), R, C, dt, p, *_draw(seed, offset, device_offset), _stream()), "nova_dropout_backward")
+    return dx
 
 
 def nova_version():
