@@ -594,7 +594,7 @@ static bool f8_flags_ok(int flags) { return flags == 0 || flags == NOVA_FLAG_REL
 extern "C" size_t nova_f8_matmul_workspace_bytes(int M, int N, int K, int block_a, int block_b, int dtype)
 {
     if (!f8_product_ok(M, N, K, dtype) || !f8_block_ok(block_a) || !f8_block_ok(block_b) || M == 0) return 0;
-    return f8_matmul_workspace(M, N, K);
+    return f8_matmul_workspace(M, N, K, dtype);
 }
 
 extern "C" int nova_f8_matmul(const void *Aq, size_t Aq_bytes, int block_a, int format_a, const void *Bq, size_t Bq_bytes, int block_b, int format_b,
@@ -609,7 +609,7 @@ extern "C" int nova_f8_matmul(const void *Aq, size_t Aq_bytes, int block_a, int 
     if (M == 0) return NOVA_OK;
     if (!Aq || !aligned16(Aq) || !write_rows_ok(out, ldout, M, N)) return NOVA_EINVAL;
     const F8Operand a = {Aq, make_f8_layout(M, K, block_a), format_a};
-    const size_t need = f8_matmul_workspace(M, N, K);
+    const size_t need = f8_matmul_workspace(M, N, K, dtype);
     if (need && (!workspace || !aligned16(workspace))) return NOVA_EINVAL;
     if (Aq_bytes < a.layout.bytes() || workspace_bytes < need) return NOVA_ENOSPC;
     return hip_result(launch_f8_matmul(a, b, bias, out, ldout, dtype, flags, workspace, stream));
@@ -618,7 +618,7 @@ extern "C" int nova_f8_matmul(const void *Aq, size_t Aq_bytes, int block_a, int 
 extern "C" size_t nova_f8_linear_workspace_bytes(int M, int N, int K, int dtype)
 {
     if (!f8_product_ok(M, N, K, dtype) || M == 0) return 0;
-    return padded(make_f8_layout(M, K, 1)) + f8_matmul_workspace(M, N, K);
+    return padded(make_f8_layout(M, K, 1)) + f8_matmul_workspace(M, N, K, dtype);
 }
 
 extern "C" int nova_f8_linear(const void *x, int64_t ldx, const void *Wq, size_t Wq_bytes, const void *bias, void *y, int64_t ldy, int M, int N, int K,
@@ -641,7 +641,7 @@ struct F8BackwardParts {
     F8Layout d, d_transposed, x_transposed;
     size_t d_at, d_transposed_at, x_at, sums_at, products_at, bytes;
 };
-static F8BackwardParts f8_backward_parts(int M, int N, int K)
+static F8BackwardParts f8_backward_parts(int M, int N, int K, int dtype)
 {
     F8BackwardParts p;
     p.d = make_f8_layout(M, N, 1);
@@ -652,15 +652,16 @@ static F8BackwardParts f8_backward_parts(int M, int N, int K)
     p.x_at = p.d_transposed_at + padded(p.d_transposed);
     p.sums_at = p.x_at + padded(p.x_transposed);
     p.products_at = p.sums_at + align256((size_t)p.d_transposed.chunks * N * 4);
-    const size_t dx = f8_matmul_workspace(M, K, N), dw = f8_matmul_workspace(N, K, M);
-    p.bytes = p.products_at + (dx > dw ? dx : dw);
+    const size_t dx = f8_matmul_workspace(M, K, N, dtype), dw = f8_matmul_workspace(N, K, M, dtype), dw_full = f8_matmul_workspace(N, K, M, NOVA_F32);
+    const size_t most = dw > dw_full ? dw : dw_full;
+    p.bytes = p.products_at + (dx > most ? dx : most);
     return p;
 }
 
 extern "C" size_t nova_f8_linear_backward_workspace_bytes(int M, int N, int K, int dtype)
 {
     if (!f8_product_ok(M, N, K, dtype) || M == 0) return 0;
-    return f8_backward_parts(M, N, K).bytes;
+    return f8_backward_parts(M, N, K, dtype).bytes;
 }
 
 extern "C" int nova_f8_linear_backward(const void *dy, int64_t lddy, const void *y, int64_t ldy, int format, const void *Wq, size_t Wq_bytes, void *dx,
@@ -684,7 +685,7 @@ extern "C" int nova_f8_linear_backward(const void *dy, int64_t lddy, const void 
     if (!read_rows_ok(dy, lddy, M, N) || (y && !read_rows_ok(y, ldy, M, N)) || (dx && !write_rows_ok(dx, lddx, M, K)) || (dw && !read_rows_ok(x, ldx, M, K)) ||
         !workspace || !aligned16(workspace))
         return NOVA_EINVAL;
-    const F8BackwardParts p = f8_backward_parts(M, N, K);
+    const F8BackwardParts p = f8_backward_parts(M, N, K, dtype);
     if (workspace_bytes < p.bytes) return NOVA_ENOSPC;
     char *const ws = (char *)workspace;
     const F8Source d = {dy, lddy, y, ldy, M, N, dtype};

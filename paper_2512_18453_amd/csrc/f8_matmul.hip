@@ -59,6 +59,25 @@ __device__ __forceinline__ void write_result(const F8Call &a, int64_t m, int n, 
     else write_four<bf16>(a, m, n, sum);
 }
 
+// Rows 16 m_tile + i, columns 16 n_tile + 4 b ..: to the result, or to the pieces of a cut sum
+__device__ __forceinline__ void put(const F8Call &a, int split, int m_tile, int n_tile, int i, int b, float4v sum)
+{
+    const int64_t m = (int64_t)m_tile * 16 + i;
+    const int n = n_tile * 16 + 4 * b;
+    if (a.splits == 1) {
+        write_result(a, m, n, sum);
+    } else if (m < a.M) {
+        float *to = a.partial + ((size_t)split * a.M + m) * a.N + n;
+        if (n + 4 <= a.N) {
+            __builtin_memcpy(to, &sum, sizeof sum);
+        } else {
+#pragma unroll
+            for (int v = 0; v < 3; ++v)
+                if (n + v < a.N) to[v] = sum[v];
+        }
+    }
+}
+
 // A wave makes 16 MT x 16 NT results from operands that it loads itself
 template <int MT, int NT, int FA, int FB, int WAY>
 __global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
@@ -105,17 +124,108 @@ __global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
 #pragma unroll
     for (int x = 0; x < MT; ++x)
 #pragma unroll
-        for (int y = 0; y < NT; ++y) {
-            const int64_t m = (int64_t)(m_tile + x) * 16 + i;
-            const int n = (n_tile + y) * 16 + 4 * b;
-            if (a.splits == 1) {
-                write_result(a, m, n, sum[x][y]);
-            } else if (m < a.M) {
+        for (int y = 0; y < NT; ++y) put(a, split, m_tile + x, n_tile + y, i, b, sum[x][y]);
+}
+
+// ---- tiles ----
+//
+// A workgroup of WM x WN waves makes 16 WM MT rows by 16 WN NT columns.  A stage is a chunk of both operands' panels with their scales; stages come straight from global
+// memory to LDS, one ahead of the one that is multiplied, and a panel lies there as it lies in memory: the 64 lanes of a wave read 1024 bytes side by side.
+template <int WM_, int WN_, int MT_, int NT_>
+struct F8Tile {
+    static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, WAVES = WM * WN, THREADS = WAVES * 64, A = WM * MT, B = WN * NT;        // panels
+    static constexpr int PANELS = (A + B) * kF8PanelBytes, STAGE = PANELS + (A + B) * kF8Rows * 4, LDS = 2 * STAGE;
+    static_assert(A % 4 == 0 && A + B == 4 * WAVES, "a wave loads four panels of one operand, and 64 scales");
+};
+
+// 64 words of 4 bytes, as global_to_lds16 takes 16
+__device__ __forceinline__ void global_to_lds4(const void *uniform_base, unsigned byte_offset, unsigned lds_wave_base)
+{
+    unsigned saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0) : "s"(lds_wave_base), "v"(byte_offset), "s"(uniform_base) : "memory");
+}
+
+// BAND: one scale of B for the 16 NT columns of a wave
+template <typename Shape, int FA, int FB, int WAY, bool BAND>
+__global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call a)
+{
+    constexpr int MT = Shape::MT, NT = Shape::NT, STAGE = Shape::STAGE;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), i = lane % 16, b = lane / 16;
+    const int wm = wave / Shape::WN, wn = wave % Shape::WN;
+    // eight tiles of rows go along the columns together: what an XCD works on at a time is a patch of tiles
+    const unsigned across = (a.b_tiles + Shape::B - 1) / Shape::B, down = (a.a_tiles + Shape::A - 1) / Shape::A, tiles = across * down;
+    const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x), split = id / tiles, tile = id % tiles;
+    const unsigned first_row = tile / (8 * across) * 8, rows = min(8u, down - first_row), in_group = tile % (8 * across);
+    const int m_tile = (int)(first_row + in_group % rows) * Shape::A, n_tile = (int)(in_group / rows) * Shape::B;
+    const int first = split * a.split_chunks, count = min(a.chunks - first, a.split_chunks);
+
+    // what this wave loads: panels 4 wave .. of A's and then B's, the scales of 64 rows
+    const bool of_a = 4 * wave < Shape::A;
+    const int panel0 = of_a ? m_tile + 4 * wave : n_tile + 4 * wave - Shape::A, last = (of_a ? a.a_tiles : a.b_tiles) - 1;
+    const char *panel[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (n + v < a.N) a.partial[((size_t)split * a.M + m) * a.N + n + v] = sum[x][y][v];
+    for (int p = 0; p < 4; ++p)                                                              // (past the last: computed and not stored)
+        panel[p] = uniform_pointer((of_a ? a.a : a.b) + ((size_t)min(panel0 + p, last) * a.chunks + first) * kF8PanelBytes);
+    const int pitch = of_a ? a.a_pitch : a.b_pitch;
+    const char *scales = uniform_pointer((const char *)((of_a ? a.a_scales : a.b_scales) + (size_t)first * pitch));
+    const unsigned scale_at = (unsigned)min((panel0 * 16 + lane) >> (of_a ? a.a_shift : a.b_shift), pitch - 1) * 4u;
+    const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(size_t)((__attribute__((address_space(3))) const void *)lds));
+    auto issue = [&](int stage) __attribute__((always_inline)) {
+        const unsigned at = lds0 + (unsigned)(stage * STAGE);
+#pragma unroll
+        for (int p = 0; p < 4; p += 2) {
+            const void *planes[4] = {panel[p], panel[p] + 1024, panel[p + 1], panel[p + 1] + 1024};
+            global_to_lds16_run<4, 1024>(planes, lane * 16u, at + (unsigned)((4 * wave + p) * kF8PanelBytes));
+        }
+        global_to_lds4(scales, scale_at, at + (unsigned)(Shape::PANELS + wave * 256));
+#pragma unroll
+        for (int p = 0; p < 4; ++p) panel[p] += kF8PanelBytes;
+        scales += (size_t)pitch * 4;
+    };
+
+    float4v sum[MT][NT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) sum[x][y] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](const char *stage) __attribute__((always_inline)) {
+        const char *const pa = stage + wm * MT * kF8PanelBytes, *const pb = stage + (Shape::A + wn * NT) * kF8PanelBytes;
+        const float *const sa = (const float *)(stage + Shape::PANELS) + wm * MT * 16, *const sb = (const float *)(stage + Shape::PANELS) + (Shape::A + wn * NT) * 16;
+        F8Input<FA, WAY> fa[MT];
+        float s[MT];
+#pragma unroll
+        for (int x = 0; x < MT; ++x) {
+            fa[x].set(load_fragment(pa + x * kF8PanelBytes, lane));
+            s[x] = sa[x * 16 + i] * (BAND ? sb[0] : 1.0f);
+        }
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+            F8Input<FB, WAY> fb;
+            fb.set(load_fragment(pb + y * kF8PanelBytes, lane));
+            float4v more;
+            if constexpr (!BAND) more = *(const float4v *)(sb + y * 16 + 4 * b);
+#pragma unroll
+            for (int x = 0; x < MT; ++x) {
+                const float4v p = f8_products<FB, FA, WAY>(fb, fa[x]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sum[x][y][v] = fma32(BAND ? s[x] : s[x] * more[v], p[v], sum[x][y][v]);
             }
         }
+    };
+
+    issue(0);
+    for (int c = 0; c < count; ++c) {
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");       // this wave's pieces of the stage have landed
+        __syncthreads();                                         // everyone's have, and the other stage is read
+        if (c + 1 < count) issue((c + 1) % 2);
+        multiply(lds + c % 2 * STAGE);
+    }
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) put(a, (int)split, m_tile + wm * MT + x, n_tile + wn * NT + y, i, b, sum[x][y]);
 }
 
 // The pieces of a cut sum, in their order
@@ -134,36 +244,74 @@ __global__ void __launch_bounds__(256) f8_join_kernel(const F8Call a)
     }
 }
 
-struct F8Shape { int mt, splits, split_chunks; };
+struct F8Shape { int kind, mt, splits, split_chunks; };           // kind: 0 waves by themselves, 1 tiles of 128 x 128, 2 of 256 x 256
 
-static F8Shape f8_shape(int M, int N, int K)
+static F8Shape f8_shape(int M, int N, int K, bool full)
 {
     F8Shape p;
     const int chunks = K / kF8Chunk + (K % kF8Chunk != 0);
+    auto tiles = [&](int edge) { return ((int64_t)M + edge - 1) / edge * ((N + edge - 1) / edge); };
+    p.kind = M <= 64 ? 0 : full || tiles(256) < 192 ? 1 : 2;
     p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    const int64_t blocks = (((int64_t)M + 16 * p.mt - 1) / (16 * p.mt)) * ((N + 127) / 128);
+    const int64_t blocks = p.kind == 0 ? (((int64_t)M + 16 * p.mt - 1) / (16 * p.mt)) * ((N + 127) / 128) : tiles(p.kind == 1 ? 128 : 256);
+    const int wanted = p.kind == 0 ? 1024 : 384;
     p.splits = 1;
-    while (blocks * p.splits < 1024 && p.splits < 16 && p.splits * 8 <= chunks) p.splits *= 2;
+    while (blocks * p.splits * 2 <= wanted && p.splits < 16 && p.splits * 8 <= chunks) p.splits *= 2;
     p.split_chunks = ceil_div(chunks, p.splits);
     p.splits = ceil_div(chunks, p.split_chunks);
     return p;
 }
 
-size_t f8_matmul_workspace(int M, int N, int K)
+size_t f8_matmul_workspace(int M, int N, int K, int dtype)
 {
-    const F8Shape p = f8_shape(M, N, K);
+    const F8Shape p = f8_shape(M, N, K, dtype == NOVA_F32);
     return p.splits > 1 ? ((size_t)p.splits * M * N * 4 + 255) & ~(size_t)255 : 0;
+}
+
+template <typename Shape, int FA, int FB, int WAY, bool BAND>
+static int run_tiles(const F8Call &a, hipStream_t s)
+{
+    const auto kernel = f8_tile_kernel<Shape, FA, FB, WAY, BAND>;
+    NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::LDS));
+    const int64_t across = (a.b_tiles + Shape::B - 1) / Shape::B * (int64_t)a.splits;
+    const int64_t step = (((int64_t)1 << 22) / across > 0 ? ((int64_t)1 << 22) / across : 1) * Shape::A;           // rows in pieces that keep a launch below 2^31 threads
+    for (int64_t tile = 0; tile < a.a_tiles; tile += step) {
+        F8Call part = a;
+        part.a_tiles = (int)(a.a_tiles - tile < step ? a.a_tiles - tile : step);
+        part.M = (int)(a.M - tile * 16 < part.a_tiles * (int64_t)16 ? a.M - tile * 16 : part.a_tiles * (int64_t)16);
+        part.a += (size_t)tile * a.chunks * kF8PanelBytes;
+        part.a_scales += (tile * 16) >> a.a_shift;
+        part.out = (char *)a.out + tile * 16 * a.ldout * (int64_t)dtype_size(a.dtype);
+        kernel<<<(unsigned)(across * ((part.a_tiles + Shape::A - 1) / Shape::A)), Shape::THREADS, Shape::LDS, s>>>(part);
+        NOVA_HIP_TRY(hipGetLastError());
+    }
+    return 0;
+}
+
+template <typename Shape, int FA, int FB, int WAY>
+static int run_tiles(const F8Call &a, hipStream_t s)
+{
+    return a.b_shift ? run_tiles<Shape, FA, FB, WAY, true>(a, s) : run_tiles<Shape, FA, FB, WAY, false>(a, s);
 }
 
 template <int FA, int FB, int WAY>
 static int run(const F8Call &a, const F8Shape &p, hipStream_t s)
 {
-    const int64_t across = (a.b_tiles + 7) / 8;
-    const unsigned blocks = (unsigned)(across * ((a.a_tiles + p.mt - 1) / p.mt) * a.splits);
-    if (p.mt == 1) f8_wave_kernel<1, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-    else if (p.mt == 2) f8_wave_kernel<2, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-    else f8_wave_kernel<4, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-    NOVA_HIP_TRY(hipGetLastError());
+    if (p.kind == 0) {
+        const int64_t across = (a.b_tiles + 7) / 8;
+        const unsigned blocks = (unsigned)(across * ((a.a_tiles + p.mt - 1) / p.mt) * a.splits);
+        if (p.mt == 1) f8_wave_kernel<1, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
+        else if (p.mt == 2) f8_wave_kernel<2, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
+        else f8_wave_kernel<4, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
+        NOVA_HIP_TRY(hipGetLastError());
+    } else {
+        if constexpr (WAY == F8_NARROW) {
+            if (p.kind == 2) { if (int err = run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY>(a, s)) return err; }
+            else if (int err = run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY>(a, s)) return err;
+        } else {
+            if (int err = run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY>(a, s)) return err;
+        }
+    }
     if (a.splits == 1) return 0;
     const size_t joins = ((size_t)a.M * ((a.N + 3) / 4) + 255) / 256;
     f8_join_kernel<<<(unsigned)(joins < 65536 ? joins : 65536), 256, 0, s>>>(a);
@@ -179,7 +327,7 @@ static int run_way(const F8Call &a, const F8Shape &p, void *stream)
 int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream)
 {
     const F8Layout &la = a.layout, &lb = b.layout;
-    const F8Shape p = f8_shape(la.rows, lb.rows, la.columns);
+    const F8Shape p = f8_shape(la.rows, lb.rows, la.columns, dtype == NOVA_F32);
     const F8Call call = {(const char *)a.q, (const char *)b.q, (const float *)((const char *)a.q + la.code_bytes), (const float *)((const char *)b.q + lb.code_bytes),
                          bias, out, (float *)workspace, ldout, la.rows, lb.rows, la.chunks, p.splits, p.split_chunks, la.row_tiles, lb.row_tiles, la.scale_pitch,
                          lb.scale_pitch, la.block == 1 ? 0 : 7, lb.block == 1 ? 0 : 7, dtype, flags};

@@ -241,7 +241,7 @@ int launch_f8_pack(const uint8_t *codes, const float *scales, const F8Layout &q,
 int launch_f8_unpack(const void *Xq, const F8Layout &q, uint8_t *codes, float *scales, void *stream);
 int launch_f8_zero(void *out, int64_t ld, int rows, int columns, int dtype, void *stream);
 struct F8Operand { const void *q; F8Layout layout; int format; };
-size_t f8_matmul_workspace(int M, int N, int K);
+size_t f8_matmul_workspace(int M, int N, int K, int dtype);
 int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream);
 // Dropout: the forward call and its gradient
 struct DropoutArgs {
