@@ -26,53 +26,64 @@ __device__ __forceinline__ F8Fragment load_fragment(const char *panel, int lane)
     return f;
 }
 
-template <typename T>
-__device__ __forceinline__ void write_four(const F8Call &a, int64_t m, int n, float4v sum)
+// COUNT (or fewer, at the right edge) neighbouring results of a row
+template <typename T, int COUNT>
+__device__ __forceinline__ void write_row(const F8Call &a, int64_t m, int n, const float (&sum)[COUNT])
 {
-    const int count = min(4, a.N - n);
+    const int count = min(COUNT, a.N - n);
     T *to = (T *)a.out + m * a.ldout + n;
-    T r[4];
+    const T *bias = (const T *)a.bias + n;
+    struct alignas(4) Results { T v[COUNT]; } r, more = {};
+    if (count == COUNT) {
+        if (a.bias) __builtin_memcpy(&more, bias, sizeof more);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        if (v < count) {
-            float s = sum[v];
-            if (a.bias) s += load_f32((const T *)a.bias + n + v);
-            if (a.flags & NOVA_FLAG_ADD) s += load_f32(to + v);
-            if (a.flags & NOVA_FLAG_RELU) s = s < 0.0f ? 0.0f : s;
-            store_from_f32(&r[v], s);
-        }
+        for (int v = 0; v < COUNT; ++v) r.v[v] = (T)0.0f;
+        if (a.flags & NOVA_FLAG_ADD) __builtin_memcpy(&r, to, sizeof r);
     }
-    if (count == 4) {
-        __builtin_memcpy(to, r, sizeof r);
+#pragma unroll
+    for (int v = 0; v < COUNT; ++v) {
+        float s = sum[v];
+        if (count == COUNT) {
+            if (a.bias) s += (float)more.v[v];
+            if (a.flags & NOVA_FLAG_ADD) s += (float)r.v[v];
+        } else if (v < count) {
+            if (a.bias) s += load_f32(bias + v);
+            if (a.flags & NOVA_FLAG_ADD) s += load_f32(to + v);
+        }
+        if (a.flags & NOVA_FLAG_RELU) s = s < 0.0f ? 0.0f : s;
+        store_from_f32(&r.v[v], s);
+    }
+    if (count == COUNT) {
+        __builtin_memcpy(to, &r, sizeof r);
     } else {
 #pragma unroll
-        for (int v = 0; v < 3; ++v)
-            if (v < count) to[v] = r[v];
+        for (int v = 0; v < COUNT - 1; ++v)
+            if (v < count) to[v] = r.v[v];
     }
 }
 
-__device__ __forceinline__ void write_result(const F8Call &a, int64_t m, int n, float4v sum)
+template <int COUNT>
+__device__ __forceinline__ void write_result(const F8Call &a, int64_t m, int n, const float (&sum)[COUNT])
 {
     if (m >= a.M || n >= a.N) return;
-    if (a.dtype == NOVA_F32) write_four<float>(a, m, n, sum);
-    else if (a.dtype == NOVA_F16) write_four<f16>(a, m, n, sum);
-    else write_four<bf16>(a, m, n, sum);
+    if (a.dtype == NOVA_F32) write_row<float>(a, m, n, sum);
+    else if (a.dtype == NOVA_F16) write_row<f16>(a, m, n, sum);
+    else write_row<bf16>(a, m, n, sum);
 }
 
-// Rows 16 m_tile + i, columns 16 n_tile + 4 b ..: to the result, or to the pieces of a cut sum
-__device__ __forceinline__ void put(const F8Call &a, int split, int m_tile, int n_tile, int i, int b, float4v sum)
+// ... to the result, or to the pieces of a cut sum
+template <int COUNT>
+__device__ __forceinline__ void put(const F8Call &a, int split, int64_t m, int n, const float (&sum)[COUNT])
 {
-    const int64_t m = (int64_t)m_tile * 16 + i;
-    const int n = n_tile * 16 + 4 * b;
     if (a.splits == 1) {
         write_result(a, m, n, sum);
     } else if (m < a.M) {
         float *to = a.partial + ((size_t)split * a.M + m) * a.N + n;
-        if (n + 4 <= a.N) {
+        if (n + COUNT <= a.N) {
             __builtin_memcpy(to, &sum, sizeof sum);
         } else {
 #pragma unroll
-            for (int v = 0; v < 3; ++v)
+            for (int v = 0; v < COUNT - 1; ++v)
                 if (n + v < a.N) to[v] = sum[v];
         }
     }
@@ -124,7 +135,10 @@ __global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
 #pragma unroll
     for (int x = 0; x < MT; ++x)
 #pragma unroll
-        for (int y = 0; y < NT; ++y) put(a, split, m_tile + x, n_tile + y, i, b, sum[x][y]);
+        for (int y = 0; y < NT; ++y) {
+            const float four[4] = {sum[x][y][0], sum[x][y][1], sum[x][y][2], sum[x][y][3]};
+            put(a, split, (int64_t)(m_tile + x) * 16 + i, (n_tile + y) * 16 + 4 * b, four);
+        }
 }
 
 // ---- tiles ----
@@ -222,10 +236,27 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
         if (c + 1 < count) issue((c + 1) % 2);
         multiply(lds + c % 2 * STAGE);
     }
+    // Results leave as rows: a lane holds four columns of one row, and 16 rows side by side would go to memory as pieces of 32 bytes (8192 x 8192 results of one chunk
+    // 69.3 us).  So a wave passes them through LDS, 32 rows at a time, and writes a row of its tile as a whole.
+    constexpr int PITCH = NT * 64 + 16, LANES = NT * 2, OWN = Shape::LDS / Shape::WAVES;         // bytes of a row; lanes that write one, eight columns each
+    static_assert(MT % 2 == 0 && 32 * PITCH <= OWN && OWN % 16 == 0, "LDS of a wave");
+    __syncthreads();                                             // everyone has read the last stage
+    char *const own = lds + wave * OWN;
+    static_for<MT / 2>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = 2 * X;
 #pragma unroll
-    for (int x = 0; x < MT; ++x)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int y = 0; y < NT; ++y) put(a, (int)split, m_tile + wm * MT + x, n_tile + wn * NT + y, i, b, sum[x][y]);
+            for (int y = 0; y < NT; ++y) *(float4v *)(own + (h * 16 + i) * PITCH + y * 64 + b * 16) = sum[x + h][y];
+        exchange_in_wave();
+#pragma unroll 1
+        for (int r = lane / LANES; r < 32; r += 64 / LANES) {
+            float eight[8];
+            __builtin_memcpy(eight, own + r * PITCH + lane % LANES * 32, sizeof eight);
+            put(a, (int)split, (int64_t)(m_tile + wm * MT + x) * 16 + r, (n_tile + wn * NT) * 16 + lane % LANES * 8, eight);
+        }
+        exchange_in_wave();
+    });
 }
 
 // The pieces of a cut sum, in their order
@@ -235,7 +266,7 @@ __global__ void __launch_bounds__(256) f8_join_kernel(const F8Call a)
     for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < (size_t)a.M * groups; idx += (size_t)gridDim.x * 256) {
         const int64_t m = idx / groups;
         const int n = (int)(idx % groups) * 4;
-        float4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int split = 0; split < a.splits; ++split)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
