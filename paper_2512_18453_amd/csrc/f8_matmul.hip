@@ -26,67 +26,60 @@ __device__ __forceinline__ F8Fragment load_fragment(const char *panel, int lane)
     return f;
 }
 
-// COUNT (or fewer, at the right edge) neighbouring results of a row
+// Where results go: COUNT neighbouring columns from n on, of the rows that a thread is given.  What does not change from row to row is decided once: checks for
+// every element in the loop over rows made the results of a 256 x 256 tile take 11 us.
 template <typename T, int COUNT>
-__device__ __forceinline__ void write_row(const F8Call &a, int64_t m, int n, const float (&sum)[COUNT])
-{
-    const int count = min(COUNT, a.N - n);
-    T *to = (T *)a.out + m * a.ldout + n;
-    const T *bias = (const T *)a.bias + n;
-    struct alignas(4) Results { T v[COUNT]; } r, more = {};
-    if (count == COUNT) {
-        if (a.bias) __builtin_memcpy(&more, bias, sizeof more);
+struct F8Columns {
+    T *to;                                        // column n of row 0
+    int64_t ld;
+    int count;                                    // of the COUNT columns exist
+    bool add, relu;
+    float bias[COUNT];
+
+    __device__ __forceinline__ F8Columns(void *out, int64_t ldout, const void *bias_row, int flags, int N, int n)
+        : to((T *)out + n), ld(ldout), count(min(COUNT, N - n)), add((flags & NOVA_FLAG_ADD) != 0), relu((flags & NOVA_FLAG_RELU) != 0)
+    {
 #pragma unroll
-        for (int v = 0; v < COUNT; ++v) r.v[v] = (T)0.0f;
-        if (a.flags & NOVA_FLAG_ADD) __builtin_memcpy(&r, to, sizeof r);
+        for (int v = 0; v < COUNT; ++v) bias[v] = bias_row && v < count ? load_f32((const T *)bias_row + n + v) : 0.0f;
     }
+    __device__ __forceinline__ void write(int64_t m, const float (&sum)[COUNT]) const
+    {
+        struct Results { T v[COUNT]; } r = {};
+        T *const at = to + m * ld;
+        if (add) {
+            if (count == COUNT) {
+                __builtin_memcpy(&r, at, sizeof r);
+            } else {
 #pragma unroll
-    for (int v = 0; v < COUNT; ++v) {
-        float s = sum[v];
-        if (count == COUNT) {
-            if (a.bias) s += (float)more.v[v];
-            if (a.flags & NOVA_FLAG_ADD) s += (float)r.v[v];
-        } else if (v < count) {
-            if (a.bias) s += load_f32(bias + v);
-            if (a.flags & NOVA_FLAG_ADD) s += load_f32(to + v);
+                for (int v = 0; v < COUNT - 1; ++v)
+                    if (v < count) r.v[v] = at[v];
+            }
         }
-        if (a.flags & NOVA_FLAG_RELU) s = s < 0.0f ? 0.0f : s;
-        store_from_f32(&r.v[v], s);
-    }
-    if (count == COUNT) {
-        __builtin_memcpy(to, &r, sizeof r);
-    } else {
 #pragma unroll
-        for (int v = 0; v < COUNT - 1; ++v)
-            if (v < count) to[v] = r.v[v];
-    }
-}
-
-template <int COUNT>
-__device__ __forceinline__ void write_result(const F8Call &a, int64_t m, int n, const float (&sum)[COUNT])
-{
-    if (m >= a.M || n >= a.N) return;
-    if (a.dtype == NOVA_F32) write_row<float>(a, m, n, sum);
-    else if (a.dtype == NOVA_F16) write_row<f16>(a, m, n, sum);
-    else write_row<bf16>(a, m, n, sum);
-}
-
-// ... to the result, or to the pieces of a cut sum
-template <int COUNT>
-__device__ __forceinline__ void put(const F8Call &a, int split, int64_t m, int n, const float (&sum)[COUNT])
-{
-    if (a.splits == 1) {
-        write_result(a, m, n, sum);
-    } else if (m < a.M) {
-        float *to = a.partial + ((size_t)split * a.M + m) * a.N + n;
-        if (n + COUNT <= a.N) {
-            __builtin_memcpy(to, &sum, sizeof sum);
+        for (int v = 0; v < COUNT; ++v) {
+            float s = sum[v] + bias[v];
+            if (add) s += (float)r.v[v];
+            if (relu) s = s < 0.0f ? 0.0f : s;
+            store_from_f32(&r.v[v], s);
+        }
+        if (count == COUNT) {
+            __builtin_memcpy(at, &r, sizeof r);
         } else {
 #pragma unroll
             for (int v = 0; v < COUNT - 1; ++v)
-                if (n + v < a.N) to[v] = sum[v];
+                if (v < count) at[v] = r.v[v];
         }
     }
+};
+
+// f(columns) with the columns n .. of the result, or of a piece of a cut sum
+template <int COUNT, typename F>
+__device__ __forceinline__ void with_columns(const F8Call &a, int split, int n, F &&f)
+{
+    if (a.splits > 1) f(F8Columns<float, COUNT>(a.partial + (size_t)split * a.M * a.N, a.N, nullptr, 0, a.N, n));
+    else if (a.dtype == NOVA_F32) f(F8Columns<float, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
+    else if (a.dtype == NOVA_F16) f(F8Columns<f16, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
+    else f(F8Columns<bf16, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
 }
 
 // A wave makes 16 MT x 16 NT results from operands that it loads itself
@@ -133,12 +126,18 @@ __global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
             }
     }
 #pragma unroll
-    for (int x = 0; x < MT; ++x)
+    for (int y = 0; y < NT; ++y) {
+        const int n = (n_tile + y) * 16 + 4 * b;
+        if (n < a.N)
+            with_columns<4>(a, split, n, [&](const auto &columns) __attribute__((always_inline)) {
 #pragma unroll
-        for (int y = 0; y < NT; ++y) {
-            const float four[4] = {sum[x][y][0], sum[x][y][1], sum[x][y][2], sum[x][y][3]};
-            put(a, split, (int64_t)(m_tile + x) * 16 + i, (n_tile + y) * 16 + 4 * b, four);
-        }
+                for (int x = 0; x < MT; ++x) {
+                    const int64_t m = (int64_t)(m_tile + x) * 16 + i;
+                    const float four[4] = {sum[x][y][0], sum[x][y][1], sum[x][y][2], sum[x][y][3]};
+                    if (m < a.M) columns.write(m, four);
+                }
+            });
+    }
 }
 
 // ---- tiles ----
@@ -242,36 +241,43 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
     static_assert(MT % 2 == 0 && 32 * PITCH <= OWN && OWN % 16 == 0, "LDS of a wave");
     __syncthreads();                                             // everyone has read the last stage
     char *const own = lds + wave * OWN;
-    static_for<MT / 2>([&](auto X) __attribute__((always_inline)) {
-        constexpr int x = 2 * X;
+    const int n = (n_tile + wn * NT) * 16 + lane % LANES * 8;
+    with_columns<8>(a, (int)split, n, [&](const auto &columns) __attribute__((always_inline)) {
+        static_for<MT / 2>([&](auto X) __attribute__((always_inline)) {
+            constexpr int x = 2 * X;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int y = 0; y < NT; ++y) *(float4v *)(own + (h * 16 + i) * PITCH + y * 64 + b * 16) = sum[x + h][y];
-        exchange_in_wave();
-#pragma unroll 1
-        for (int r = lane / LANES; r < 32; r += 64 / LANES) {
-            float eight[8];
-            __builtin_memcpy(eight, own + r * PITCH + lane % LANES * 32, sizeof eight);
-            put(a, (int)split, (int64_t)(m_tile + wm * MT + x) * 16 + r, (n_tile + wn * NT) * 16 + lane % LANES * 8, eight);
-        }
-        exchange_in_wave();
+                for (int y = 0; y < NT; ++y) *(float4v *)(own + (h * 16 + i) * PITCH + y * 64 + b * 16) = sum[x + h][y];
+            exchange_in_wave();
+#pragma unroll
+            for (int k = 0; k < 32 * LANES / 64; ++k) {
+                const int r = lane / LANES + k * (64 / LANES);
+                const int64_t m = (int64_t)(m_tile + wm * MT + x) * 16 + r;
+                const float4v *from = (const float4v *)(own + r * PITCH + lane % LANES * 32);
+                const float4v low = from[0], high = from[1];
+                const float eight[8] = {low[0], low[1], low[2], low[3], high[0], high[1], high[2], high[3]};
+                if (m < a.M && n < a.N) columns.write(m, eight);
+            }
+            exchange_in_wave();
+        });
     });
 }
 
 // The pieces of a cut sum, in their order
-__global__ void __launch_bounds__(256) f8_join_kernel(const F8Call a)
+__global__ void __launch_bounds__(256) f8_join_kernel(F8Call a)
 {
-    const int groups = (a.N + 3) / 4;
+    const int groups = (a.N + 3) / 4, splits = a.splits;
+    a.splits = 1;
     for (size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x; idx < (size_t)a.M * groups; idx += (size_t)gridDim.x * 256) {
         const int64_t m = idx / groups;
         const int n = (int)(idx % groups) * 4;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int split = 0; split < a.splits; ++split)
+        for (int split = 0; split < splits; ++split)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 if (n + v < a.N) sum[v] += a.partial[((size_t)split * a.M + m) * a.N + n + v];
-        write_result(a, m, n, sum);
+        with_columns<4>(a, 0, n, [&](const auto &columns) __attribute__((always_inline)) { columns.write(m, sum); });
     }
 }
 
