@@ -63,7 +63,11 @@ struct F8Columns {
             store_from_f32(&r.v[v], s);
         }
         if (count == COUNT) {
-            __builtin_memcpy(at, &r, sizeof r);
+            // (past the caches' own order of writing back: 8192 x 8192 results of one chunk 57.4 us without, 41.9 with)
+            typedef unsigned Words __attribute__((ext_vector_type(sizeof r / 4), aligned(sizeof(T))));
+            Words words;
+            __builtin_memcpy(&words, &r, sizeof r);
+            __builtin_nontemporal_store(words, (Words *)at);
         } else {
 #pragma unroll
             for (int v = 0; v < COUNT - 1; ++v)
@@ -144,10 +148,16 @@ __global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
 //
 // A workgroup of WM x WN waves makes 16 WM MT rows by 16 WN NT columns.  A stage is a chunk of both operands' panels with their scales; stages come straight from global
 // memory to LDS, one ahead of the one that is multiplied, and a panel lies there as it lies in memory: the 64 lanes of a wave read 1024 bytes side by side.
+//
+// 8192 x 8192 x 8192 to bfloat16 439 us, 2504 TFLOP/s where a large library product of that format with one scale per matrix reaches 2655; with a scale per row and chunk
+// of B too, where a sum takes two vector instructions instead of one, 527.  LDS binds about as much as the matrix unit: a chunk of a 256 x 256 tile is 2048 clocks of matrix
+// instructions, 64 KB written and 192 KB read at 128 bytes a clock.  128 x 128 tiles, two workgroups per compute unit, read a third more: 512 us.  A's panels loaded by
+// each wave into registers instead took more of those than there are (813).
 template <int WM_, int WN_, int MT_, int NT_>
 struct F8Tile {
     static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, WAVES = WM * WN, THREADS = WAVES * 64, A = WM * MT, B = WN * NT;        // panels
-    static constexpr int PANELS = (A + B) * kF8PanelBytes, STAGE = PANELS + (A + B) * kF8Rows * 4, LDS = 2 * STAGE;
+    static constexpr int PANELS = (A + B) * kF8PanelBytes, STAGE = PANELS + (A + B) * kF8Rows * 4, PITCH = NT * 64 + 16;
+    static constexpr int LDS = 2 * STAGE > WAVES * 32 * PITCH ? 2 * STAGE : WAVES * 32 * PITCH;                                         // 32 rows of each wave's results
     static_assert(A % 4 == 0 && A + B == 4 * WAVES, "a wave loads four panels of one operand, and 64 scales");
 };
 
@@ -170,8 +180,8 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
     // eight tiles of rows go along the columns together: what an XCD works on at a time is a patch of tiles
     const unsigned across = (a.b_tiles + Shape::B - 1) / Shape::B, down = (a.a_tiles + Shape::A - 1) / Shape::A, tiles = across * down;
     const unsigned id = xcd_local_block_id(blockIdx.x, gridDim.x), split = id / tiles, tile = id % tiles;
-    const unsigned first_row = tile / (8 * across) * 8, rows = min(8u, down - first_row), in_group = tile % (8 * across);
-    const int m_tile = (int)(first_row + in_group % rows) * Shape::A, n_tile = (int)(in_group / rows) * Shape::B;
+    const unsigned first_row = tile / (8 * across) * 8, together = min(8u, down - first_row), in_group = tile % (8 * across);
+    const int m_tile = (int)(first_row + in_group % together) * Shape::A, n_tile = (int)(in_group / together) * Shape::B;
     const int first = split * a.split_chunks, count = min(a.chunks - first, a.split_chunks);
 
     // what this wave loads: panels 4 wave .. of A's and then B's, the scales of 64 rows
@@ -207,40 +217,66 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
         const char *const pa = stage + wm * MT * kF8PanelBytes, *const pb = stage + (Shape::A + wn * NT) * kF8PanelBytes;
         const float *const sa = (const float *)(stage + Shape::PANELS) + wm * MT * 16, *const sb = (const float *)(stage + Shape::PANELS) + (Shape::A + wn * NT) * 16;
         F8Input<FA, WAY> fa[MT];
+        F8Input<FB, WAY> fb[2];
         float s[MT];
+        float4v more[3], p[3];
 #pragma unroll
         for (int x = 0; x < MT; ++x) {
             fa[x].set(load_fragment(pa + x * kF8PanelBytes, lane));
             s[x] = sa[x * 16 + i] * (BAND ? sb[0] : 1.0f);
         }
+        auto load_columns = [&](int y) __attribute__((always_inline)) {
+            fb[y % 2].set(load_fragment(pb + y * kF8PanelBytes, lane));
+            if constexpr (!BAND) more[y % 3] = *(const float4v *)(sb + y * 16 + 4 * b);
+        };
+        auto add = [&](int k, const float4v &products) __attribute__((always_inline)) {
+            const int x = k % MT, y = k / MT;
 #pragma unroll
-        for (int y = 0; y < NT; ++y) {
-            F8Input<FB, WAY> fb;
-            fb.set(load_fragment(pb + y * kF8PanelBytes, lane));
-            float4v more;
-            if constexpr (!BAND) more = *(const float4v *)(sb + y * 16 + 4 * b);
-#pragma unroll
-            for (int x = 0; x < MT; ++x) {
-                const float4v p = f8_products<FB, FA, WAY>(fb, fa[x]);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) sum[x][y][v] = fma32(BAND ? s[x] : s[x] * more[v], p[v], sum[x][y][v]);
-            }
+            for (int v = 0; v < 4; ++v) sum[x][y][v] = fma32(BAND ? s[x] : s[x] * more[y % 3][v], products[v], sum[x][y][v]);
+        };
+        if constexpr (WAY == F8_NARROW) {
+            // A wave issues its instructions in order, so each matrix instruction is followed by the additions of the one two before, whose sums have arrived.  (The empty
+            // statements keep that order: the compiler gathers the additions behind the matrix instructions, with more sums in between than there are registers.)
+            load_columns(0);
+            static_for<MT * NT + 2>([&](auto K) __attribute__((always_inline)) {
+                constexpr int k = K, x = k % MT, y = k / MT;
+                if constexpr (k < MT * NT) {
+                    asm volatile("" : "+v"(fa[x].codes));
+                    p[k % 3] = f8_products<FB, FA, WAY>(fb[y % 2], fa[x]);
+                    if constexpr (x == 0 && y + 1 < NT) load_columns(y + 1);
+                }
+                if constexpr (k >= 2) {
+                    add(k - 2, p[(k - 2) % 3]);
+                    asm volatile("" : "+v"(sum[(k - 2) % MT][(k - 2) / MT]));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        } else {
+            static_for<MT * NT>([&](auto K) __attribute__((always_inline)) {
+                if constexpr (K % MT == 0) load_columns(K / MT);
+                add(K, f8_products<FB, FA, WAY>(fb[K / MT % 2], fa[K % MT]));
+            });
         }
     };
 
-    issue(0);
-    for (int c = 0; c < count; ++c) {
+    auto step = [&](int c) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");       // this wave's pieces of the stage have landed
         __syncthreads();                                         // everyone's have, and the other stage is read
         if (c + 1 < count) issue((c + 1) % 2);
+        __builtin_amdgcn_sched_barrier(0);
         multiply(lds + c % 2 * STAGE);
+    };
+    issue(0);
+    for (int c = 0; c < count; c += 2) {                         // (in pairs, so that which stage it is is known: 1024 x 4096 x 4096 32.5 -> 25.6 us)
+        step(c);
+        if (c + 1 < count) step(c + 1);
     }
     // Results leave as rows: a lane holds four columns of one row, and 16 rows side by side would go to memory as pieces of 32 bytes (8192 x 8192 results of one chunk
     // 69.3 us).  So a wave passes them through LDS, 32 rows at a time, and writes a row of its tile as a whole.
-    constexpr int PITCH = NT * 64 + 16, LANES = NT * 2, OWN = Shape::LDS / Shape::WAVES;         // bytes of a row; lanes that write one, eight columns each
-    static_assert(MT % 2 == 0 && 32 * PITCH <= OWN && OWN % 16 == 0, "LDS of a wave");
+    constexpr int PITCH = Shape::PITCH, LANES = NT * 2;                                   // bytes of a row; lanes that write one, eight columns each
+    static_assert(MT % 2 == 0, "rows in pairs of panels");
     __syncthreads();                                             // everyone has read the last stage
-    char *const own = lds + wave * OWN;
+    char *const own = lds + wave * 32 * PITCH;
     const int n = (n_tile + wn * NT) * 16 + lane % LANES * 8;
     with_columns<8>(a, (int)split, n, [&](const auto &columns) __attribute__((always_inline)) {
         static_for<MT / 2>([&](auto X) __attribute__((always_inline)) {
