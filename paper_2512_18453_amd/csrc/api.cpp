@@ -632,8 +632,7 @@ extern "C" int nova_f8_linear(const void *x, int64_t ldx, const void *Wq, size_t
     if (workspace_bytes < nova_f8_linear_workspace_bytes(M, N, K, dtype)) return NOVA_ENOSPC;
     const F8Source src = {x, ldx, nullptr, 0, M, K, dtype};
     const F8Operand a = {workspace, make_f8_layout(M, K, 1), NOVA_F8_E4M3};
-    if (int err = launch_f8_quantize(src, a.layout, a.format, 0, workspace, stream)) return hip_result(err);
-    return hip_result(launch_f8_matmul(a, w, bias, y, ldy, dtype, flags, (char *)workspace + padded(a.layout), stream));
+    return hip_result(launch_f8_linear(src, a, w, bias, y, ldy, flags, (char *)workspace + padded(a.layout), stream));
 }
 
 // The parts of a backward call's workspace, in their order

@@ -20,32 +20,6 @@ struct F8Quantize {
 
 __device__ __forceinline__ float *f8_scales(char *q, const F8Layout &layout) { return (float *)(q + layout.code_bytes); }
 
-// Largest magnitude as bits (infinity is above every number, NaN above infinity) -> scale; a block that holds one of them has scale NaN
-template <int FORMAT>
-__device__ __forceinline__ float scale_of(unsigned bits)
-{
-    return bits < 0x7f800000u ? __uint_as_float(bits) / kLargestCode<FORMAT> : __builtin_nanf("");
-}
-
-__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
-// Quotients as nova.h defines them: divided in binary32, kept within the largest code (a scale that is subnormal can be too small by half); 0 for scales of 0 and NaN
-template <int FORMAT>
-__device__ __forceinline__ float quotient(float v, float scale)
-{
-    constexpr float L = kLargestCode<FORMAT>;
-    return scale > 0.0f ? __builtin_amdgcn_fmed3f(v / scale, -L, L) : 0.0f;
-}
-
-// The largest value over the 16 lanes of a row of the wave
-__device__ __forceinline__ unsigned largest_of_16(unsigned v)
-{
-    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false));      // rotations by 8, 4, 2, 1
-    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
-    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
-    return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
-}
-
 // A tile's codes from LDS to the panels row_tile .. of a chunk
 __device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
 {
@@ -130,9 +104,10 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
                     if (j == 0 && row + k < a.rows_layout.scale_pitch)
                         f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + row + k] = s;
                 }
+                const F8Quotient<FORMAT> quotient(s);
                 float q[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = quotient<FORMAT>(v[k][e], s);
+                for (int e = 0; e < 8; ++e) q[e] = quotient(v[k][e]);
                 unsigned *at = (unsigned *)staged + (g / 2 * kF8PanelBytes + j / 2 % 2 * 1024 + (j / 4 * 16 + g % 2 * 8 + k) * 16 + j % 2 * 8) / 4;
                 at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
                 at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);
@@ -152,9 +127,10 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
                     if (g == 0 && column + e < a.columns_layout.scale_pitch)
                         f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + column + e] = s;
                 }
+                const F8Quotient<FORMAT> quotient(s);
                 float q[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) q[k] = quotient<FORMAT>(v[k][e], s);
+                for (int k = 0; k < 8; ++k) q[k] = quotient(v[k][e]);
                 unsigned *at = (unsigned *)staged + (j / 2 * kF8PanelBytes + g / 2 % 2 * 1024 + (g / 4 * 16 + j % 2 * 8 + e) * 16 + g % 2 * 8) / 4;
                 at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
                 at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);

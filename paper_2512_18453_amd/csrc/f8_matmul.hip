@@ -86,61 +86,116 @@ __device__ __forceinline__ void with_columns(const F8Call &a, int split, int n, 
     else f(F8Columns<bf16, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
 }
 
-// A wave makes 16 MT x 16 NT results from operands that it loads itself
-template <int MT, int NT, int FA, int FB, int WAY>
-__global__ void __launch_bounds__(256) f8_wave_kernel(const F8Call a)
+// ---- up to 64 rows ----
+//
+// Bound by B's bytes.  A workgroup makes 16 columns for all rows; its waves take the chunks of those columns in turn, load B's panels straight into registers, AHEAD - 1 ahead, and
+// add up through LDS in the order of their numbers.  A's panels come the same way from L2; or, with few rows, every workgroup quantises x by itself first, into LDS,
+// which saves the launch that would do it.
+constexpr int kLaidOut = -1;
+struct F8RowsOf { const void *x; int64_t ld; int K; };           // what A is quantised from
+constexpr size_t kFusedElements = 32768, kFusedLds = 128 * 1024;
+
+// MT panels of rows; DT: kLaidOut, or the type of x
+template <int MT, int FA, int FB, int WAY, bool BAND, int DT>
+__global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8RowsOf rows)
 {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = lane % 16, b = lane / 16;
-    const int across = (a.b_tiles + 4 * NT - 1) / (4 * NT);
-    const int split = blockIdx.x % a.splits;
-    const unsigned at = blockIdx.x / a.splits;
-    const int n_tile = (int)(at % across) * 4 * NT + wave * NT, m_tile = (int)(at / across) * MT;
-    if (n_tile >= a.b_tiles) return;
-    float4v sum[MT][NT];
+    constexpr bool FUSED = DT != kLaidOut;
+    constexpr int AHEAD = MT == 4 ? 2 : MT == 2 ? 3 : 4;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, i = lane % 16, b = lane / 16;
+    const int tile = blockIdx.x % a.b_tiles, split = blockIdx.x / a.b_tiles;
+    const int first = split * a.split_chunks, count = min(a.chunks - first, a.split_chunks);
+    const int steps = count > wave ? (count - wave + waves - 1) / waves : 0;
+    const char *const panels = a.b + ((size_t)tile * a.chunks + first) * kF8PanelBytes;
+    float *const scales_in_lds = (float *)(lds + (size_t)count * a.M * kF8Chunk);
+
+    struct Stage {
+        F8Fragment b, a[FUSED ? 1 : MT];
+        float4v b_scale;
+        float a_scale[MT];
+    };
+    auto load = [&](int step, Stage &s) __attribute__((always_inline)) {
+        // (past the last: the last once more, and not multiplied, so that no load is in a branch)
+        const int c = wave + min(step, steps - 1) * waves;
+        const char *const at = panels + (size_t)c * kF8PanelBytes + lane * 16u;
+        s.b.half[0] = __builtin_nontemporal_load((const uint4v *)at);
+        s.b.half[1] = __builtin_nontemporal_load((const uint4v *)(at + 1024));
+        const float *const sb = a.b_scales + (size_t)(first + c) * a.b_pitch;
+        if constexpr (BAND) s.b_scale[0] = sb[(tile * 16) >> a.b_shift];
+        else s.b_scale = *(const float4v *)(sb + tile * 16 + 4 * b);
+        if constexpr (!FUSED) {
 #pragma unroll
-    for (int x = 0; x < MT; ++x)
+            for (int x = 0; x < MT; ++x) {
+                const int t = min(x, a.a_tiles - 1);
+                s.a[x] = load_fragment(a.a + ((size_t)t * a.chunks + first + c) * kF8PanelBytes, lane);
+                s.a_scale[x] = a.a_scales[(size_t)(first + c) * a.a_pitch + ((t * 16 + i) >> a.a_shift)];
+            }
+        }
+    };
+    float4v sum[MT];
 #pragma unroll
-        for (int y = 0; y < NT; ++y) sum[x][y] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    const int last = min(a.chunks, (split + 1) * a.split_chunks);
-    for (int c = split * a.split_chunks; c < last; ++c) {
-        F8Input<FA, WAY> fa[MT];
-        F8Input<FB, WAY> fb[NT];
-        float sa[MT];
-        float4v sb[NT];
+    for (int x = 0; x < MT; ++x) sum[x] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](int step, Stage &s) __attribute__((always_inline)) {
+        if constexpr (FUSED) {
+            const int at = (wave + step * waves) * a.M + min(i, a.M - 1);
+            s.a[0].half[0] = *(const uint4v *)(lds + (size_t)at * kF8Chunk + b * 32);
+            s.a[0].half[1] = *(const uint4v *)(lds + (size_t)at * kF8Chunk + b * 32 + 16);
+            s.a_scale[0] = scales_in_lds[at];
+        }
+        F8Input<FB, WAY> fb;
+        fb.set(s.b);
 #pragma unroll
         for (int x = 0; x < MT; ++x) {
-            const int tile = min(m_tile + x, a.a_tiles - 1);
-            fa[x].set(load_fragment(a.a + ((size_t)tile * a.chunks + c) * kF8PanelBytes, lane));
-            sa[x] = a.a_scales[(size_t)c * a.a_pitch + ((tile * 16 + i) >> a.a_shift)];
+            F8Input<FA, WAY> fa;
+            fa.set(s.a[x]);
+            const float4v p = f8_products<FB, FA, WAY>(fb, fa);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sum[x][v] = fma32(s.a_scale[x] * s.b_scale[BAND ? 0 : v], p[v], sum[x][v]);
         }
+    };
+
+    Stage stage[AHEAD];
+    if (steps > 0) static_for<AHEAD - 1>([&](auto I) __attribute__((always_inline)) { load(I, stage[I]); });
+    if constexpr (FUSED) {
+        // sixteen lanes take a row's chunk, eight elements each
+        for (int at = threadIdx.x / 16; at < count * a.M; at += blockDim.x / 16) {
+            const int c = at / a.M, m = at % a.M, column = (first + c) * kF8Chunk + lane % 16 * 8;
+            const Eight<Storage<DT>> x = load_eight((const Storage<DT> *)rows.x + m * rows.ld + column, rows.K - column, column >= 8 && column < rows.K);
+            unsigned largest = 0;
 #pragma unroll
-        for (int y = 0; y < NT; ++y) {
-            const int tile = min(n_tile + y, a.b_tiles - 1);
-            fb[y].set(load_fragment(a.b + ((size_t)tile * a.chunks + c) * kF8PanelBytes, lane));
+            for (int e = 0; e < 8; ++e) largest = max(largest, magnitude((float)x.v[e]));
+            const float scale = scale_of<FA>(largest_of_16(largest));
+            const F8Quotient<FA> quotient(scale);
+            float q[8];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sb[y][v] = a.b_scales[(size_t)c * a.b_pitch + ((tile * 16 + 4 * b + v) >> a.b_shift)];
+            for (int e = 0; e < 8; ++e) q[e] = quotient((float)x.v[e]);
+            unsigned *const to = (unsigned *)(lds + (size_t)at * kF8Chunk + lane % 16 * 8);
+            to[0] = f8_codes<FA>(q[0], q[1], q[2], q[3]);
+            to[1] = f8_codes<FA>(q[4], q[5], q[6], q[7]);
+            if (lane % 16 == 0) scales_in_lds[at] = scale;
         }
-#pragma unroll
-        for (int x = 0; x < MT; ++x)
-#pragma unroll
-            for (int y = 0; y < NT; ++y) {
-                const float4v p = f8_products<FB, FA, WAY>(fb[y], fa[x]);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) sum[x][y][v] = fma32(sa[x] * sb[y][v], p[v], sum[x][y][v]);
-            }
+        __syncthreads();
     }
+    for (int step = 0; step < steps; step += AHEAD)
+        static_for<AHEAD>([&](auto I) __attribute__((always_inline)) {
+            load(step + I + AHEAD - 1, stage[(I + AHEAD - 1) % AHEAD]);
+            if (step + I < steps) multiply(step + I, stage[I]);
+        });
+
+    if constexpr (FUSED) __syncthreads();
+    float4v *const sums = (float4v *)lds;
 #pragma unroll
-    for (int y = 0; y < NT; ++y) {
-        const int n = (n_tile + y) * 16 + 4 * b;
-        if (n < a.N)
-            with_columns<4>(a, split, n, [&](const auto &columns) __attribute__((always_inline)) {
+    for (int x = 0; x < MT; ++x) sums[(wave * MT + x) * 64 + lane] = sum[x];
+    __syncthreads();
+    for (int e = threadIdx.x; e < MT * 64; e += blockDim.x) {
+        float four[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int w = 0; w < waves; ++w) {
+            const float4v part = sums[w * MT * 64 + e];
 #pragma unroll
-                for (int x = 0; x < MT; ++x) {
-                    const int64_t m = (int64_t)(m_tile + x) * 16 + i;
-                    const float four[4] = {sum[x][y][0], sum[x][y][1], sum[x][y][2], sum[x][y][3]};
-                    if (m < a.M) columns.write(m, four);
-                }
-            });
+            for (int v = 0; v < 4; ++v) four[v] += part[v];
+        }
+        const int m = e / 64 * 16 + i, n = tile * 16 + 4 * b;
+        if (m < a.M && n < a.N) with_columns<4>(a, split, n, [&](const auto &columns) __attribute__((always_inline)) { columns.write(m, four); });
     }
 }
 
@@ -317,20 +372,27 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8Call a)
     }
 }
 
-struct F8Shape { int kind, mt, splits, split_chunks; };           // kind: 0 waves by themselves, 1 tiles of 128 x 128, 2 of 256 x 256
+struct F8Shape { int kind, mt, waves, splits, split_chunks; };           // kind: 0 up to 64 rows, 1 tiles of 128 x 128, 2 of 256 x 256
 
 static F8Shape f8_shape(int M, int N, int K, bool full)
 {
-    F8Shape p;
+    F8Shape p = {};
     const int chunks = K / kF8Chunk + (K % kF8Chunk != 0);
     auto tiles = [&](int edge) { return ((int64_t)M + edge - 1) / edge * ((N + edge - 1) / edge); };
-    p.kind = M <= 64 ? 0 : full || tiles(256) < 192 ? 1 : 2;
-    p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    const int64_t blocks = p.kind == 0 ? (((int64_t)M + 16 * p.mt - 1) / (16 * p.mt)) * ((N + 127) / 128) : tiles(p.kind == 1 ? 128 : 256);
-    const int wanted = p.kind == 0 ? 1024 : 384;
     p.splits = 1;
-    while (blocks * p.splits * 2 <= wanted && p.splits < 16 && p.splits * 8 <= chunks) p.splits *= 2;
-    p.split_chunks = ceil_div(chunks, p.splits);
+    if (M <= 64) {
+        p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+        // a column tile is one workgroup's; fewer than the chip holds, of long sums, are cut
+        const int64_t panels = (N + 15) / 16;
+        while (panels * p.splits * 2 <= 512 && p.splits < 64 && chunks / (p.splits * 2) >= 32) p.splits *= 2;
+        p.split_chunks = ceil_div(chunks, p.splits);
+        p.waves = p.split_chunks >= 8 ? 8 : p.split_chunks >= 4 ? 4 : p.split_chunks;
+    } else {
+        p.kind = full || tiles(256) < 192 ? 1 : 2;
+        const int64_t blocks = tiles(p.kind == 1 ? 128 : 256);
+        while (blocks * p.splits * 2 <= 384 && p.splits < 16 && p.splits * 8 <= chunks) p.splits *= 2;
+        p.split_chunks = ceil_div(chunks, p.splits);
+    }
     p.splits = ceil_div(chunks, p.split_chunks);
     return p;
 }
@@ -361,52 +423,79 @@ static int run_tiles(const F8Call &a, hipStream_t s)
     return 0;
 }
 
-template <typename Shape, int FA, int FB, int WAY>
-static int run_tiles(const F8Call &a, hipStream_t s)
+template <int MT, int FA, int FB, int WAY, bool BAND, int DT>
+static int run_rows(const F8Call &a, const F8RowsOf &rows, const F8Shape &p, hipStream_t s)
 {
-    return a.b_shift ? run_tiles<Shape, FA, FB, WAY, true>(a, s) : run_tiles<Shape, FA, FB, WAY, false>(a, s);
-}
-
-template <int FA, int FB, int WAY>
-static int run(const F8Call &a, const F8Shape &p, hipStream_t s)
-{
-    if (p.kind == 0) {
-        const int64_t across = (a.b_tiles + 7) / 8;
-        const unsigned blocks = (unsigned)(across * ((a.a_tiles + p.mt - 1) / p.mt) * a.splits);
-        if (p.mt == 1) f8_wave_kernel<1, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-        else if (p.mt == 2) f8_wave_kernel<2, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-        else f8_wave_kernel<4, 2, FA, FB, WAY><<<blocks, 256, 0, s>>>(a);
-        NOVA_HIP_TRY(hipGetLastError());
-    } else {
-        if constexpr (WAY == F8_NARROW) {
-            if (p.kind == 2) { if (int err = run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY>(a, s)) return err; }
-            else if (int err = run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY>(a, s)) return err;
-        } else {
-            if (int err = run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY>(a, s)) return err;
-        }
-    }
-    if (a.splits == 1) return 0;
-    const size_t joins = ((size_t)a.M * ((a.N + 3) / 4) + 255) / 256;
-    f8_join_kernel<<<(unsigned)(joins < 65536 ? joins : 65536), 256, 0, s>>>(a);
+    const auto kernel = f8_rows_kernel<MT, FA, FB, WAY, BAND, DT>;
+    const size_t sums = (size_t)p.waves * MT * 1024, operand = DT == kLaidOut ? 0 : (size_t)a.split_chunks * a.M * (kF8Chunk + 4);
+    const size_t lds = sums > operand ? sums : operand;
+    if (DT != kLaidOut) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFusedLds));
+    kernel<<<(unsigned)(a.b_tiles * (int64_t)a.splits), p.waves * 64, lds, s>>>(a, rows);
     return (int)hipGetLastError();
 }
 
-template <int FA, int FB>
-static int run_way(const F8Call &a, const F8Shape &p, void *stream)
+template <int FA, int FB, int WAY, bool BAND>
+static int run_band(const F8Call &a, const F8Shape &p, hipStream_t s)
 {
-    return a.dtype == NOVA_F32 ? run<FA, FB, F8_FULL>(a, p, (hipStream_t)stream) : run<FA, FB, F8_NARROW>(a, p, (hipStream_t)stream);
+    if (p.kind == 2) {
+        if constexpr (WAY == F8_NARROW) return run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY, BAND>(a, s);
+    }
+    if (p.kind >= 1) return run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY, BAND>(a, s);
+    if (p.mt == 1) return run_rows<1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+    if (p.mt == 2) return run_rows<2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+    return run_rows<4, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+}
+
+template <int FA, int FB>
+static int run(const F8Call &a, const F8Shape &p, hipStream_t s)
+{
+    const bool band = a.b_shift > 0;
+    if (a.dtype == NOVA_F32) return band ? run_band<FA, FB, F8_FULL, true>(a, p, s) : run_band<FA, FB, F8_FULL, false>(a, p, s);
+    return band ? run_band<FA, FB, F8_NARROW, true>(a, p, s) : run_band<FA, FB, F8_NARROW, false>(a, p, s);
+}
+
+static int join(const F8Call &a, hipStream_t s)
+{
+    if (a.splits == 1) return 0;
+    const size_t blocks = ((size_t)a.M * ((a.N + 3) / 4) + 255) / 256;
+    f8_join_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(a);
+    return (int)hipGetLastError();
+}
+
+static F8Call make_call(const F8Operand &a, const F8Operand &b, const F8Shape &p, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace)
+{
+    const F8Layout &la = a.layout, &lb = b.layout;
+    return {(const char *)a.q, (const char *)b.q, (const float *)((const char *)a.q + la.code_bytes), (const float *)((const char *)b.q + lb.code_bytes), bias, out,
+            (float *)workspace, ldout, la.rows, lb.rows, la.chunks, p.splits, p.split_chunks, la.row_tiles, lb.row_tiles, la.scale_pitch, lb.scale_pitch,
+            la.block == 1 ? 0 : 7, lb.block == 1 ? 0 : 7, dtype, flags};
 }
 
 int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream)
 {
-    const F8Layout &la = a.layout, &lb = b.layout;
-    const F8Shape p = f8_shape(la.rows, lb.rows, la.columns, dtype == NOVA_F32);
-    const F8Call call = {(const char *)a.q, (const char *)b.q, (const float *)((const char *)a.q + la.code_bytes), (const float *)((const char *)b.q + lb.code_bytes),
-                         bias, out, (float *)workspace, ldout, la.rows, lb.rows, la.chunks, p.splits, p.split_chunks, la.row_tiles, lb.row_tiles, la.scale_pitch,
-                         lb.scale_pitch, la.block == 1 ? 0 : 7, lb.block == 1 ? 0 : 7, dtype, flags};
-    if (a.format == NOVA_F8_E4M3)
-        return b.format == NOVA_F8_E4M3 ? run_way<NOVA_F8_E4M3, NOVA_F8_E4M3>(call, p, stream) : run_way<NOVA_F8_E4M3, NOVA_F8_E5M2>(call, p, stream);
-    return b.format == NOVA_F8_E4M3 ? run_way<NOVA_F8_E5M2, NOVA_F8_E4M3>(call, p, stream) : run_way<NOVA_F8_E5M2, NOVA_F8_E5M2>(call, p, stream);
+    const F8Shape p = f8_shape(a.layout.rows, b.layout.rows, a.layout.columns, dtype == NOVA_F32);
+    const F8Call call = make_call(a, b, p, bias, out, ldout, dtype, flags, workspace);
+    hipStream_t s = (hipStream_t)stream;
+    const int err = a.format == NOVA_F8_E4M3 ? b.format == NOVA_F8_E4M3 ? run<NOVA_F8_E4M3, NOVA_F8_E4M3>(call, p, s) : run<NOVA_F8_E4M3, NOVA_F8_E5M2>(call, p, s)
+                    : b.format == NOVA_F8_E4M3 ? run<NOVA_F8_E5M2, NOVA_F8_E4M3>(call, p, s)
+                                               : run<NOVA_F8_E5M2, NOVA_F8_E5M2>(call, p, s);
+    return err ? err : join(call, s);
+}
+
+// The layer y = Q(x) W^T: x is quantised into `a` (a layout in the caller's workspace), or on the way
+int launch_f8_linear(const F8Source &x, const F8Operand &a, const F8Operand &w, const void *bias, void *y, int64_t ldy, int flags, void *workspace, void *stream)
+{
+    const F8Shape p = f8_shape(x.rows, w.layout.rows, x.columns, x.dtype == NOVA_F32);
+    if (p.kind == 0 && p.mt == 1 && (size_t)x.rows * p.split_chunks * kF8Chunk <= kFusedElements) {
+        const F8Call call = make_call(a, w, p, bias, y, ldy, x.dtype, flags, workspace);
+        const F8RowsOf rows = {x.x, x.ld, x.columns};
+        hipStream_t s = (hipStream_t)stream;
+        const int err = x.dtype == NOVA_F32   ? run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_FULL, true, NOVA_F32>(call, rows, p, s)
+                        : x.dtype == NOVA_F16 ? run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_F16>(call, rows, p, s)
+                                              : run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_BF16>(call, rows, p, s);
+        return err ? err : join(call, s);
+    }
+    if (int err = launch_f8_quantize(x, a.layout, a.format, 0, const_cast<void *>(a.q), stream)) return err;
+    return launch_f8_matmul(a, w, bias, y, ldy, x.dtype, flags, workspace, stream);
 }
 
 }  // namespace nova

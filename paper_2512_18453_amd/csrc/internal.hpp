@@ -243,6 +243,7 @@ int launch_f8_zero(void *out, int64_t ld, int rows, int columns, int dtype, void
 struct F8Operand { const void *q; F8Layout layout; int format; };
 size_t f8_matmul_workspace(int M, int N, int K, int dtype);
 int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream);
+int launch_f8_linear(const F8Source &x, const F8Operand &a, const F8Operand &w, const void *bias, void *y, int64_t ldy, int flags, void *workspace, void *stream);
 // Dropout: the forward call and its gradient
 struct DropoutArgs {
     const void *x; int64_t ldx; const void *residual; int64_t ldresidual; const void *gate; int64_t ldgate; void *y; int64_t ldy;
