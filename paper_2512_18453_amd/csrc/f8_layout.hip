@@ -29,6 +29,50 @@ __device__ __forceinline__ void write_panels(const uint4v *staged, char *q, cons
     }
 }
 
+// A scale per row and chunk, and nothing but the rows' layout: a panel is one wave's
+template <int DT, int FORMAT>
+__global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const F8Quantize a)
+{
+    typedef Storage<DT> T;
+    __shared__ uint4v staged[4][kF8PanelBytes / 16];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, j = lane % 16, g = lane / 16;
+    const F8Layout &q = a.rows_layout;
+    const size_t panels = (size_t)q.row_tiles * q.chunks;
+    for (size_t panel = (size_t)blockIdx.x * 4 + wave; panel < panels; panel += (size_t)gridDim.x * 4) {
+        const int chunk = (int)(panel % q.chunks);
+        const int64_t row = (int64_t)(panel / q.chunks) * kF8Rows + g;
+        const int64_t column = (int64_t)chunk * kF8Chunk + 8 * j;
+        const int count = (int)min((int64_t)8, max((int64_t)0, a.src.columns - column));
+        Eight<T> x[4], gate[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int here = row + 4 * k < a.src.rows ? count : 0;
+            x[k] = load_eight((const T *)a.src.x + (row + 4 * k) * a.src.ld + column, here, here > 0 && column >= 8);
+            if (a.src.gate) gate[k] = load_eight((const T *)a.src.gate + (row + 4 * k) * a.src.ldgate + column, here, here > 0 && column >= 8);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[8];
+            unsigned m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = a.src.gate && !((float)gate[k].v[e] > 0.0f) ? 0.0f : (float)x[k].v[e];
+                m = max(m, magnitude(v[e]));
+            }
+            const float s = scale_of<FORMAT>(largest_of_16(m));
+            unsigned words[2];
+            F8Encoder<FORMAT>(s).encode(v, words);
+            __builtin_memcpy((uint64_t *)staged[wave] + (j / 2 % 2 * 1024 + (j / 4 * 16 + 4 * k + g) * 16 + j % 2 * 8) / 8, words, 8);
+            if (j == 0) f8_scales(a.rows_q, q)[(size_t)chunk * q.scale_pitch + row + 4 * k] = s;
+        }
+        exchange_in_wave();
+        uint4v *const to = (uint4v *)(a.rows_q + panel * kF8PanelBytes);
+        to[lane] = staged[wave][lane];
+        to[lane + 64] = staged[wave][lane + 64];
+        exchange_in_wave();
+    }
+}
+
 // BLOCK: 1 or 128, of whichever layouts there are
 template <int DT, int FORMAT, int BLOCK>
 __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
@@ -104,13 +148,9 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
                     if (j == 0 && row + k < a.rows_layout.scale_pitch)
                         f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + row + k] = s;
                 }
-                const F8Quotient<FORMAT> quotient(s);
-                float q[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = quotient(v[k][e]);
-                unsigned *at = (unsigned *)staged + (g / 2 * kF8PanelBytes + j / 2 % 2 * 1024 + (j / 4 * 16 + g % 2 * 8 + k) * 16 + j % 2 * 8) / 4;
-                at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
-                at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);
+                unsigned words[2];
+                F8Encoder<FORMAT>(s).encode(v[k], words);
+                __builtin_memcpy((uint64_t *)staged + (g / 2 * kF8PanelBytes + j / 2 % 2 * 1024 + (j / 4 * 16 + g % 2 * 8 + k) * 16 + j % 2 * 8) / 8, words, 8);
             }
             if (BLOCK > 1 && t == 0) f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + tile_row] = whole;
             __syncthreads();
@@ -127,13 +167,10 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
                     if (g == 0 && column + e < a.columns_layout.scale_pitch)
                         f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + column + e] = s;
                 }
-                const F8Quotient<FORMAT> quotient(s);
-                float q[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) q[k] = quotient(v[k][e]);
-                unsigned *at = (unsigned *)staged + (j / 2 * kF8PanelBytes + g / 2 % 2 * 1024 + (g / 4 * 16 + j % 2 * 8 + e) * 16 + g % 2 * 8) / 4;
-                at[0] = f8_codes<FORMAT>(q[0], q[1], q[2], q[3]);
-                at[1] = f8_codes<FORMAT>(q[4], q[5], q[6], q[7]);
+                const float column_values[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+                unsigned words[2];
+                F8Encoder<FORMAT>(s).encode(column_values, words);
+                __builtin_memcpy((uint64_t *)staged + (j / 2 * kF8PanelBytes + g / 2 % 2 * 1024 + (g / 4 * 16 + j % 2 * 8 + e) * 16 + g % 2 * 8) / 8, words, 8);
             }
             if (BLOCK > 1 && t == 0) f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + tile_column] = whole;
             __syncthreads();
@@ -215,7 +252,10 @@ template <int DT, int FORMAT>
 static void run_quantize(const F8Quantize &a, int block, hipStream_t s)
 {
     const unsigned blocks = (unsigned)(a.tiles < (1 << 22) ? a.tiles : 1 << 22);
-    if (block == 1) f8_quantize_kernel<DT, FORMAT, 1><<<blocks, 256, 0, s>>>(a);
+    if (block == 1 && a.rows_q && !a.columns_q && !a.partial) {
+        const size_t wanted = ((size_t)a.rows_layout.row_tiles * a.rows_layout.chunks + 3) / 4;
+        f8_quantize_rows_kernel<DT, FORMAT><<<(unsigned)(wanted < (1 << 22) ? wanted : 1 << 22), 256, 0, s>>>(a);
+    } else if (block == 1) f8_quantize_kernel<DT, FORMAT, 1><<<blocks, 256, 0, s>>>(a);
     else f8_quantize_kernel<DT, FORMAT, 128><<<blocks, 256, 0, s>>>(a);
 }
 

@@ -165,13 +165,12 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
 #pragma unroll
             for (int e = 0; e < 8; ++e) largest = max(largest, magnitude((float)x.v[e]));
             const float scale = scale_of<FA>(largest_of_16(largest));
-            const F8Quotient<FA> quotient(scale);
-            float q[8];
+            float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = quotient((float)x.v[e]);
-            unsigned *const to = (unsigned *)(lds + (size_t)at * kF8Chunk + lane % 16 * 8);
-            to[0] = f8_codes<FA>(q[0], q[1], q[2], q[3]);
-            to[1] = f8_codes<FA>(q[4], q[5], q[6], q[7]);
+            for (int e = 0; e < 8; ++e) v[e] = (float)x.v[e];
+            unsigned words[2];
+            F8Encoder<FA>(scale).encode(v, words);
+            __builtin_memcpy(__builtin_assume_aligned(lds + (size_t)at * kF8Chunk + lane % 16 * 8, 8), words, 8);
             if (lane % 16 == 0) scales_in_lds[at] = scale;
         }
         __syncthreads();
