@@ -76,53 +76,68 @@ struct F8Columns {
     }
 };
 
-// f(columns) with the columns n .. of the result, or of a piece of a cut sum
-template <int COUNT, typename F>
-__device__ __forceinline__ void with_columns(const F8Call &a, int split, int n, F &&f)
+// f(element of the results' type, where they go, elements from row to row, bias, flags): of the result, or of a piece of a cut sum
+template <typename F>
+__device__ __forceinline__ void with_results(const F8Call &a, int split, F &&f)
 {
-    if (a.splits > 1) f(F8Columns<float, COUNT>(a.partial + (size_t)split * a.M * a.N, a.N, nullptr, 0, a.N, n));
-    else if (a.dtype == NOVA_F32) f(F8Columns<float, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
-    else if (a.dtype == NOVA_F16) f(F8Columns<f16, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
-    else f(F8Columns<bf16, COUNT>(a.out, a.ldout, a.bias, a.flags, a.N, n));
+    if (a.splits > 1) f(0.0f, a.partial + (size_t)split * a.M * a.N, (int64_t)a.N, nullptr, 0);
+    else if (a.dtype == NOVA_F32) f(0.0f, a.out, a.ldout, a.bias, a.flags);
+    else if (a.dtype == NOVA_F16) f((f16)0.0f, a.out, a.ldout, a.bias, a.flags);
+    else f((bf16)0.0f, a.out, a.ldout, a.bias, a.flags);
+}
+
+// Four results of a row
+__device__ __forceinline__ void write_four(const F8Call &a, int split, int64_t m, int n, const float (&four)[4])
+{
+    if (m < a.M && n < a.N)
+        with_results(a, split, [&](auto element, void *out, int64_t ld, const void *bias, int flags) __attribute__((always_inline)) {
+            F8Columns<decltype(element), 4>(out, ld, bias, flags, a.N, n).write(m, four);
+        });
 }
 
 // ---- up to 64 rows ----
 //
-// Bound by B's bytes.  A workgroup makes 16 columns for all rows; its waves take the chunks of those columns in turn, load B's panels straight into registers, AHEAD - 1 ahead, and
+// Bound by B's bytes.  A workgroup makes 16 NT columns for all rows; its waves take the chunks of those columns in turn, load B's panels straight into registers, AHEAD - 1 ahead, and
 // add up through LDS in the order of their numbers.  A's panels come the same way from L2; or, with few rows, every workgroup quantises x by itself first, into LDS,
 // which saves the launch that would do it.
 constexpr int kLaidOut = -1;
 struct F8RowsOf { const void *x; int64_t ld; int K; };           // what A is quantised from
 constexpr size_t kFusedElements = 32768, kFusedLds = 128 * 1024;
 
-// MT panels of rows; DT: kLaidOut, or the type of x
-template <int MT, int FA, int FB, int WAY, bool BAND, int DT>
+// MT panels of rows, NT of columns; DT: kLaidOut, or the type of x
+template <int MT, int NT, int FA, int FB, int WAY, bool BAND, int DT>
 __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8RowsOf rows)
 {
     constexpr bool FUSED = DT != kLaidOut;
     constexpr int AHEAD = MT == 4 ? 2 : MT == 2 ? 3 : 4;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, i = lane % 16, b = lane / 16;
-    const int tile = blockIdx.x % a.b_tiles, split = blockIdx.x / a.b_tiles;
+    const int across = (a.b_tiles + NT - 1) / NT, tile = (int)(blockIdx.x % across) * NT, split = blockIdx.x / across;
     const int first = split * a.split_chunks, count = min(a.chunks - first, a.split_chunks);
     const int steps = count > wave ? (count - wave + waves - 1) / waves : 0;
-    const char *const panels = a.b + ((size_t)tile * a.chunks + first) * kF8PanelBytes;
+    const char *panels[NT];
+#pragma unroll
+    for (int y = 0; y < NT; ++y) panels[y] = a.b + ((size_t)min(tile + y, a.b_tiles - 1) * a.chunks + first) * kF8PanelBytes;          // (past the last: computed and not stored)
     float *const scales_in_lds = (float *)(lds + (size_t)count * a.M * kF8Chunk);
 
     struct Stage {
-        F8Fragment b, a[FUSED ? 1 : MT];
-        float4v b_scale;
+        F8Fragment b[NT], a[FUSED ? 1 : MT];
+        float4v b_scale[NT];
         float a_scale[MT];
     };
     auto load = [&](int step, Stage &s) __attribute__((always_inline)) {
         // (past the last: the last once more, and not multiplied, so that no load is in a branch)
         const int c = wave + min(step, steps - 1) * waves;
-        const char *const at = panels + (size_t)c * kF8PanelBytes + lane * 16u;
-        s.b.half[0] = __builtin_nontemporal_load((const uint4v *)at);
-        s.b.half[1] = __builtin_nontemporal_load((const uint4v *)(at + 1024));
         const float *const sb = a.b_scales + (size_t)(first + c) * a.b_pitch;
-        if constexpr (BAND) s.b_scale[0] = sb[(tile * 16) >> a.b_shift];
-        else s.b_scale = *(const float4v *)(sb + tile * 16 + 4 * b);
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+            const char *const at = panels[y] + (size_t)c * kF8PanelBytes + lane * 16u;
+            s.b[y].half[0] = __builtin_nontemporal_load((const uint4v *)at);
+            s.b[y].half[1] = __builtin_nontemporal_load((const uint4v *)(at + 1024));
+            const int t = min(tile + y, a.b_tiles - 1);
+            if constexpr (BAND) s.b_scale[y][0] = sb[(t * 16) >> a.b_shift];
+            else s.b_scale[y] = *(const float4v *)(sb + t * 16 + 4 * b);
+        }
         if constexpr (!FUSED) {
 #pragma unroll
             for (int x = 0; x < MT; ++x) {
@@ -132,9 +147,11 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
             }
         }
     };
-    float4v sum[MT];
+    float4v sum[NT][MT];
 #pragma unroll
-    for (int x = 0; x < MT; ++x) sum[x] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int x = 0; x < MT; ++x) sum[y][x] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     auto multiply = [&](int step, Stage &s) __attribute__((always_inline)) {
         if constexpr (FUSED) {
             const int at = (wave + step * waves) * a.M + min(i, a.M - 1);
@@ -142,15 +159,19 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
             s.a[0].half[1] = *(const uint4v *)(lds + (size_t)at * kF8Chunk + b * 32 + 16);
             s.a_scale[0] = scales_in_lds[at];
         }
-        F8Input<FB, WAY> fb;
-        fb.set(s.b);
+        F8Input<FB, WAY> fb[NT];
+#pragma unroll
+        for (int y = 0; y < NT; ++y) fb[y].set(s.b[y]);
 #pragma unroll
         for (int x = 0; x < MT; ++x) {
             F8Input<FA, WAY> fa;
             fa.set(s.a[x]);
-            const float4v p = f8_products<FB, FA, WAY>(fb, fa);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sum[x][v] = fma32(s.a_scale[x] * s.b_scale[BAND ? 0 : v], p[v], sum[x][v]);
+            for (int y = 0; y < NT; ++y) {
+                const float4v p = f8_products<FB, FA, WAY>(fb[y], fa);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sum[y][x][v] = fma32(s.a_scale[x] * s.b_scale[y][BAND ? 0 : v], p[v], sum[y][x][v]);
+            }
         }
     };
 
@@ -184,17 +205,19 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
     if constexpr (FUSED) __syncthreads();
     float4v *const sums = (float4v *)lds;
 #pragma unroll
-    for (int x = 0; x < MT; ++x) sums[(wave * MT + x) * 64 + lane] = sum[x];
+    for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int x = 0; x < MT; ++x) sums[((wave * NT + y) * MT + x) * 64 + lane] = sum[y][x];
     __syncthreads();
-    for (int e = threadIdx.x; e < MT * 64; e += blockDim.x) {
+    for (int e = threadIdx.x; e < NT * MT * 64; e += blockDim.x) {
         float four[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int w = 0; w < waves; ++w) {
-            const float4v part = sums[w * MT * 64 + e];
+            const float4v part = sums[w * NT * MT * 64 + e];
 #pragma unroll
             for (int v = 0; v < 4; ++v) four[v] += part[v];
         }
-        const int m = e / 64 * 16 + i, n = tile * 16 + 4 * b;
-        if (m < a.M && n < a.N) with_columns<4>(a, split, n, [&](const auto &columns) __attribute__((always_inline)) { columns.write(m, four); });
+        const int m = e / 64 % MT * 16 + i, n = (tile + e / 64 / MT) * 16 + 4 * b;
+        write_four(a, split, m, n, four);
     }
 }
 
@@ -210,9 +233,10 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
 template <int WM_, int WN_, int MT_, int NT_>
 struct F8Tile {
     static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, WAVES = WM * WN, THREADS = WAVES * 64, A = WM * MT, B = WN * NT;        // panels
+    static constexpr int PER_WAVE = (A + B) / WAVES, SCALE_LOADS = (A + B) / 4;                                                         // panels; 64 scales each
     static constexpr int PANELS = (A + B) * kF8PanelBytes, STAGE = PANELS + (A + B) * kF8Rows * 4, PITCH = NT * 64 + 16;
     static constexpr int LDS = 2 * STAGE > WAVES * 32 * PITCH ? 2 * STAGE : WAVES * 32 * PITCH;                                         // 32 rows of each wave's results
-    static_assert(A % 4 == 0 && A + B == 4 * WAVES, "a wave loads four panels of one operand, and 64 scales");
+    static_assert(A % 4 == 0 && (A + B) % 4 == 0 && PER_WAVE * WAVES == A + B && PER_WAVE % 2 == 0 && A % PER_WAVE == 0 && SCALE_LOADS <= WAVES, "what a wave loads is of one operand");
 };
 
 // 64 words of 4 bytes, as global_to_lds16 takes 16
@@ -238,27 +262,28 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
     const int m_tile = (int)(first_row + in_group % together) * Shape::A, n_tile = (int)(in_group / together) * Shape::B;
     const int first = split * a.split_chunks, count = min(a.chunks - first, a.split_chunks);
 
-    // what this wave loads: panels 4 wave .. of A's and then B's, the scales of 64 rows
-    const bool of_a = 4 * wave < Shape::A;
-    const int panel0 = of_a ? m_tile + 4 * wave : n_tile + 4 * wave - Shape::A, last = (of_a ? a.a_tiles : a.b_tiles) - 1;
-    const char *panel[4];
+    // what this wave loads: PW panels of A's and then B's, and of the scales of A's and then B's rows, 64 by 64, one piece (or none)
+    constexpr int PW = Shape::PER_WAVE;
+    const bool of_a = PW * wave < Shape::A, scales_of_a = 4 * wave < Shape::A;
+    const int panel0 = of_a ? m_tile + PW * wave : n_tile + PW * wave - Shape::A, last = (of_a ? a.a_tiles : a.b_tiles) - 1;
+    const char *panel[PW];
 #pragma unroll
-    for (int p = 0; p < 4; ++p)                                                              // (past the last: computed and not stored)
+    for (int p = 0; p < PW; ++p)                                                             // (past the last: computed and not stored)
         panel[p] = uniform_pointer((of_a ? a.a : a.b) + ((size_t)min(panel0 + p, last) * a.chunks + first) * kF8PanelBytes);
-    const int pitch = of_a ? a.a_pitch : a.b_pitch;
-    const char *scales = uniform_pointer((const char *)((of_a ? a.a_scales : a.b_scales) + (size_t)first * pitch));
-    const unsigned scale_at = (unsigned)min((panel0 * 16 + lane) >> (of_a ? a.a_shift : a.b_shift), pitch - 1) * 4u;
+    const int pitch = scales_of_a ? a.a_pitch : a.b_pitch, row0 = (scales_of_a ? m_tile + 4 * wave : n_tile + 4 * wave - Shape::A) * 16;
+    const char *scales = uniform_pointer((const char *)((scales_of_a ? a.a_scales : a.b_scales) + (size_t)first * pitch));
+    const unsigned scale_at = (unsigned)min((row0 + lane) >> (scales_of_a ? a.a_shift : a.b_shift), pitch - 1) * 4u;
     const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(size_t)((__attribute__((address_space(3))) const void *)lds));
     auto issue = [&](int stage) __attribute__((always_inline)) {
         const unsigned at = lds0 + (unsigned)(stage * STAGE);
 #pragma unroll
-        for (int p = 0; p < 4; p += 2) {
+        for (int p = 0; p < PW; p += 2) {
             const void *planes[4] = {panel[p], panel[p] + 1024, panel[p + 1], panel[p + 1] + 1024};
-            global_to_lds16_run<4, 1024>(planes, lane * 16u, at + (unsigned)((4 * wave + p) * kF8PanelBytes));
+            global_to_lds16_run<4, 1024>(planes, lane * 16u, at + (unsigned)((PW * wave + p) * kF8PanelBytes));
         }
-        global_to_lds4(scales, scale_at, at + (unsigned)(Shape::PANELS + wave * 256));
+        if (Shape::SCALE_LOADS == Shape::WAVES || wave < Shape::SCALE_LOADS) global_to_lds4(scales, scale_at, at + (unsigned)(Shape::PANELS + wave * 256));
 #pragma unroll
-        for (int p = 0; p < 4; ++p) panel[p] += kF8PanelBytes;
+        for (int p = 0; p < PW; ++p) panel[p] += kF8PanelBytes;
         scales += (size_t)pitch * 4;
     };
 
@@ -327,12 +352,15 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
     }
     // Results leave as rows: a lane holds four columns of one row, and 16 rows side by side would go to memory as pieces of 32 bytes (8192 x 8192 results of one chunk
     // 69.3 us).  So a wave passes them through LDS, 32 rows at a time, and writes a row of its tile as a whole.
-    constexpr int PITCH = Shape::PITCH, LANES = NT * 2;                                   // bytes of a row; lanes that write one, eight columns each
+    constexpr int PITCH = Shape::PITCH;                          // bytes of a row
     static_assert(MT % 2 == 0, "rows in pairs of panels");
     __syncthreads();                                             // everyone has read the last stage
     char *const own = lds + wave * 32 * PITCH;
-    const int n = (n_tile + wn * NT) * 16 + lane % LANES * 8;
-    with_columns<8>(a, (int)split, n, [&](const auto &columns) __attribute__((always_inline)) {
+    with_results(a, (int)split, [&](auto element, void *out, int64_t ld, const void *bias, int flags) __attribute__((always_inline)) {
+        typedef decltype(element) T;
+        constexpr int COUNT = 16 / sizeof(T), LANES = NT * 16 / COUNT;                       // columns of a lane; lanes that write a row
+        const int n = (n_tile + wn * NT) * 16 + lane % LANES * COUNT;
+        const F8Columns<T, COUNT> columns(out, ld, bias, flags, a.N, n);
         static_for<MT / 2>([&](auto X) __attribute__((always_inline)) {
             constexpr int x = 2 * X;
 #pragma unroll
@@ -344,10 +372,14 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
             for (int k = 0; k < 32 * LANES / 64; ++k) {
                 const int r = lane / LANES + k * (64 / LANES);
                 const int64_t m = (int64_t)(m_tile + wm * MT + x) * 16 + r;
-                const float4v *from = (const float4v *)(own + r * PITCH + lane % LANES * 32);
-                const float4v low = from[0], high = from[1];
-                const float eight[8] = {low[0], low[1], low[2], low[3], high[0], high[1], high[2], high[3]};
-                if (m < a.M && n < a.N) columns.write(m, eight);
+                float results[COUNT];
+#pragma unroll
+                for (int q = 0; q < COUNT; q += 4) {
+                    const float4v four = *(const float4v *)(own + r * PITCH + (lane % LANES * COUNT + q) * 4);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) results[q + v] = four[v];
+                }
+                if (m < a.M && n < a.N) columns.write(m, results);
             }
             exchange_in_wave();
         });
@@ -367,11 +399,11 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8Call a)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 if (n + v < a.N) sum[v] += a.partial[((size_t)split * a.M + m) * a.N + n + v];
-        with_columns<4>(a, 0, n, [&](const auto &columns) __attribute__((always_inline)) { columns.write(m, sum); });
+        write_four(a, 0, m, n, sum);
     }
 }
 
-struct F8Shape { int kind, mt, waves, splits, split_chunks; };           // kind: 0 up to 64 rows, 1 tiles of 128 x 128, 2 of 256 x 256
+struct F8Shape { int kind, mt, nt, waves, splits, split_chunks; };           // kind: 0 up to 64 rows, 1 tiles of 128 x 128, 2 of 256 x 256
 
 static F8Shape f8_shape(int M, int N, int K, bool full)
 {
@@ -381,15 +413,28 @@ static F8Shape f8_shape(int M, int N, int K, bool full)
     p.splits = 1;
     if (M <= 64) {
         p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-        // a column tile is one workgroup's; fewer than the chip holds, of long sums, are cut
+        // More than 16 rows and 32 MB of weights: two panels of columns share the rows that a wave loads (32 rows by 25088 x 4096 32.8 -> 29.9 us, 64 by 4096 x 25088
+        // 47 -> 40; 32 by 4096 x 4096, where workgroups count for more, 11.0 -> 12.1).  Fewer workgroups than compute units, of long sums, are cut.  A workgroup is
+        // four waves (1 row by 4096 x 25088 19.5 us, with eight 21.0), eight where it has a compute unit for itself (1 by 25088 x 4096 22.1, with four 24.1).
         const int64_t panels = (N + 15) / 16;
-        while (panels * p.splits * 2 <= 512 && p.splits < 64 && chunks / (p.splits * 2) >= 32) p.splits *= 2;
+        p.nt = p.mt > 1 && panels * chunks >= 16384 ? 2 : 1;
+        const int64_t groups = (panels + p.nt - 1) / p.nt;
+        while (groups * p.splits * 2 <= 256 && p.splits < 64 && chunks / (p.splits * 2) >= 32) p.splits *= 2;
         p.split_chunks = ceil_div(chunks, p.splits);
-        p.waves = p.split_chunks >= 8 ? 8 : p.split_chunks >= 4 ? 4 : p.split_chunks;
+        p.waves = p.mt == 1 && groups * p.splits <= 256 && p.split_chunks >= 8 ? 8 : p.split_chunks >= 4 ? 4 : p.split_chunks;
     } else {
-        p.kind = full || tiles(256) < 192 ? 1 : 2;
-        const int64_t blocks = tiles(p.kind == 1 ? 128 : 256);
-        while (blocks * p.splits * 2 <= 384 && p.splits < 16 && p.splits * 8 <= chunks) p.splits *= 2;
+        // An estimate in us of each way.  128 x 128: one or two workgroups per compute unit, so a chunk of one or both; 256 x 256: one.  (From 1024 x 4096 x 4096 and
+        // 8192 x 8192 x 8192, with 128 columns of B per scale.)  A cut sum's pieces are written and read, and another kernel joins them.
+        double least = 0;
+        for (int kind = 1; kind <= (full ? 1 : 2); ++kind)
+            for (int splits = 1; splits <= 16 && splits <= chunks; ++splits) {
+                const int k = ceil_div(chunks, splits);
+                const int64_t blocks = tiles(kind == 1 ? 128 : 256) * splits, together = kind == 1 ? 512 : 256, rounds = blocks / together, rest = blocks % together;
+                const double round = kind == 1 ? k * (full ? 1.72 : 1.0) + 5 : k * 1.5 + 7;
+                const double part = kind == 1 && rest <= 256 ? k * (full ? 1.2 : 0.65) + 4 : round;
+                const double time = rounds * round + (rest ? part : 0) + (splits > 1 ? 4 + 2e-6 * splits * M * N : 0);
+                if (least == 0 || time < least) least = time, p.kind = kind, p.splits = splits;
+            }
         p.split_chunks = ceil_div(chunks, p.splits);
     }
     p.splits = ceil_div(chunks, p.split_chunks);
@@ -422,14 +467,14 @@ static int run_tiles(const F8Call &a, hipStream_t s)
     return 0;
 }
 
-template <int MT, int FA, int FB, int WAY, bool BAND, int DT>
+template <int MT, int NT, int FA, int FB, int WAY, bool BAND, int DT>
 static int run_rows(const F8Call &a, const F8RowsOf &rows, const F8Shape &p, hipStream_t s)
 {
-    const auto kernel = f8_rows_kernel<MT, FA, FB, WAY, BAND, DT>;
-    const size_t sums = (size_t)p.waves * MT * 1024, operand = DT == kLaidOut ? 0 : (size_t)a.split_chunks * a.M * (kF8Chunk + 4);
+    const auto kernel = f8_rows_kernel<MT, NT, FA, FB, WAY, BAND, DT>;
+    const size_t sums = (size_t)p.waves * MT * NT * 1024, operand = DT == kLaidOut ? 0 : (size_t)a.split_chunks * a.M * (kF8Chunk + 4);
     const size_t lds = sums > operand ? sums : operand;
     if (DT != kLaidOut) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFusedLds));
-    kernel<<<(unsigned)(a.b_tiles * (int64_t)a.splits), p.waves * 64, lds, s>>>(a, rows);
+    kernel<<<(unsigned)((a.b_tiles + NT - 1) / NT * (int64_t)a.splits), p.waves * 64, lds, s>>>(a, rows);
     return (int)hipGetLastError();
 }
 
@@ -439,10 +484,11 @@ static int run_band(const F8Call &a, const F8Shape &p, hipStream_t s)
     if (p.kind == 2) {
         if constexpr (WAY == F8_NARROW) return run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY, BAND>(a, s);
     }
-    if (p.kind >= 1) return run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY, BAND>(a, s);
-    if (p.mt == 1) return run_rows<1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
-    if (p.mt == 2) return run_rows<2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
-    return run_rows<4, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+    // (eight waves hide more of each other's waits: 517 x 5001 x 2055 18.2 -> 14.9 us; as binary16, where each makes its operands, four)
+    if (p.kind >= 1) return run_tiles<std::conditional_t<WAY == F8_NARROW, F8Tile<2, 4, 4, 2>, F8Tile<2, 2, 4, 4>>, FA, FB, WAY, BAND>(a, s);
+    if (p.mt == 1) return run_rows<1, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+    if (p.mt == 2) return p.nt == 1 ? run_rows<2, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s) : run_rows<2, 2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
+    return p.nt == 1 ? run_rows<4, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s) : run_rows<4, 2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
 }
 
 template <int FA, int FB>
@@ -488,9 +534,9 @@ int launch_f8_linear(const F8Source &x, const F8Operand &a, const F8Operand &w, 
         const F8Call call = make_call(a, w, p, bias, y, ldy, x.dtype, flags, workspace);
         const F8RowsOf rows = {x.x, x.ld, x.columns};
         hipStream_t s = (hipStream_t)stream;
-        const int err = x.dtype == NOVA_F32   ? run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_FULL, true, NOVA_F32>(call, rows, p, s)
-                        : x.dtype == NOVA_F16 ? run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_F16>(call, rows, p, s)
-                                              : run_rows<1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_BF16>(call, rows, p, s);
+        const int err = x.dtype == NOVA_F32   ? run_rows<1, 1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_FULL, true, NOVA_F32>(call, rows, p, s)
+                        : x.dtype == NOVA_F16 ? run_rows<1, 1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_F16>(call, rows, p, s)
+                                              : run_rows<1, 1, NOVA_F8_E4M3, NOVA_F8_E4M3, F8_NARROW, true, NOVA_BF16>(call, rows, p, s);
         return err ? err : join(call, s);
     }
     if (int err = launch_f8_quantize(x, a.layout, a.format, 0, const_cast<void *>(a.q), stream)) return err;
