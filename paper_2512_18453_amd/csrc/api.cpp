@@ -688,16 +688,15 @@ extern "C" int nova_f8_linear_backward(const void *dy, int64_t lddy, const void 
     if (workspace_bytes < p.bytes) return NOVA_ENOSPC;
     char *const ws = (char *)workspace;
     const F8Source d = {dy, lddy, y, ldy, M, N, dtype};
-    if (int err = launch_f8_quantize_both(d, format, dx ? ws + p.d_at : nullptr, dw ? ws + p.d_transposed_at : nullptr, dbias, (float *)(ws + p.sums_at),
-                                          (flags & NOVA_FLAG_ADD) != 0, stream))
+    const F8Source xs = {x, ldx, nullptr, 0, M, K, dtype};
+    if (int err = launch_f8_quantize_backward(d, format, dx ? ws + p.d_at : nullptr, dw ? ws + p.d_transposed_at : nullptr, dbias, (float *)(ws + p.sums_at),
+                                              (flags & NOVA_FLAG_ADD) != 0, xs, dw ? ws + p.x_at : nullptr, stream))
         return hip_result(err);
     if (dx) {
         const F8Operand a = {ws + p.d_at, p.d, format};
         if (int err = launch_f8_matmul(a, w, nullptr, dx, lddx, dtype, 0, ws + p.products_at, stream)) return hip_result(err);
     }
     if (dw) {
-        const F8Source xs = {x, ldx, nullptr, 0, M, K, dtype};
-        if (int err = launch_f8_quantize(xs, p.x_transposed, NOVA_F8_E4M3, 1, ws + p.x_at, stream)) return hip_result(err);
         const F8Operand a = {ws + p.d_transposed_at, p.d_transposed, format}, b = {ws + p.x_at, p.x_transposed, NOVA_F8_E4M3};
         if (int err = launch_f8_matmul(a, b, nullptr, dw, lddw, dw_dtype, flags & NOVA_FLAG_ADD, ws + p.products_at, stream)) return hip_result(err);
     }

@@ -110,6 +110,12 @@ struct F8Encoder {
             words[w] = scale > 0.0f ? codes : 0;
         }
     }
+    // two, in 16 bits
+    __device__ __forceinline__ void encode(const float (&v)[2], uint16_t &half) const
+    {
+        const unsigned codes = f8_codes<FORMAT>(quotient(v[0]), quotient(v[1]), 0.0f, 0.0f);
+        half = scale > 0.0f ? (uint16_t)codes : 0;
+    }
 };
 
 // The largest value over the 16 lanes of a row of the wave

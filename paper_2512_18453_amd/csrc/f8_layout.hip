@@ -1,6 +1,6 @@
 // Matrices in 8-bit floating point: from rows of numbers to the layout that the products read (nova_f8_quantize in nova.h), from codes, and back.
 //
-// A workgroup takes 128 x 128 elements of the source, a thread 8 x 8 of them, and holds them in registers: what is largest in a row, a column or all of them
+// A workgroup takes 128 x 128 elements of the source (32 x 128 where there are no more rows), a thread 8 x 8 (2 x 8) of them, and holds them in registers: what is largest in a row, a column or all of them
 // is known before any is divided, and one read serves the layout of the rows, of the columns, and the columns' sums.  Codes go through LDS, where they are put
 // in the panels' order, so that memory sees whole 16-byte pieces side by side.
 #include "f8_common.hpp"
@@ -21,12 +21,19 @@ struct F8Quantize {
 
 __device__ __forceinline__ float *f8_scales(char *q, const F8Layout &layout) { return (float *)(q + layout.code_bytes); }
 
-// A tile's codes from LDS to the panels row_tile .. of a chunk
+// Where a 16-byte piece of a tile's panel lies in LDS: neighbours in the eight bytes that a wave's lanes write at a time are a panel, or 256 bytes, apart, and would all lie
+// in the same banks
+__device__ __forceinline__ int staged_piece(int panel, int piece) { return panel * 128 + (piece ^ ((piece / 16 ^ panel) & 7)); }
+
+// A tile's codes from LDS to the panels row_tile .. of a chunk, of which the first FILLED of four quarters hold codes
+template <int FILLED>
 __device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
 {
     for (int piece = threadIdx.x; piece < kTile * kTile / 16; piece += 256) {
-        const int r = row_tile + piece / 128;
-        if (r < layout.row_tiles) *(uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16) = staged[piece];
+        const int panel = piece / 128, r = row_tile + panel;
+        if (r < layout.row_tiles)
+            *(uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16) =
+                piece % 64 / 16 < FILLED ? staged[staged_piece(panel, piece % 128)] : uint4v{0, 0, 0, 0};
     }
 }
 
@@ -95,23 +102,30 @@ __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const F8Quantize 
     }
 }
 
-// BLOCK: 1 or 128.  WHAT: the rows' layout, the columns', or what there is of them and of the columns' sums, behind a gate if there is one
+// What a workgroup shares
+struct F8Shared {
+    uint4v staged[kTile * kTile / 16];
+    unsigned largest[4][kTile];
+    float sums[4][kTile];
+};
+
+// BLOCK: 1 or 128.  WHAT: the rows' layout, the columns', or what there is of them and of the columns' sums, behind a gate if there is one.  R: rows of a thread, 8, or
+// 2 where the source has at most 32 rows.  The workgroup is number `block` of `blocks`.
 enum { F8_ROWS, F8_COLUMNS, F8_GRADIENT };
-template <int DT, int FORMAT, int BLOCK, int WHAT>
-__global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
+template <int DT, int FORMAT, int BLOCK, int WHAT, int R>
+__device__ __forceinline__ void f8_quantize_tiles(const F8Quantize &a, unsigned block, unsigned blocks, F8Shared &shared)
 {
     typedef Storage<DT> T;
-    __shared__ uint4v staged[kTile * kTile / 16];
-    __shared__ unsigned largest[4][kTile];
-    __shared__ float sums[4][kTile];
+    static_assert(R == 8 || (R == 2 && BLOCK == 1), "rows of a thread");
     const bool rows = WHAT == F8_GRADIENT ? a.rows_q != nullptr : WHAT == F8_ROWS, columns = WHAT == F8_GRADIENT ? a.columns_q != nullptr : WHAT == F8_COLUMNS;
     const bool summed = WHAT == F8_GRADIENT && a.partial;
     const int t = threadIdx.x, j = t % 16, g = t / 16, wave = t / 64;
-    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    char *const staged = (char *)shared.staged;
+    for (int64_t tile = block; tile < a.tiles; tile += blocks) {
         const int tile_row = (int)(tile / a.tiles_across), tile_column = (int)(tile % a.tiles_across);
-        const int64_t row = (int64_t)tile_row * kTile + 8 * g, column = (int64_t)tile_column * kTile + 8 * j;
-        float v[8][8];
-        load_rows<T, 8, 1, WHAT == F8_GRADIENT>(a.src, row, column, v);
+        const int64_t row = (int64_t)tile_row * kTile + R * g, column = (int64_t)tile_column * kTile + 8 * j;
+        float v[R][8];
+        load_rows<T, R, 1, WHAT == F8_GRADIENT>(a.src, row, column, v);
 
         // the largest of each column, and with them of the tile
         __syncthreads();
@@ -120,10 +134,10 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
             for (int e = 0; e < 8; ++e) {
                 unsigned m = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) m = max(m, magnitude(v[k][e]));
+                for (int k = 0; k < R; ++k) m = max(m, magnitude(v[k][e]));
                 m = max(m, (unsigned)__shfl_xor((int)m, 16));
                 m = max(m, (unsigned)__shfl_xor((int)m, 32));
-                if (t % 64 < 16) largest[wave][8 * j + e] = m;
+                if (t % 64 < 16) shared.largest[wave][8 * j + e] = m;
             }
         }
         if (summed) {
@@ -131,15 +145,15 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
             for (int e = 0; e < 8; ++e) {
                 float s = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s += v[k][e];
+                for (int k = 0; k < R; ++k) s += v[k][e];
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
-                if (t % 64 < 16) sums[wave][8 * j + e] = s;
+                if (t % 64 < 16) shared.sums[wave][8 * j + e] = s;
             }
         }
         __syncthreads();
         if (summed && t < kTile && tile_column * (int64_t)kTile + t < a.src.columns) {
-            const float s = (sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]);
+            const float s = (shared.sums[0][t] + shared.sums[1][t]) + (shared.sums[2][t] + shared.sums[3][t]);
             float *const to = a.partial + (size_t)tile_row * a.src.columns + tile_column * kTile + t;
             *to = a.add ? (float)((double)*to + s) : s;
         }
@@ -149,13 +163,13 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) m = max(m, largest[w][8 * j + e]);
+                for (int w = 0; w < 4; ++w) m = max(m, shared.largest[w][8 * j + e]);
             whole = scale_of<FORMAT>(largest_of_16(m));
         }
 
         if (rows) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < R; ++k) {
                 float s = whole;
                 if constexpr (BLOCK == 1) {
                     unsigned m = 0;
@@ -167,33 +181,57 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
                 }
                 unsigned words[2];
                 F8Encoder<FORMAT>(s).encode(v[k], words);
-                __builtin_memcpy((uint64_t *)staged + (g / 2 * kF8PanelBytes + j / 2 % 2 * 1024 + (j / 4 * 16 + g % 2 * 8 + k) * 16 + j % 2 * 8) / 8, words, 8);
+                const int r = R * g + k, piece = j / 2 % 2 * 64 + j / 4 * 16 + r % 16;
+                *(uint64_t *)(staged + staged_piece(r / 16, piece) * 16 + j % 2 * 8) = (uint64_t)words[1] << 32 | words[0];
             }
             if (BLOCK > 1 && t == 0) f8_scales(a.rows_q, a.rows_layout)[(size_t)tile_column * a.rows_layout.scale_pitch + tile_row] = whole;
             __syncthreads();
-            write_panels(staged, a.rows_q, a.rows_layout, tile_row * (kTile / kF8Rows), tile_column);
+            write_panels<4>(shared.staged, a.rows_q, a.rows_layout, tile_row * (kTile / kF8Rows), tile_column);
             __syncthreads();
         }
         if (columns) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                const int n = 8 * j + e, first = R * g, piece = first / 16 % 2 * 64 + first / 32 * 16 + n % 16;
                 float s = whole;
                 if constexpr (BLOCK == 1) {
-                    const int n = 8 * j + e;
-                    s = scale_of<FORMAT>(max(max(largest[0][n], largest[1][n]), max(largest[2][n], largest[3][n])));
+                    s = scale_of<FORMAT>(max(max(shared.largest[0][n], shared.largest[1][n]), max(shared.largest[2][n], shared.largest[3][n])));
                     if (g == 0 && column + e < a.columns_layout.scale_pitch)
                         f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + column + e] = s;
                 }
-                const float column_values[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-                unsigned words[2];
-                F8Encoder<FORMAT>(s).encode(column_values, words);
-                __builtin_memcpy((uint64_t *)staged + (j / 2 * kF8PanelBytes + g / 2 % 2 * 1024 + (g / 4 * 16 + j % 2 * 8 + e) * 16 + g % 2 * 8) / 8, words, 8);
+                float of_column[R];
+#pragma unroll
+                for (int k = 0; k < R; ++k) of_column[k] = v[k][e];
+                char *const to = staged + staged_piece(n / 16, piece) * 16 + first % 16;
+                if constexpr (R == 8) {
+                    unsigned words[2];
+                    F8Encoder<FORMAT>(s).encode(of_column, words);
+                    *(uint64_t *)to = (uint64_t)words[1] << 32 | words[0];
+                } else {
+                    F8Encoder<FORMAT>(s).encode(of_column, *(uint16_t *)to);
+                }
             }
             if (BLOCK > 1 && t == 0) f8_scales(a.columns_q, a.columns_layout)[(size_t)tile_row * a.columns_layout.scale_pitch + tile_column] = whole;
             __syncthreads();
-            write_panels(staged, a.columns_q, a.columns_layout, tile_column * (kTile / kF8Rows), tile_row);
+            write_panels<R == 8 ? 4 : 1>(shared.staged, a.columns_q, a.columns_layout, tile_column * (kTile / kF8Rows), tile_row);
         }
     }
+}
+
+template <int DT, int FORMAT, int BLOCK, int WHAT, int R>
+__global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
+{
+    __shared__ F8Shared shared;
+    f8_quantize_tiles<DT, FORMAT, BLOCK, WHAT, R>(a, blockIdx.x, gridDim.x, shared);
+}
+
+// What a backward pass needs of the gradient, and of the layer's input, in one launch
+template <int DT, int FORMAT, int R>
+__global__ void __launch_bounds__(256, 3) f8_quantize_backward_kernel(const F8Quantize d, const F8Quantize x, unsigned d_blocks)
+{
+    __shared__ F8Shared shared;
+    if (blockIdx.x < d_blocks) f8_quantize_tiles<DT, FORMAT, 1, F8_GRADIENT, R>(d, blockIdx.x, d_blocks, shared);
+    else f8_quantize_tiles<DT, NOVA_F8_E4M3, 1, F8_COLUMNS, R>(x, blockIdx.x - d_blocks, gridDim.x - d_blocks, shared);
 }
 
 // out (+)= the pieces' sums, in their order
@@ -202,6 +240,7 @@ __global__ void __launch_bounds__(256) f8_sums_kernel(const float *__restrict__ 
     const int n = blockIdx.x * 256 + threadIdx.x;
     if (n >= columns) return;
     double s = add ? out[n] : 0.0;
+#pragma unroll 16
     for (int p = 0; p < pieces; ++p) s += partial[(size_t)p * columns + n];
     out[n] = (float)s;
 }
@@ -265,51 +304,78 @@ __global__ void __launch_bounds__(256) f8_unpack_kernel(const char *__restrict__
 
 static unsigned blocks_for(size_t threads) { return (unsigned)(threads > ((size_t)1 << 30) ? (1 << 22) : (threads + 255) / 256); }
 
-template <int DT, int FORMAT>
-static void run_quantize(const F8Quantize &a, int block, bool gradient, hipStream_t s)
+static void count_tiles(F8Quantize &a)
 {
-    const unsigned blocks = (unsigned)(a.tiles < (1 << 22) ? a.tiles : 1 << 22);
-    if (gradient) {
-        f8_quantize_kernel<DT, FORMAT, 1, F8_GRADIENT><<<blocks, 256, 0, s>>>(a);
-    } else if (block > 1) {
-        if (a.rows_q) f8_quantize_kernel<DT, FORMAT, 128, F8_ROWS><<<blocks, 256, 0, s>>>(a);
-        else f8_quantize_kernel<DT, FORMAT, 128, F8_COLUMNS><<<blocks, 256, 0, s>>>(a);
+    a.tiles_across = (int)(((int64_t)a.src.columns + kTile - 1) / kTile);
+    a.tiles = (int64_t)a.tiles_across * (((int64_t)a.src.rows + kTile - 1) / kTile);
+}
+static unsigned tile_blocks(const F8Quantize &a) { return (unsigned)(a.tiles < (1 << 21) ? a.tiles : 1 << 21); }
+constexpr int kFewRows = 32;
+
+template <int DT, int FORMAT>
+static void run_quantize(const F8Quantize &a, int block, hipStream_t s)
+{
+    const unsigned blocks = tile_blocks(a);
+    if (block > 1) {
+        if (a.rows_q) f8_quantize_kernel<DT, FORMAT, 128, F8_ROWS, 8><<<blocks, 256, 0, s>>>(a);
+        else f8_quantize_kernel<DT, FORMAT, 128, F8_COLUMNS, 8><<<blocks, 256, 0, s>>>(a);
     } else if (a.rows_q) {
         const size_t wanted = ((size_t)a.rows_layout.row_tiles * a.rows_layout.chunks + 3) / 4;
         f8_quantize_rows_kernel<DT, FORMAT><<<(unsigned)(wanted < (1 << 22) ? wanted : 1 << 22), 256, 0, s>>>(a);
+    } else if (a.src.rows <= kFewRows) {
+        f8_quantize_kernel<DT, FORMAT, 1, F8_COLUMNS, 2><<<blocks, 256, 0, s>>>(a);
     } else {
-        f8_quantize_kernel<DT, FORMAT, 1, F8_COLUMNS><<<blocks, 256, 0, s>>>(a);
+        f8_quantize_kernel<DT, FORMAT, 1, F8_COLUMNS, 8><<<blocks, 256, 0, s>>>(a);
     }
 }
 
-static int quantize(F8Quantize a, int format, int block, bool gradient, void *stream)
+template <int DT, int FORMAT>
+static void run_backward(const F8Quantize &d, const F8Quantize &x, hipStream_t s)
 {
-    hipStream_t s = (hipStream_t)stream;
-    a.tiles_across = (int)(((int64_t)a.src.columns + kTile - 1) / kTile);
-    a.tiles = (int64_t)a.tiles_across * (((int64_t)a.src.rows + kTile - 1) / kTile);
-    const bool e4m3 = format == NOVA_F8_E4M3;
-    if (a.src.dtype == NOVA_F32) e4m3 ? run_quantize<NOVA_F32, NOVA_F8_E4M3>(a, block, gradient, s) : run_quantize<NOVA_F32, NOVA_F8_E5M2>(a, block, gradient, s);
-    else if (a.src.dtype == NOVA_F16) e4m3 ? run_quantize<NOVA_F16, NOVA_F8_E4M3>(a, block, gradient, s) : run_quantize<NOVA_F16, NOVA_F8_E5M2>(a, block, gradient, s);
-    else e4m3 ? run_quantize<NOVA_BF16, NOVA_F8_E4M3>(a, block, gradient, s) : run_quantize<NOVA_BF16, NOVA_F8_E5M2>(a, block, gradient, s);
-    return (int)hipGetLastError();
+    const unsigned d_blocks = tile_blocks(d), blocks = d_blocks + (x.columns_q ? tile_blocks(x) : 0);
+    if (d.src.rows <= kFewRows) f8_quantize_backward_kernel<DT, FORMAT, 2><<<blocks, 256, 0, s>>>(d, x, d_blocks);
+    else f8_quantize_backward_kernel<DT, FORMAT, 8><<<blocks, 256, 0, s>>>(d, x, d_blocks);
+}
+
+// f(std::integral_constant of dtype, of format)
+template <typename F>
+static void by_type(int dtype, int format, F &&f)
+{
+    auto of_format = [&](auto dt) {
+        if (format == NOVA_F8_E4M3) f(dt, std::integral_constant<int, NOVA_F8_E4M3>{});
+        else f(dt, std::integral_constant<int, NOVA_F8_E5M2>{});
+    };
+    if (dtype == NOVA_F32) of_format(std::integral_constant<int, NOVA_F32>{});
+    else if (dtype == NOVA_F16) of_format(std::integral_constant<int, NOVA_F16>{});
+    else of_format(std::integral_constant<int, NOVA_BF16>{});
 }
 
 int launch_f8_quantize(const F8Source &x, const F8Layout &q, int format, int transposed, void *Xq, void *stream)
 {
     F8Quantize a = {x, nullptr, nullptr, nullptr, 0, q, q, 0, 0};
     (transposed ? a.columns_q : a.rows_q) = (char *)Xq;
-    return quantize(a, format, q.block, false, stream);
+    count_tiles(a);
+    by_type(x.dtype, format, [&](auto dt, auto f) { run_quantize<dt, f>(a, q.block, (hipStream_t)stream); });
+    return (int)hipGetLastError();
 }
 
-int launch_f8_quantize_both(const F8Source &x, int format, void *Xq, void *Xq_transposed, float *sums, float *partial, int add, void *stream)
+int launch_f8_quantize_backward(const F8Source &d, int format, void *dq, void *dq_transposed, float *sums, float *partial, int add, const F8Source &x,
+                                void *xq_transposed, void *stream)
 {
     // (up to 128 rows the sums are whole)
-    const bool whole = x.rows <= kTile;
-    const F8Quantize a = {x, (char *)Xq, (char *)Xq_transposed, !sums ? nullptr : whole ? sums : partial, whole && add, make_f8_layout(x.rows, x.columns, 1),
-                          make_f8_layout(x.columns, x.rows, 1), 0, 0};
-    if (int err = quantize(a, format, 1, true, stream)) return err;
+    const bool whole = d.rows <= kTile;
+    F8Quantize a = {d, (char *)dq, (char *)dq_transposed, !sums ? nullptr : whole ? sums : partial, whole && add, make_f8_layout(d.rows, d.columns, 1),
+                    make_f8_layout(d.columns, d.rows, 1), 0, 0};
+    F8Quantize b = {x, nullptr, (char *)xq_transposed, nullptr, 0, {}, {}, 0, 0};
+    count_tiles(a);
+    if (xq_transposed) {
+        b.columns_layout = make_f8_layout(x.columns, x.rows, 1);
+        count_tiles(b);
+    }
+    by_type(d.dtype, format, [&](auto dt, auto f) { run_backward<dt, f>(a, b, (hipStream_t)stream); });
+    NOVA_HIP_TRY(hipGetLastError());
     if (!sums || whole) return 0;
-    f8_sums_kernel<<<(x.columns + 255) / 256, 256, 0, (hipStream_t)stream>>>(partial, sums, a.columns_layout.chunks, x.columns, add);
+    f8_sums_kernel<<<(d.columns + 255) / 256, 256, 0, (hipStream_t)stream>>>(partial, sums, a.columns_layout.chunks, d.columns, add);
     return (int)hipGetLastError();
 }
 

@@ -473,7 +473,7 @@ static int run_rows(const F8Call &a, const F8RowsOf &rows, const F8Shape &p, hip
     const auto kernel = f8_rows_kernel<MT, NT, FA, FB, WAY, BAND, DT>;
     const size_t sums = (size_t)p.waves * MT * NT * 1024, operand = DT == kLaidOut ? 0 : (size_t)a.split_chunks * a.M * (kF8Chunk + 4);
     const size_t lds = sums > operand ? sums : operand;
-    if (DT != kLaidOut) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFusedLds));
+    if (lds > 64 * 1024) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFusedLds));
     kernel<<<(unsigned)((a.b_tiles + NT - 1) / NT * (int64_t)a.splits), p.waves * 64, lds, s>>>(a, rows);
     return (int)hipGetLastError();
 }

@@ -236,7 +236,8 @@ struct F8Source {
     int rows, columns, dtype;
 };
 int launch_f8_quantize(const F8Source &x, const F8Layout &q, int format, int transposed, void *Xq, void *stream);
-int launch_f8_quantize_both(const F8Source &x, int format, void *Xq, void *Xq_transposed, float *sums, float *partial, int add, void *stream);
+int launch_f8_quantize_backward(const F8Source &d, int format, void *dq, void *dq_transposed, float *sums, float *partial, int add, const F8Source &x,
+                                void *xq_transposed, void *stream);
 int launch_f8_pack(const uint8_t *codes, const float *scales, const F8Layout &q, int transposed, void *Xq, void *stream);
 int launch_f8_unpack(const void *Xq, const F8Layout &q, uint8_t *codes, float *scales, void *stream);
 int launch_f8_zero(void *out, int64_t ld, int rows, int columns, int dtype, void *stream);

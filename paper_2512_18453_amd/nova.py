@@ -637,9 +637,9 @@ def _f8_dtype(format):
 
 def _here(*tensors):
     """The library works on the current device."""
-    at = torch.cuda.current_device()
+    at = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != at:
+        if t is not None and t.get_device() != at and t.is_cuda:
             raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{at}")
 
 
