@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(256) f8_quantize_kernel(const F8Quantize a)
 
 // What a backward pass needs of the gradient, and of the layer's input, in one launch
 template <int DT, int FORMAT, int R>
-__global__ void __launch_bounds__(256, 3) f8_quantize_backward_kernel(const F8Quantize d, const F8Quantize x, unsigned d_blocks)
+__global__ void __launch_bounds__(256, DT == NOVA_F32 ? 2 : 3) f8_quantize_backward_kernel(const F8Quantize d, const F8Quantize x, unsigned d_blocks)
 {
     __shared__ F8Shared shared;
     if (blockIdx.x < d_blocks) f8_quantize_tiles<DT, FORMAT, 1, F8_GRADIENT, R>(d, blockIdx.x, d_blocks, shared);

@@ -484,8 +484,16 @@ static int run_band(const F8Call &a, const F8Shape &p, hipStream_t s)
     if (p.kind == 2) {
         if constexpr (WAY == F8_NARROW) return run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY, BAND>(a, s);
     }
-    // (eight waves hide more of each other's waits: 517 x 5001 x 2055 18.2 -> 14.9 us; as binary16, where each makes its operands, four)
-    if (p.kind >= 1) return run_tiles<std::conditional_t<WAY == F8_NARROW, F8Tile<2, 4, 4, 2>, F8Tile<2, 2, 4, 4>>, FA, FB, WAY, BAND>(a, s);
+    // Eight waves hide more of each other's waits: 517 x 5001 x 2055 to bfloat16 18.2 -> 14.9 us, to binary32 25.8 -> 24.1.  But as binary16 each wave makes its operands,
+    // and where compute units hold two workgroups, four are the faster (8192 x 8192 x 8192 937 -> 883).
+    if (p.kind >= 1) {
+        if constexpr (WAY == F8_NARROW) {
+            return run_tiles<F8Tile<2, 4, 4, 2>, FA, FB, WAY, BAND>(a, s);
+        } else {
+            const int64_t blocks = (int64_t)((a.a_tiles + 7) / 8) * ((a.b_tiles + 7) / 8) * a.splits;
+            return blocks <= 256 ? run_tiles<F8Tile<4, 2, 2, 4>, FA, FB, WAY, BAND>(a, s) : run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY, BAND>(a, s);
+        }
+    }
     if (p.mt == 1) return run_rows<1, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
     if (p.mt == 2) return p.nt == 1 ? run_rows<2, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s) : run_rows<2, 2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
     return p.nt == 1 ? run_rows<4, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s) : run_rows<4, 2, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);
