@@ -549,18 +549,19 @@ extern "C" int nova_logprobs_backward(const void *logits, int64_t stride, const 
 static bool f8_block_ok(int block) { return block == 1 || block == 128; }
 static bool f8_format_ok(int format) { return format == NOVA_F8_E4M3 || format == NOVA_F8_E5M2; }
 static bool f8_size_ok(int n) { return n >= 1 && n <= (1 << 24); }
+static bool f8_length_ok(int n) { return n >= 1 && n <= INT32_MAX - 127; }          // rounded up to whole panels it is still an int
 static size_t padded(const F8Layout &q) { return align256(q.bytes()); }
 
 extern "C" size_t nova_f8_bytes(int rows, int columns, int block)
 {
-    if (rows < 1 || columns < 1 || !f8_block_ok(block)) return 0;
+    if (!f8_length_ok(rows) || !f8_length_ok(columns) || !f8_block_ok(block)) return 0;
     return make_f8_layout(rows, columns, block).bytes();
 }
 
 extern "C" int nova_f8_quantize(const void *x, int64_t ldx, int rows, int columns, int dtype, int format, int block, int transposed, void *Xq, size_t Xq_bytes,
                                 void *stream)
 {
-    if (rows < 1 || columns < 1 || !any_dtype_ok(dtype) || !f8_format_ok(format) || !f8_block_ok(block) || (transposed & ~1) || !Xq || !aligned16(Xq) ||
+    if (!f8_length_ok(rows) || !f8_length_ok(columns) || !any_dtype_ok(dtype) || !f8_format_ok(format) || !f8_block_ok(block) || (transposed & ~1) || !Xq || !aligned16(Xq) ||
         !read_rows_ok(x, ldx, rows, columns))
         return NOVA_EINVAL;
     const F8Layout q = transposed ? make_f8_layout(columns, rows, block) : make_f8_layout(rows, columns, block);
@@ -571,7 +572,7 @@ extern "C" int nova_f8_quantize(const void *x, int64_t ldx, int rows, int column
 
 extern "C" int nova_f8_pack(const uint8_t *codes, const float *scales, int rows, int columns, int block, int transposed, void *Xq, size_t Xq_bytes, void *stream)
 {
-    if (!codes || !scales || rows < 1 || columns < 1 || !f8_block_ok(block) || (transposed & ~1) || (transposed && block == 1) || !Xq || !aligned16(Xq))
+    if (!codes || !scales || !f8_length_ok(rows) || !f8_length_ok(columns) || !f8_block_ok(block) || (transposed & ~1) || (transposed && block == 1) || !Xq || !aligned16(Xq))
         return NOVA_EINVAL;
     const F8Layout q = transposed ? make_f8_layout(columns, rows, block) : make_f8_layout(rows, columns, block);
     if (Xq_bytes < q.bytes()) return NOVA_ENOSPC;
@@ -580,13 +581,14 @@ extern "C" int nova_f8_pack(const uint8_t *codes, const float *scales, int rows,
 
 extern "C" int nova_f8_unpack(const void *Xq, size_t Xq_bytes, int rows, int columns, int block, uint8_t *codes, float *scales, void *stream)
 {
-    if (!Xq || !aligned16(Xq) || !codes || rows < 1 || columns < 1 || !f8_block_ok(block)) return NOVA_EINVAL;
+    if (!Xq || !aligned16(Xq) || !codes || !f8_length_ok(rows) || !f8_length_ok(columns) || !f8_block_ok(block))
+        return NOVA_EINVAL;
     const F8Layout q = make_f8_layout(rows, columns, block);
     if (Xq_bytes < q.bytes()) return NOVA_ENOSPC;
     return hip_result(launch_f8_unpack(Xq, q, codes, scales, stream));
 }
 
-static bool f8_product_ok(int M, int N, int K, int dtype) { return M >= 0 && f8_size_ok(N) && f8_size_ok(K) && any_dtype_ok(dtype); }
+static bool f8_product_ok(int M, int N, int K, int dtype) { return (M == 0 || f8_length_ok(M)) && f8_size_ok(N) && f8_size_ok(K) && any_dtype_ok(dtype); }
 
 // ReLU alone, or a sum that is added to what is there
 static bool f8_flags_ok(int flags) { return flags == 0 || flags == NOVA_FLAG_RELU || flags == NOVA_FLAG_ADD; }

@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropoutArgs a)
     const uint64_t total = (uint64_t)a.rows * groups;
     const unsigned upper = (unsigned)(a.threshold >> 16), lower = (unsigned)(a.threshold & 0xffff);      // upper: up to 65536
     for (uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (uint64_t)gridDim.x * 256) {
-        const unsigned row = (unsigned)(idx / groups), group = (unsigned)(idx % groups);
+        const unsigned row = total >> 32 ? (unsigned)(idx / groups) : (unsigned)idx / groups, group = (unsigned)idx - row * groups;          // (the lower words)
         const int64_t column = (int64_t)group * 8;
         const int count = (int)min((int64_t)8, a.columns - column);
         const bool before = column >= 8;

@@ -34,7 +34,8 @@ def near(got, want, bound, dtype):
     """got is want, summed in binary32 with an error below `bound`, rounded once to dtype."""
     err = (got.double().cpu() - want).abs()
     allowed = bound + HALF_STEP[dtype] * (want.abs() + bound) + SMALLEST[dtype]
-    assert bool((err <= allowed).all()), (err - allowed).max().item()
+    over = (err - allowed).max().item()
+    assert over <= 0, over
 
 
 # ---- quantisation ----

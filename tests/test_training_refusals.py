@@ -18,10 +18,11 @@ def test_sizes():
     assert L.nova_f8_bytes(4096, 25088, 1) == 4096 * 25088 + 196 * 4096 * 4
     assert L.nova_f8_bytes(17, 129, 1) == 2 * 2 * 2048 + 2 * 32 * 4
     assert L.nova_f8_bytes(17, 129, 128) == 2 * 2 * 2048 + 2 * 4
-    assert L.nova_f8_bytes(2 ** 31 - 1, 2 ** 31 - 1, 1) > 2 ** 62                   # (no overflow on the way)
-    for bad in ((0, 1, 1), (1, 0, 1), (-1, 1, 1), (1, 1, 0), (1, 1, 64), (1, 1, 129)):
+    most = 2 ** 31 - 128                                                            # (no overflow on the way)
+    assert L.nova_f8_bytes(most, most, 1) == most * most + most // 128 * most * 4 and L.nova_f8_bytes(most, 1, 128) == most * 128 + most // 128 * 4
+    for bad in ((most + 1, 1, 1), (1, most + 1, 1), (2 ** 31 - 1, 1, 128), (0, 1, 1), (1, 0, 1), (-1, 1, 1), (1, 1, 0), (1, 1, 64), (1, 1, 129)):
         assert L.nova_f8_bytes(*bad) == 0, bad
-    for bad in ((-1, 4, 4, F16), (4, 0, 4, F16), (4, 4, 0, F16), (4, (1 << 24) + 1, 4, F16), (4, 4, (1 << 24) + 1, F16), (4, 4, 4, 3), (0, 4, 4, F16)):
+    for bad in ((-1, 4, 4, F16), (4, 0, 4, F16), (4, 4, 0, F16), (4, (1 << 24) + 1, 4, F16), (4, 4, (1 << 24) + 1, F16), (4, 4, 4, 3), (0, 4, 4, F16), (most + 1, 4, 4, F16)):
         assert L.nova_f8_linear_workspace_bytes(*bad) == 0, bad
         assert L.nova_f8_linear_backward_workspace_bytes(*bad) == 0, bad
         assert L.nova_f8_matmul_workspace_bytes(*bad[:3], 1, 128, bad[3]) == 0, bad
@@ -38,7 +39,7 @@ def test_layouts():
     L = nova.lib()
     need = L.nova_f8_bytes(20, 300, 1)
     refused(L.nova_f8_quantize, dict(x=AT, ldx=300, rows=20, columns=300, dtype=F16, format=0, block=1, transposed=0, Xq=AT, Xq_bytes=need, stream=None),
-            [(dict(x=None), EINVAL), (dict(Xq=None), EINVAL), (dict(Xq=AT + 8), EINVAL), (dict(rows=0), EINVAL), (dict(columns=-3), EINVAL), (dict(ldx=299), EINVAL),
+            [(dict(x=None), EINVAL), (dict(Xq=None), EINVAL), (dict(Xq=AT + 8), EINVAL), (dict(rows=0), EINVAL), (dict(rows=2 ** 31 - 1, Xq_bytes=BIG), EINVAL), (dict(columns=-3), EINVAL), (dict(ldx=299), EINVAL),
              (dict(ldx=-300), EINVAL), (dict(dtype=3), EINVAL), (dict(format=2), EINVAL), (dict(format=-1), EINVAL), (dict(block=2), EINVAL), (dict(transposed=2), EINVAL),
              (dict(Xq_bytes=need - 1), ENOSPC), (dict(transposed=1, Xq_bytes=L.nova_f8_bytes(300, 20, 1) - 1), ENOSPC)])
     need = L.nova_f8_bytes(20, 300, 128)

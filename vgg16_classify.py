@@ -1,10 +1,10 @@
 #!/usr/bin/env python3
 """An image network from pixels to answers: the 13-layer VGG-16 convolution stack (F(m x m, 3 x 3), ReLU and max-pool fused), the three fully connected
 layers behind it with 4-bit weights, and the log probabilities of the 1000 classes with their entropy and the best five; then the gradient of
-the answers' log probabilities back through the three layers to the features, as adapters or a saliency map take it.  Random He-normal weights, N(0,1)
-images, binary16.
+the answers' log probabilities back through the three layers to the features, as adapters or a saliency map take it.  With --train, that many steps of training
+the three layers on the features: products in 8-bit floating point, dropout behind the hidden layers.  Random He-normal weights, N(0,1) images, binary16.
 
-    python vgg16_classify.py [--m 8] [--batch 32] [--points nova] [--group 128] [--reps 10]
+    python vgg16_classify.py [--m 8] [--batch 32] [--points nova] [--group 128] [--reps 10] [--train 0]
 
 Prints one JSON line: times of the stack, the layers, the log probabilities and the gradient, of one image or a batch; the whole forward pass as calls and as one
 graph.
@@ -86,6 +86,66 @@ class Head:
         return d
 
 
+class TrainedHead:
+    """The same layers as they train: binary32 weights, of which every step lays out 8-bit codes for both directions; dropout behind the two hidden layers, with masks that
+    depend on a step number on the device, so that a captured step draws new ones; plain gradient descent."""
+
+    def __init__(self, gen, batch, features, p=0.5, rate=1e-3, seed=16):
+        self.p, self.rate, self.seed, self.layers = p, rate, seed, []
+        self.step = torch.zeros(1, dtype=torch.int64, device=DEV)
+        sizes = [features, HIDDEN, HIDDEN, CLASSES]
+        for i, (K, N) in enumerate(zip(sizes, sizes[1:])):
+            half = dict(dtype=torch.float16, device=DEV)
+            hidden = i < 2
+            L = dict(N=N, K=K, weight=he_normal(gen, N, K).float(), master_bias=torch.zeros(N, device=DEV), bias=torch.zeros(N, **half), hidden=hidden,
+                     forward=torch.empty(nova.nova_f8_bytes(N, K, 128), dtype=torch.uint8, device=DEV),
+                     backward=torch.empty(nova.nova_f8_bytes(K, N, 128), dtype=torch.uint8, device=DEV),
+                     y=torch.empty((batch, N), **half), kept=torch.empty((batch, N), **half) if hidden else None, dy=torch.empty((batch, N), **half) if hidden else None,
+                     dx=torch.empty((batch, K), **half) if i else None, dw=torch.empty((N, K), device=DEV), dbias=torch.empty(N, device=DEV),
+                     workspace=torch.empty(max(nova.nova_f8_linear_workspace_bytes(batch, N, K, torch.float16),
+                                               nova.nova_f8_linear_backward_workspace_bytes(batch, N, K, torch.float16)), dtype=torch.uint8, device=DEV))
+            self.layers.append(L)
+            self.lay_out(L)
+        self.workspace = torch.empty(nova.nova_logprobs_workspace_bytes(batch, CLASSES, 0, torch.float16), dtype=torch.uint8, device=DEV)
+        self.dlogits = torch.empty((batch, CLASSES), dtype=torch.float16, device=DEV)
+
+    def lay_out(self, L):
+        nova.nova_f8_quantize(L["weight"], 128, Xq=L["forward"])
+        nova.nova_f8_quantize(L["weight"], 128, transposed=True, Xq=L["backward"])
+
+    def logits(self, x):
+        for i, L in enumerate(self.layers):
+            L["x"] = x
+            x = nova.nova_f8_linear(x, L["forward"], L["N"], bias=L["bias"], y=L["y"], flags=nova.NOVA_FLAG_RELU if L["hidden"] else 0, workspace=L["workspace"])
+            if L["hidden"]:
+                x = nova.nova_dropout(x, self.p, self.seed + i, device_offset=self.step, y=L["kept"])
+        return x
+
+    def gradient(self, logits, labels, answers, g_logprob):
+        d = nova.nova_logprobs_backward(logits, answers.stats, labels, g_logprob=g_logprob, dlogits=self.dlogits)
+        for i, L in reversed(list(enumerate(self.layers))):
+            if L["hidden"]:
+                d = nova.nova_dropout_backward(d, self.p, self.seed + i, device_offset=self.step, dx=L["dy"])
+            # (the first layer's input takes no gradient)
+            d, _, _ = nova.nova_f8_linear_backward(d, L["backward"] if i else None, L["x"], y=L["y"] if L["hidden"] else None, dx=L["dx"], dw=L["dw"], dbias=L["dbias"],
+                                                   workspace=L["workspace"])
+
+    def update(self):
+        for L in self.layers:
+            L["weight"].add_(L["dw"], alpha=-self.rate)
+            L["master_bias"].add_(L["dbias"], alpha=-self.rate)
+            L["bias"].copy_(L["master_bias"])
+            self.lay_out(L)
+        self.step.add_(1)
+
+    def train(self, x, labels, g_logprob):
+        logits = self.logits(x)
+        answers = nova.nova_logprobs(logits, labels, workspace=self.workspace)
+        self.gradient(logits, labels, answers, g_logprob)
+        self.update()
+        return answers
+
+
 def timed(f, reps):
     for _ in range(3):
         f()
@@ -107,6 +167,7 @@ def main(argv=None):
     ap.add_argument("--points", default="nova")
     ap.add_argument("--group", type=int, default=128, choices=(32, 64, 128))
     ap.add_argument("--reps", type=int, default=10)
+    ap.add_argument("--train", type=int, default=0, help="steps of training the fully connected layers")
     args = ap.parse_args(argv)
     gen = torch.Generator(device=DEV).manual_seed(16)
     images = torch.randn((args.batch, 3, args.size, args.size), device=DEV, generator=gen).half()
@@ -128,12 +189,25 @@ def main(argv=None):
     with torch.cuda.graph(graph):
         replayed = forward()
     times["forward_as_graph"] = timed(graph.replay, args.reps)
+    training, trained = None, None
+    if args.train:
+        trained = TrainedHead(gen, args.batch, stack.features)
+        start = torch.cuda.Event(enable_timing=True)
+        end = torch.cuda.Event(enable_timing=True)
+        losses = [-trained.train(features, labels, g).logprob.mean()]                    # (the first step alone: allocations, launches for the first time)
+        start.record()
+        for _ in range(args.train - 1):
+            losses.append(-trained.train(features, labels, g).logprob.mean())
+        end.record()
+        torch.cuda.synchronize()
+        training = dict(steps=args.train, ms_per_step=round(start.elapsed_time(end) / max(args.train - 1, 1), 4), losses=[round(v.item(), 4) for v in losses])
     print(json.dumps({
         "workload": f"VGG-16, batch {args.batch}, {args.size}x{args.size}, F({args.m},3), {args.points} points, fp16; fully connected layers in 4 bits, groups of {args.group}",
         "ms": times, "entropy": round(answers.entropy.mean().item(), 4), "log_probability": round(answers.logprob.mean().item(), 4),
         "best_of_first_image": answers.top_ids[0].tolist(), "finite": bool(torch.isfinite(gradient).all().item()),
+        **({"training": training} if training else {}),
     }))
-    return dict(features=features, logits=logits, labels=labels, answers=answers, gradient=gradient, replayed=replayed, head=head, g=g)
+    return dict(features=features, logits=logits, labels=labels, answers=answers, gradient=gradient, replayed=replayed, head=head, g=g, trained=trained)
 
 
 if __name__ == "__main__":
