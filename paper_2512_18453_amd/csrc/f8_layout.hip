@@ -25,15 +25,22 @@ __device__ __forceinline__ float *f8_scales(char *q, const F8Layout &layout) { r
 // in the same banks
 __device__ __forceinline__ int staged_piece(int panel, int piece) { return panel * 128 + (piece ^ ((piece / 16 ^ panel) & 7)); }
 
+// A layout that is a quarter of the last-level cache or more goes past the caches (4096 x 25088 in 128 x 128 56 -> 50 us); a smaller one is there when its product is formed
+// (the backward pass of 512 rows through 4096 x 4096 70 us, past the caches 75)
+__device__ __forceinline__ bool streamed(const F8Layout &layout) { return layout.code_bytes >= (size_t)64 << 20; }
+
 // A tile's codes from LDS to the panels row_tile .. of a chunk, of which the first FILLED of four quarters hold codes
 template <int FILLED>
 __device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
 {
     for (int piece = threadIdx.x; piece < kTile * kTile / 16; piece += 256) {
         const int panel = piece / 128, r = row_tile + panel;
-        if (r < layout.row_tiles)
-            *(uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16) =
-                piece % 64 / 16 < FILLED ? staged[staged_piece(panel, piece % 128)] : uint4v{0, 0, 0, 0};
+        if (r < layout.row_tiles) {
+            const uint4v codes = piece % 64 / 16 < FILLED ? staged[staged_piece(panel, piece % 128)] : uint4v{0, 0, 0, 0};
+            uint4v *const to = (uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16);
+            if (streamed(layout)) __builtin_nontemporal_store(codes, to);
+            else *to = codes;
+        }
     }
 }
 
@@ -289,7 +296,10 @@ __global__ void __launch_bounds__(256) f8_unpack_kernel(const char *__restrict__
         __builtin_memcpy(v, q + panel * kF8PanelBytes + piece % 2 * 1024 + (piece / 2 * 16 + row_in) * 16, 16);
         uint8_t *to = codes + row * layout.columns + column;
         if (column + 16 <= layout.columns) {
-            __builtin_memcpy(to, v, 16);
+            typedef unsigned Piece __attribute__((ext_vector_type(4), aligned(1)));
+            Piece whole;
+            __builtin_memcpy(&whole, v, 16);
+            __builtin_nontemporal_store(whole, (Piece *)to);
         } else {
 #pragma unroll
             for (int i = 0; i < 15; ++i)
