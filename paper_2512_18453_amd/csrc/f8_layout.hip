@@ -29,19 +29,26 @@ __device__ __forceinline__ int staged_piece(int panel, int piece) { return panel
 // (the backward pass of 512 rows through 4096 x 4096 70 us, past the caches 75)
 __device__ __forceinline__ bool streamed(const F8Layout &layout) { return layout.code_bytes >= (size_t)64 << 20; }
 
-// A tile's codes from LDS to the panels row_tile .. of a chunk, of which the first FILLED of four quarters hold codes
-template <int FILLED>
-__device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
+template <int FILLED, bool STREAMED>
+__device__ __forceinline__ void copy_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
 {
     for (int piece = threadIdx.x; piece < kTile * kTile / 16; piece += 256) {
         const int panel = piece / 128, r = row_tile + panel;
-        if (r < layout.row_tiles) {
-            const uint4v codes = piece % 64 / 16 < FILLED ? staged[staged_piece(panel, piece % 128)] : uint4v{0, 0, 0, 0};
-            uint4v *const to = (uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16);
-            if (streamed(layout)) __builtin_nontemporal_store(codes, to);
-            else *to = codes;
-        }
+        if (r >= layout.row_tiles) continue;
+        const uint4v codes = piece % 64 / 16 < FILLED ? staged[staged_piece(panel, piece % 128)] : uint4v{0, 0, 0, 0};
+        uint4v *const to = (uint4v *)(q + ((size_t)r * layout.chunks + chunk) * kF8PanelBytes + piece % 128 * 16);
+        if constexpr (STREAMED) __builtin_nontemporal_store(codes, to);
+        else *to = codes;
     }
+}
+
+// A tile's codes from LDS to the panels row_tile .. of a chunk, of which the first FILLED of four quarters hold codes.  (Two loops: of two stores in one the compiler makes one
+// that goes through the caches.)
+template <int FILLED>
+__device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
+{
+    if (streamed(layout)) copy_panels<FILLED, true>(staged, q, layout, row_tile, chunk);
+    else copy_panels<FILLED, false>(staged, q, layout, row_tile, chunk);
 }
 
 // Eight columns of COUNT rows from row on, STEP apart, `count` of which exist; elements whose gate is closed, and rows and columns behind the last, are zero.  (Rows behind
