@@ -25,9 +25,9 @@ __device__ __forceinline__ float *f8_scales(char *q, const F8Layout &layout) { r
 // in the same banks
 __device__ __forceinline__ int staged_piece(int panel, int piece) { return panel * 128 + (piece ^ ((piece / 16 ^ panel) & 7)); }
 
-// A layout that is a quarter of the last-level cache or more goes past the caches (4096 x 25088 in 128 x 128 56 -> 50 us); a smaller one is there when its product is formed
-// (the backward pass of 512 rows through 4096 x 4096 70 us, past the caches 75)
-__device__ __forceinline__ bool streamed(const F8Layout &layout) { return layout.code_bytes >= (size_t)64 << 20; }
+// Layouts of 8 MB and more go past the caches: 4096 x 25088 in 128 x 128 56 -> 50 us, 2048 rows through a layer of 4096 x 4096, whose product reads them at once, 44.6 -> 42.9.
+// Smaller ones stay in them (the backward pass of 512 rows through that layer 70 us, past the caches 75).
+constexpr size_t kStreamedLayout = (size_t)8 << 20;
 
 template <int FILLED, bool STREAMED>
 __device__ __forceinline__ void copy_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
@@ -47,7 +47,7 @@ __device__ __forceinline__ void copy_panels(const uint4v *staged, char *q, const
 template <int FILLED>
 __device__ __forceinline__ void write_panels(const uint4v *staged, char *q, const F8Layout &layout, int row_tile, int chunk)
 {
-    if (streamed(layout)) copy_panels<FILLED, true>(staged, q, layout, row_tile, chunk);
+    if (layout.code_bytes >= kStreamedLayout) copy_panels<FILLED, true>(staged, q, layout, row_tile, chunk);
     else copy_panels<FILLED, false>(staged, q, layout, row_tile, chunk);
 }
 
@@ -83,7 +83,7 @@ __device__ __forceinline__ void load_rows(const F8Source &src, int64_t row, int6
 }
 
 // A scale per row and chunk, and nothing but the rows' layout: a panel is one wave's
-template <int DT, int FORMAT>
+template <int DT, int FORMAT, bool STREAMED>
 __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const F8Quantize a)
 {
     typedef Storage<DT> T;
@@ -110,8 +110,13 @@ __global__ void __launch_bounds__(256) f8_quantize_rows_kernel(const F8Quantize 
         }
         exchange_in_wave();
         uint4v *const to = (uint4v *)(a.rows_q + panel * kF8PanelBytes);
-        to[lane] = staged[wave][lane];
-        to[lane + 64] = staged[wave][lane + 64];
+        if constexpr (STREAMED) {
+            __builtin_nontemporal_store(staged[wave][lane], to + lane);
+            __builtin_nontemporal_store(staged[wave][lane + 64], to + lane + 64);
+        } else {
+            to[lane] = staged[wave][lane];
+            to[lane + 64] = staged[wave][lane + 64];
+        }
         exchange_in_wave();
     }
 }
@@ -271,17 +276,21 @@ __global__ void __launch_bounds__(256) f8_pack_kernel(const uint8_t *__restrict_
 {
     const size_t stride = (size_t)gridDim.x * 256, first = (size_t)blockIdx.x * 256 + threadIdx.x;
     for (size_t idx = first; idx < layout.code_bytes / 16; idx += stride) {
-        const int piece = idx % 128, lane = piece % 64;
+        // neighbours take neighbouring pieces of a row, or, transposed, neighbouring columns of the source
+        const int at = idx % 128, row_in = transposed ? at % 16 : at / 8, eighth = transposed ? at / 16 : at % 8;
         const size_t panel = idx / 128;
-        const int64_t row = (int64_t)(panel / layout.chunks) * kF8Rows + lane % 16;
-        const int64_t column = (int64_t)(panel % layout.chunks) * kF8Chunk + lane / 16 * 32 + piece / 64 * 16;
+        const int64_t row = (int64_t)(panel / layout.chunks) * kF8Rows + row_in, column = (int64_t)(panel % layout.chunks) * kF8Chunk + eighth * 16;
         uint8_t v[16];
+        if (!transposed && row < layout.rows && column + 16 <= layout.columns) {
+            __builtin_memcpy(v, codes + row * layout.columns + column, 16);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const bool real = row < layout.rows && column + i < layout.columns;
-            v[i] = real ? codes[transposed ? (column + i) * layout.rows + row : row * layout.columns + column + i] : (uint8_t)0;
+            for (int i = 0; i < 16; ++i) {
+                const bool real = row < layout.rows && column + i < layout.columns;
+                v[i] = real ? codes[transposed ? (column + i) * layout.rows + row : row * layout.columns + column + i] : (uint8_t)0;
+            }
         }
-        __builtin_memcpy(q + idx * 16, v, 16);
+        __builtin_memcpy(q + panel * kF8PanelBytes + eighth % 2 * 1024 + (eighth / 2 * 16 + row_in) * 16, v, 16);
     }
     const int bands = (int)(((int64_t)layout.rows + layout.block - 1) / layout.block);
     for (size_t idx = first; idx < layout.scale_count; idx += stride) {
@@ -338,7 +347,9 @@ static void run_quantize(const F8Quantize &a, int block, hipStream_t s)
         else f8_quantize_kernel<DT, FORMAT, 128, F8_COLUMNS, 8><<<blocks, 256, 0, s>>>(a);
     } else if (a.rows_q) {
         const size_t wanted = ((size_t)a.rows_layout.row_tiles * a.rows_layout.chunks + 3) / 4;
-        f8_quantize_rows_kernel<DT, FORMAT><<<(unsigned)(wanted < (1 << 22) ? wanted : 1 << 22), 256, 0, s>>>(a);
+        const unsigned panels_blocks = (unsigned)(wanted < (1 << 22) ? wanted : 1 << 22);
+        if (a.rows_layout.code_bytes >= kStreamedLayout) f8_quantize_rows_kernel<DT, FORMAT, true><<<panels_blocks, 256, 0, s>>>(a);
+        else f8_quantize_rows_kernel<DT, FORMAT, false><<<panels_blocks, 256, 0, s>>>(a);
     } else if (a.src.rows <= kFewRows) {
         f8_quantize_kernel<DT, FORMAT, 1, F8_COLUMNS, 2><<<blocks, 256, 0, s>>>(a);
     } else {

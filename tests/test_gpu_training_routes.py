@@ -22,13 +22,13 @@ def linear(M, N, K, dtype):
     (1, 1000, 4096, F32, ["f8_rows_kernel<1, 1, 0, 0, 1, 1, 0>"]),
     (1, 4096, 25088, F16, ["f8_rows_kernel<1, 1, 0, 0, 0, 1, 1>"]),
     (8, 4096, 4096, BF16, ["f8_rows_kernel<1, 1, 0, 0, 0, 1, 2>"]),
-    (9, 4096, 4096, BF16, ["f8_quantize_rows_kernel<2, 0>", "f8_rows_kernel<1, 1, 0, 0, 0, 1, -1>"]),
-    (32, 4096, 4096, F16, ["f8_quantize_rows_kernel<1, 0>", "f8_rows_kernel<2, 1, 0, 0, 0, 1, -1>"]),
-    (64, 25088, 4096, F16, ["f8_quantize_rows_kernel<1, 0>", "f8_rows_kernel<4, 2, 0, 0, 0, 1, -1>"]),
-    (65, 25088, 400, F16, ["f8_quantize_rows_kernel<1, 0>", "f8_tile_kernel<nova::F8Tile<2, 4, 4, 2>, 0, 0, 0, 1>"]),
-    (4096, 8192, 8192, BF16, ["f8_quantize_rows_kernel<2, 0>", "f8_tile_kernel<nova::F8Tile<4, 2, 4, 8>, 0, 0, 0, 1>"]),
-    (517, 5001, 2055, F32, ["f8_quantize_rows_kernel<0, 0>", "f8_tile_kernel<nova::F8Tile<4, 2, 2, 4>, 0, 0, 1, 1>"]),
-    (4096, 8192, 256, F32, ["f8_quantize_rows_kernel<0, 0>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 0, 0, 1, 1>"]),
+    (9, 4096, 4096, BF16, ["f8_quantize_rows_kernel<2, 0, 0>", "f8_rows_kernel<1, 1, 0, 0, 0, 1, -1>"]),
+    (32, 4096, 4096, F16, ["f8_quantize_rows_kernel<1, 0, 0>", "f8_rows_kernel<2, 1, 0, 0, 0, 1, -1>"]),
+    (64, 25088, 4096, F16, ["f8_quantize_rows_kernel<1, 0, 0>", "f8_rows_kernel<4, 2, 0, 0, 0, 1, -1>"]),
+    (65, 25088, 400, F16, ["f8_quantize_rows_kernel<1, 0, 0>", "f8_tile_kernel<nova::F8Tile<2, 4, 4, 2>, 0, 0, 0, 1>"]),
+    (4096, 8192, 8192, BF16, ["f8_quantize_rows_kernel<2, 0, 1>", "f8_tile_kernel<nova::F8Tile<4, 2, 4, 8>, 0, 0, 0, 1>"]),
+    (517, 5001, 2055, F32, ["f8_quantize_rows_kernel<0, 0, 0>", "f8_tile_kernel<nova::F8Tile<4, 2, 2, 4>, 0, 0, 1, 1>"]),
+    (4096, 8192, 256, F32, ["f8_quantize_rows_kernel<0, 0, 0>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 0, 0, 1, 1>"]),
 ])
 def test_linear(M, N, K, dtype, want):
     assert linear(M, N, K, dtype) == want
