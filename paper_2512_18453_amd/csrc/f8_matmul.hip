@@ -95,6 +95,8 @@ __device__ __forceinline__ void write_four(const F8Call &a, int split, int64_t m
         });
 }
 
+struct F8Shape { int kind, mt, nt, waves, splits, split_chunks; };           // kind: 0 up to 64 rows, 1 tiles of 128 x 128, 2 of 256 x 256
+
 // ---- up to 64 rows ----
 //
 // Bound by B's bytes.  A workgroup makes 16 NT columns for all rows; its waves take the chunks of those columns in turn, load B's panels straight into registers, AHEAD - 1 ahead, and
@@ -102,7 +104,15 @@ __device__ __forceinline__ void write_four(const F8Call &a, int split, int64_t m
 // which saves the launch that would do it.
 constexpr int kLaidOut = -1;
 struct F8RowsOf { const void *x; int64_t ld; int K; };           // what A is quantised from
-constexpr size_t kFusedElements = 32768, kFusedLds = 128 * 1024;
+
+// Whether it saves more than it costs: every workgroup does the same, and LDS holds no more than 32768 elements.  Up to four rows it does (in us, with a launch of its own
+// first and without: 1 row by 32768 x 4096 33.6, 29.2; 1 by 25088 x 4096 25.4, 22.6; 4 by 4096 x 16384 20.9, 19.9); more rows save less of what is loaded of A (a panel has 16),
+// and then the workgroups' elements count: 8 by 2048 x 4096 10.3, 7.9; 6 by 4096 x 4096 10.3, 10.1; 7 10.4, 10.8; 16 by 2048 x 4096 9.8, 10.6; 8 by 2048 x 16384 14.8, 17.1.
+static bool quantised_on_the_way(int M, int N, const F8Shape &p)
+{
+    const size_t elements = (size_t)M * p.split_chunks * kF8Chunk, workgroups = (size_t)ceil_div(N, 16) * p.splits;
+    return p.kind == 0 && p.mt == 1 && elements <= 32768 && (M <= 4 || elements * workgroups <= (size_t)6 << 20);
+}
 
 // MT panels of rows, NT of columns; DT: kLaidOut, or the type of x
 template <int MT, int NT, int FA, int FB, int WAY, bool BAND, int DT>
@@ -226,7 +236,7 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
 // A workgroup of WM x WN waves makes 16 WM MT rows by 16 WN NT columns.  A stage is a chunk of both operands' panels with their scales; stages come straight from global
 // memory to LDS, one ahead of the one that is multiplied, and a panel lies there as it lies in memory: the 64 lanes of a wave read 1024 bytes side by side.
 //
-// 8192 x 8192 x 8192 to bfloat16 439 us, 2504 TFLOP/s where a large library product of that format with one scale per matrix reaches 2655; with a scale per row and chunk
+// 8192 x 8192 x 8192 to bfloat16 439 us (469 on another card), 2504 TFLOP/s where a large library product of that format with one scale per matrix reaches 2655; with a scale per row and chunk
 // of B too, where a sum takes two vector instructions instead of one, 527.  LDS binds about as much as the matrix unit: a chunk of a 256 x 256 tile is 2048 clocks of matrix
 // instructions, 64 KB written and 192 KB read at 128 bytes a clock.  128 x 128 tiles, two workgroups per compute unit, read a third more: 512 us.  A's panels loaded by
 // each wave into registers instead took more of those than there are (813).
@@ -403,8 +413,6 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8Call a)
     }
 }
 
-struct F8Shape { int kind, mt, nt, waves, splits, split_chunks; };           // kind: 0 up to 64 rows, 1 tiles of 128 x 128, 2 of 256 x 256
-
 static F8Shape f8_shape(int M, int N, int K, bool full)
 {
     F8Shape p = {};
@@ -473,8 +481,7 @@ static int run_rows(const F8Call &a, const F8RowsOf &rows, const F8Shape &p, hip
 {
     const auto kernel = f8_rows_kernel<MT, NT, FA, FB, WAY, BAND, DT>;
     const size_t sums = (size_t)p.waves * MT * NT * 1024, operand = DT == kLaidOut ? 0 : (size_t)a.split_chunks * a.M * (kF8Chunk + 4);
-    const size_t lds = sums > operand ? sums : operand;
-    if (lds > 64 * 1024) NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFusedLds));
+    const size_t lds = sums > operand ? sums : operand;          // 33 KB at most
     kernel<<<(unsigned)((a.b_tiles + NT - 1) / NT * (int64_t)a.splits), p.waves * 64, lds, s>>>(a, rows);
     return (int)hipGetLastError();
 }
@@ -539,7 +546,7 @@ int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, v
 int launch_f8_linear(const F8Source &x, const F8Operand &a, const F8Operand &w, const void *bias, void *y, int64_t ldy, int flags, void *workspace, void *stream)
 {
     const F8Shape p = f8_shape(x.rows, w.layout.rows, x.columns, x.dtype == NOVA_F32);
-    if (p.kind == 0 && p.mt == 1 && (size_t)x.rows * p.split_chunks * kF8Chunk <= kFusedElements) {
+    if (quantised_on_the_way(x.rows, w.layout.rows, p)) {
         const F8Call call = make_call(a, w, p, bias, y, ldy, x.dtype, flags, workspace);
         const F8RowsOf rows = {x.x, x.ld, x.columns};
         hipStream_t s = (hipStream_t)stream;
