@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(512) f8_rows_kernel(const F8Call a, const F8Ro
 // A workgroup of WM x WN waves makes 16 WM MT rows by 16 WN NT columns.  A stage is a chunk of both operands' panels with their scales; stages come straight from global
 // memory to LDS, one ahead of the one that is multiplied, and a panel lies there as it lies in memory: the 64 lanes of a wave read 1024 bytes side by side.
 //
-// 8192 x 8192 x 8192 to bfloat16 439 us (469 on another card), 2504 TFLOP/s where a large library product of that format with one scale per matrix reaches 2655; with a scale per row and chunk
+// 8192 x 8192 x 8192 to bfloat16 439 us (479 on another card), 2504 TFLOP/s where a large library product of that format with one scale per matrix reaches 2655; with a scale per row and chunk
 // of B too, where a sum takes two vector instructions instead of one, 527.  LDS binds about as much as the matrix unit: a chunk of a 256 x 256 tile is 2048 clocks of matrix
 // instructions, 64 KB written and 192 KB read at 128 bytes a clock.  128 x 128 tiles, two workgroups per compute unit, read a third more: 512 us.  A's panels loaded by
 // each wave into registers instead took more of those than there are (813).
@@ -433,7 +433,7 @@ static F8Shape f8_shape(int M, int N, int K, bool full)
     } else {
         // An estimate in us of each way.  128 x 128: one or two workgroups per compute unit, so a chunk of one or both; 256 x 256: one.  (From 1024 x 4096 x 4096 and
         // 8192 x 8192 x 8192, with 128 columns of B per scale.)  A cut sum's pieces are written and read, and another kernel joins them.  On 45 drawn calls of 65 to 4096 rows the
-        // way and cut that it chooses took 1.03 times as long as the best of up to 16 tried, on the average.
+        // way and cut that it chooses took 1.014 times as long as the best of up to 16 tried, on the average; on the 45 it was fitted with, 1.03.
         double least = 0;
         for (int kind = 1; kind <= (full ? 1 : 2); ++kind)
             for (int splits = 1; splits <= 16 && splits <= chunks; ++splits) {
