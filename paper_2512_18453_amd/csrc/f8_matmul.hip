@@ -493,13 +493,14 @@ static int run_band(const F8Call &a, const F8Shape &p, hipStream_t s)
         if constexpr (WAY == F8_NARROW) return run_tiles<F8Tile<4, 2, 4, 8>, FA, FB, WAY, BAND>(a, s);
     }
     // Eight waves hide more of each other's waits: 517 x 5001 x 2055 to bfloat16 18.2 -> 14.9 us, to binary32 25.8 -> 24.1.  But as binary16 each wave makes its operands,
-    // and where compute units hold two workgroups, four are the faster (8192 x 8192 x 8192 937 -> 883).
+    // and where compute units hold two workgroups and sums are long, four are the faster (8192 x 8192 x 8192 937 -> 883, 4096 x 4096 x 1024 42.9 -> 41.8; but x 512 27.5, with
+    // four 27.9, and the gradients of 32 rows by 25088 x 4096 122.6, with four 131.6).
     if (p.kind >= 1) {
         if constexpr (WAY == F8_NARROW) {
             return run_tiles<F8Tile<2, 4, 4, 2>, FA, FB, WAY, BAND>(a, s);
         } else {
             const int64_t blocks = (int64_t)((a.a_tiles + 7) / 8) * ((a.b_tiles + 7) / 8) * a.splits;
-            return blocks <= 256 ? run_tiles<F8Tile<4, 2, 2, 4>, FA, FB, WAY, BAND>(a, s) : run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY, BAND>(a, s);
+            return blocks <= 256 || a.split_chunks <= 6 ? run_tiles<F8Tile<4, 2, 2, 4>, FA, FB, WAY, BAND>(a, s) : run_tiles<F8Tile<2, 2, 4, 4>, FA, FB, WAY, BAND>(a, s);
         }
     }
     if (p.mt == 1) return run_rows<1, 1, FA, FB, WAY, BAND, kLaidOut>(a, {}, p, s);

@@ -156,7 +156,7 @@ def test_matmul(M, N, K, blocks):
         assert torch.equal(again, got)
 
 
-@pytest.mark.parametrize("M,N,K", SIZES + [(1, 4096, 8200), (520, 1030, 390)])
+@pytest.mark.parametrize("M,N,K", SIZES + [(1, 4096, 8200), (520, 1030, 390), (2100, 2200, 1000)])
 @pytest.mark.parametrize("dtype", [F32, F16])
 def test_matmul_of_whole_numbers(M, N, K, dtype):
     """Codes -1, 0, 1 under scales of 1 and 2 (2^-1): sums are whole multiples of 1/4 below 2^9, which every way of summing and binary16 hold exactly."""
@@ -177,7 +177,7 @@ def test_matmul_of_whole_numbers(M, N, K, dtype):
             assert torch.equal(got.cpu().double(), want), (block_a, block_b, fa, fb)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 100, 129), (20, 130, 4100), (150, 259, 300), (300, 700, 257)])
+@pytest.mark.parametrize("M,N,K", [(1, 100, 129), (20, 130, 4100), (150, 259, 300), (300, 700, 257), (2100, 2200, 900)])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_bias_relu_add(M, N, K, dtype):
     a, Aq = operand(M, K, 0, 1, seed=1)

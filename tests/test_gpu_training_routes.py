@@ -28,15 +28,15 @@ def linear(M, N, K, dtype):
     (65, 25088, 400, F16, ["f8_quantize_rows_kernel<1, 0, 0>", "f8_tile_kernel<nova::F8Tile<2, 4, 4, 2>, 0, 0, 0, 1>"]),
     (4096, 8192, 8192, BF16, ["f8_quantize_rows_kernel<2, 0, 1>", "f8_tile_kernel<nova::F8Tile<4, 2, 4, 8>, 0, 0, 0, 1>"]),
     (517, 5001, 2055, F32, ["f8_quantize_rows_kernel<0, 0, 0>", "f8_tile_kernel<nova::F8Tile<4, 2, 2, 4>, 0, 0, 1, 1>"]),
-    (4096, 8192, 256, F32, ["f8_quantize_rows_kernel<0, 0, 0>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 0, 0, 1, 1>"]),
+    (4096, 8192, 2048, F32, ["f8_quantize_rows_kernel<0, 0, 1>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 0, 0, 1, 1>"]),
 ])
 def test_linear(M, N, K, dtype, want):
     assert linear(M, N, K, dtype) == want
 
 
 @pytest.mark.parametrize("M,dtype,want", [
-    (32, F16, ["f8_quantize_backward_kernel<1, 1, 2>", "f8_rows_kernel<2, 2, 1, 0, 0, 1, -1>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 1, 0, 1, 0>"]),
-    (100, BF16, ["f8_quantize_backward_kernel<2, 1, 8>", "f8_tile_kernel<nova::F8Tile<2, 4, 4, 2>, 1, 0, 0, 1>", "f8_tile_kernel<nova::F8Tile<2, 2, 4, 4>, 1, 0, 1, 0>"]),
+    (32, F16, ["f8_quantize_backward_kernel<1, 1, 2>", "f8_rows_kernel<2, 2, 1, 0, 0, 1, -1>", "f8_tile_kernel<nova::F8Tile<4, 2, 2, 4>, 1, 0, 1, 0>"]),
+    (100, BF16, ["f8_quantize_backward_kernel<2, 1, 8>", "f8_tile_kernel<nova::F8Tile<2, 4, 4, 2>, 1, 0, 0, 1>", "f8_tile_kernel<nova::F8Tile<4, 2, 2, 4>, 1, 0, 1, 0>"]),
 ])
 def test_backward(M, dtype, want):
     N, K = 2048, 16384
