@@ -83,19 +83,25 @@ def sanitize_selftest():
     is not part of it.  Returns what the two programs printed; raises if one of them fails."""
     os.makedirs(OBJ, exist_ok=True)
     oracle_dir = os.path.join(HERE, "..", "oracle")
-    host = os.path.join(OBJ, "host_selftest_sanitized")
     orac = os.path.join(OBJ, "conv_oracle_selftest_sanitized")
-    subprocess.check_call(["g++", "-std=c++17", "-pthread"] + SANITIZE + ["-o", host] +
-                          [os.path.join(SRC, f) for f in ("host_selftest.cpp", "transforms.cpp", "discovery.cpp")])
     subprocess.check_call(["gcc", "-std=c11", "-ffp-contract=off", "-fopenmp"] + SANITIZE +
                           ["-o", orac, os.path.join(oracle_dir, "conv_oracle_selftest.c"), "-lm"])
-    out = []
-    for prog in (host, orac):
-        res = subprocess.run([prog], capture_output=True, text=True)
-        if res.returncode != 0:
-            raise RuntimeError(f"{os.path.basename(prog)} failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
-        out.append(res.stdout.strip())
-    return out
+    return [host_program("host_selftest.cpp", "transforms.cpp", "discovery.cpp"), _output(orac)]
+
+
+def host_program(*sources, flags=SANITIZE):
+    """Builds a program of csrc/ that needs no GPU, named by its first source, and runs it.  Returns what it printed; raises if it fails."""
+    os.makedirs(OBJ, exist_ok=True)
+    prog = os.path.join(OBJ, sources[0].removesuffix(".cpp"))
+    subprocess.check_call(["g++", "-std=c++17", "-pthread", "-ffp-contract=off"] + flags + ["-o", prog] + [os.path.join(SRC, f) for f in sources])
+    return _output(prog)
+
+
+def _output(prog):
+    res = subprocess.run([prog], capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"{os.path.basename(prog)} failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+    return res.stdout.strip()
 
 
 if __name__ == "__main__":

@@ -2,21 +2,10 @@
 //
 // The products of a chunk are summed on the matrix unit, from zero, and the sum is scaled and added in binary32.  The matrix unit's rows are B's (n) and its
 // columns A's (m): a lane then holds four neighbouring n of one m, so that A's scale is one number per lane and B's, where 128 rows share it, one per wave.
+#include "f8_call.hpp"
 #include "f8_common.hpp"
 
 namespace nova {
-
-struct F8Call {
-    const char *a, *b;
-    const float *a_scales, *b_scales;
-    const void *bias;
-    void *out;
-    float *partial;                               // [splits][M][N]
-    int64_t ldout;
-    int M, N, chunks, splits, split_chunks;
-    int a_tiles, b_tiles, a_pitch, b_pitch, a_shift, b_shift;      // panels; scales from chunk to chunk; rows -> scales
-    int dtype, flags;
-};
 
 __device__ __forceinline__ F8Fragment load_fragment(const char *panel, int lane)
 {
@@ -81,7 +70,7 @@ struct F8Columns {
 template <int WIDE = -1, typename F>
 __device__ __forceinline__ void with_results(const F8Call &a, int split, F &&f)
 {
-    if (a.splits > 1) f(0.0f, a.partial + (size_t)split * a.M * a.N, (int64_t)a.N, nullptr, 0);
+    if (a.splits > 1) f(0.0f, a.partial + f8_piece_at(a, split), (int64_t)a.N, nullptr, 0);
     else if (WIDE < 0 ? a.dtype == NOVA_F32 : WIDE) f(0.0f, a.out, a.ldout, a.bias, a.flags);
     else if (a.dtype == NOVA_F16) f((f16)0.0f, a.out, a.ldout, a.bias, a.flags);
     else f((bf16)0.0f, a.out, a.ldout, a.bias, a.flags);
@@ -283,9 +272,9 @@ __global__ void __launch_bounds__(Shape::THREADS, 2) f8_tile_kernel(const F8Call
 #pragma unroll
     for (int p = 0; p < PW; ++p)                                                             // (past the last: computed and not stored)
         panel[p] = uniform_pointer((of_a ? a.a : a.b) + ((size_t)min(panel0 + p, last) * a.chunks + first) * kF8PanelBytes);
-    const int pitch = scales_of_a ? a.a_pitch : a.b_pitch, row0 = (scales_of_a ? m_tile + 4 * wave : n_tile + 4 * wave - Shape::A) * 16;
+    const int pitch = scales_of_a ? a.a_pitch : a.b_pitch, left = scales_of_a ? a.a_left : a.b_pitch, row0 = (scales_of_a ? m_tile + 4 * wave : n_tile + 4 * wave - Shape::A) * 16;
     const char *scales = uniform_pointer((const char *)((scales_of_a ? a.a_scales : a.b_scales) + (size_t)first * pitch));
-    const unsigned scale_at = (unsigned)min((row0 + lane) >> (scales_of_a ? a.a_shift : a.b_shift), pitch - 1) * 4u;
+    const unsigned scale_at = (unsigned)f8_scale_at(row0 + lane, scales_of_a ? a.a_shift : a.b_shift, left) * 4u;
     const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(size_t)((__attribute__((address_space(3))) const void *)lds));
     auto issue = [&](int stage) __attribute__((always_inline)) {
         const unsigned at = lds0 + (unsigned)(stage * STAGE);
@@ -411,7 +400,7 @@ __global__ void __launch_bounds__(256) f8_join_kernel(F8Call a)
         for (int split = 0; split < splits; ++split)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-                if (n + v < a.N) sum[v] += a.partial[((size_t)split * a.M + m) * a.N + n + v];
+                if (n + v < a.N) sum[v] += a.partial[f8_piece_at(a, split) + m * a.N + n + v];
         write_four(a, 0, m, n, sum);
     }
 }
@@ -465,14 +454,9 @@ static int run_tiles(const F8Call &a, hipStream_t s)
     const auto kernel = f8_tile_kernel<Shape, FA, FB, WAY, BAND>;
     NOVA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::LDS));
     const int64_t across = (a.b_tiles + Shape::B - 1) / Shape::B * (int64_t)a.splits;
-    const int64_t step = (((int64_t)1 << 22) / across > 0 ? ((int64_t)1 << 22) / across : 1) * Shape::A;           // rows in pieces that keep a launch below 2^31 threads
-    for (int64_t tile = 0; tile < a.a_tiles; tile += step) {
-        F8Call part = a;
-        part.a_tiles = (int)(a.a_tiles - tile < step ? a.a_tiles - tile : step);
-        part.M = (int)(a.M - tile * 16 < part.a_tiles * (int64_t)16 ? a.M - tile * 16 : part.a_tiles * (int64_t)16);
-        part.a += (size_t)tile * a.chunks * kF8PanelBytes;
-        part.a_scales += (tile * 16) >> a.a_shift;
-        part.out = (char *)a.out + tile * 16 * a.ldout * (int64_t)dtype_size(a.dtype);
+    const int64_t step = f8_launch_panels(across, Shape::A, kF8LaunchBlocks);
+    for (int64_t first = 0; first < a.a_tiles; first += step) {
+        const F8Call part = f8_launch(a, first, step);
         kernel<<<(unsigned)(across * ((part.a_tiles + Shape::A - 1) / Shape::A)), Shape::THREADS, Shape::LDS, s>>>(part);
         NOVA_HIP_TRY(hipGetLastError());
     }
@@ -533,7 +517,7 @@ static F8Call make_call(const F8Operand &a, const F8Operand &b, const F8Shape &p
     const F8Layout &la = a.layout, &lb = b.layout;
     return {(const char *)a.q, (const char *)b.q, (const float *)((const char *)a.q + la.code_bytes), (const float *)((const char *)b.q + lb.code_bytes), bias, out,
             (float *)workspace, ldout, la.rows, lb.rows, la.chunks, p.splits, p.split_chunks, la.row_tiles, lb.row_tiles, la.scale_pitch, lb.scale_pitch,
-            la.block == 1 ? 0 : 7, lb.block == 1 ? 0 : 7, dtype, flags};
+            la.block == 1 ? 0 : 7, lb.block == 1 ? 0 : 7, dtype, flags, la.scale_pitch, la.rows};
 }
 
 int launch_f8_matmul(const F8Operand &a, const F8Operand &b, const void *bias, void *out, int64_t ldout, int dtype, int flags, void *workspace, void *stream)
