@@ -44,3 +44,68 @@ def test_quiet_products_beside_loud_ones(M, N, K, dtype):
     dx = nova.nova_f8_linear_backward(x.to(dtype).to(DEV), nova.nova_f8_pack(codes.T.contiguous().to(DEV), scales.T.contiguous().to(DEV), 128, transposed=True), None, K=N,
                                       format=nova.NOVA_F8_E4M3, need_dbias=False)[0]
     near(dx, want, bound, dtype)
+
+
+# ---- more rows, results in 16 bits: the cut-off that nova.h describes ----
+
+def powers(codes, lowest):
+    """The exponent of every code's power of two; subnormal codes have the lowest normal one's, zeros none."""
+    return torch.where(codes == 0, -1000.0, torch.floor(torch.log2(codes.abs().clamp(min=2.0 ** lowest))))
+
+
+def cut_sums(a, b, formats):
+    """Sums of chunks [M, N, chunks], in 64 bits, of codes [M, K], [N, K]: of eight neighbouring products everything below 2^-13 of the largest product of the two codes' powers
+    of two is cut off, toward zero."""
+    (M, K), N = a.shape, len(b)
+    ea, eb = powers(a, -6 if formats[0] == 0 else -14), powers(b, -6 if formats[1] == 0 else -14)
+    out = torch.zeros((M, N, K // 128), dtype=torch.float64, device=DEV)
+    for k in range(0, K, 8):
+        step = 2.0 ** ((ea[:, None, k:k + 8] + eb[None, :, k:k + 8]).amax(2, keepdim=True).clamp(min=-100) - 13)
+        out[:, :, k // 128] += (torch.trunc(a[:, None, k:k + 8] * b[None, :, k:k + 8] / step) * step).sum(2)
+    return out
+
+
+def normal(rows, K, gen):
+    return torch.randn((rows, K), generator=gen)
+
+
+def loud_columns(by):
+    def draw(rows, K, gen):
+        return torch.randn((rows, K), generator=gen) * (1 + (by - 1) * (torch.rand((K,), generator=gen) < 0.005))
+    return draw
+
+
+def log_normal(rows, K, gen):
+    return torch.randn((rows, K), generator=gen).sign() * torch.exp(2 * torch.randn((rows, K), generator=gen))
+
+
+# what the cut-off adds to an error in binary16 whose root mean square is otherwise the rounding's: at most this share of it
+@pytest.mark.parametrize("draw,formats,share", [(normal, (0, 0), 0.1), (loud_columns(20), (0, 0), 0.2), (loud_columns(100), (0, 0), 0.35), (normal, (1, 0), 0.1),
+                                                (log_normal, (1, 0), 0.45)])
+@pytest.mark.parametrize("M,N,K", [(128, 128, 1024), (65, 200, 512)])
+def test_cut_off_of_more_rows(M, N, K, draw, formats, share):
+    gen = torch.Generator().manual_seed(5)
+    x, w = draw(M, K, gen), normal(N, K, gen) * (2.0 / K) ** 0.5
+    (a, sa), (b, sb) = plain.quantized(x, formats[0], 1), plain.quantized(w, formats[1], 128)
+    scales = sa.double()[:, None, :] * sb.double().repeat_interleave(128, 0)[None, :N]
+    want = (plain.values(a, sa, 1) @ plain.values(b, sb, 128).T).to(DEV)
+    cut = (cut_sums(a.double().to(DEV), b.double().to(DEV), formats) * scales.to(DEV)).sum(2)
+    got = nova.nova_f8_matmul(nova.nova_f8_pack(a.to(DEV), sa.to(DEV), 1), nova.nova_f8_pack(b.to(DEV), sb.to(DEV), 128), M, N, K, format_a=formats[0], format_b=formats[1], dtype=F16)
+    # Besides the cut-off there are binary32's roundings: some hundred, of random sign, of partial sums of a result's size, 2^-24 sqrt(200 / 3) of it.  They change the rounding
+    # to binary16, with steps of 2^-10 to 2^-11 of it, in 1e-3 of the results; of exact sums the cut-off changes 4 to 12 in a hundred.
+    assert (got != cut.to(F16)).double().mean().item() < 0.005
+    rounding = (want.to(F16).double() - want).square().mean().sqrt()
+    assert (cut - want).square().mean().sqrt() < share * rounding
+    # Squares of errors of n results scatter by less than 2 / sqrt(n) of their mean; six times that
+    total = (got.double() - want).square().mean().sqrt()
+    assert total < ((1 + share ** 2) * (1 + 12 / (M * N) ** 0.5)) ** 0.5 * rounding
+
+
+@pytest.mark.parametrize("quiet,left", [(0.25, 0.0), (0.5, 0.5), (0.75, 0.5), (1.25, 1.0), (1.5, 1.5)])
+def test_what_is_left_beside_a_loud_product(quiet, left):
+    """Of products beside one of 4096 whole multiples of 1/2 are left."""
+    M, N, K = 70, 40, 256
+    a, b = torch.where(torch.arange(K) % 8 == 3, 64.0, 1.0).repeat(M, 1), torch.where(torch.arange(K) % 8 == 3, 64.0 * (1 - 2 * (torch.arange(K) // 8 % 2)), quiet).repeat(N, 1)
+    operands = [nova.nova_f8_pack(v.to(torch.float8_e4m3fn).to(DEV), torch.ones((len(v), K // 128), device=DEV), 1) for v in (a, b)]
+    for dtype, each in ((F16, left), (BF16, left), (F32, quiet)):
+        assert bool((nova.nova_f8_matmul(*operands, M, N, K, block_b=1, dtype=dtype) == each * (K // 8 * 7)).all())
