@@ -99,7 +99,8 @@ class TrainedHead:
             hidden = i < 2
             L = dict(N=N, K=K, weight=he_normal(gen, N, K).float(), master_bias=torch.zeros(N, device=DEV), bias=torch.zeros(N, **half), hidden=hidden,
                      forward=torch.empty(nova.nova_f8_bytes(N, K, 128), dtype=torch.uint8, device=DEV),
-                     backward=torch.empty(nova.nova_f8_bytes(K, N, 128), dtype=torch.uint8, device=DEV),
+                     # (the first layer's input takes no gradient)
+                     backward=torch.empty(nova.nova_f8_bytes(K, N, 128), dtype=torch.uint8, device=DEV) if i else None,
                      y=torch.empty((batch, N), **half), kept=torch.empty((batch, N), **half) if hidden else None, dy=torch.empty((batch, N), **half) if hidden else None,
                      dx=torch.empty((batch, K), **half) if i else None, dw=torch.empty((N, K), device=DEV), dbias=torch.empty(N, device=DEV),
                      workspace=torch.empty(max(nova.nova_f8_linear_workspace_bytes(batch, N, K, torch.float16),
@@ -111,7 +112,8 @@ class TrainedHead:
 
     def lay_out(self, L):
         nova.nova_f8_quantize(L["weight"], 128, Xq=L["forward"])
-        nova.nova_f8_quantize(L["weight"], 128, transposed=True, Xq=L["backward"])
+        if L["backward"] is not None:
+            nova.nova_f8_quantize(L["weight"], 128, transposed=True, Xq=L["backward"])
 
     def logits(self, x):
         for i, L in enumerate(self.layers):
@@ -126,8 +128,7 @@ class TrainedHead:
         for i, L in reversed(list(enumerate(self.layers))):
             if L["hidden"]:
                 d = nova.nova_dropout_backward(d, self.p, self.seed + i, device_offset=self.step, dx=L["dy"])
-            # (the first layer's input takes no gradient)
-            d, _, _ = nova.nova_f8_linear_backward(d, L["backward"] if i else None, L["x"], y=L["y"] if L["hidden"] else None, dx=L["dx"], dw=L["dw"], dbias=L["dbias"],
+            d, _, _ = nova.nova_f8_linear_backward(d, L["backward"], L["x"], y=L["y"] if L["hidden"] else None, dx=L["dx"], dw=L["dw"], dbias=L["dbias"],
                                                    workspace=L["workspace"])
 
     def update(self):
