@@ -168,7 +168,7 @@ def main(argv=None):
     ap.add_argument("--points", default="nova")
     ap.add_argument("--group", type=int, default=128, choices=(32, 64, 128))
     ap.add_argument("--reps", type=int, default=10)
-    ap.add_argument("--train", type=int, default=0, help="steps of training the fully connected layers")
+    ap.add_argument("--train", type=int, default=0, help="steps of training the fully connected layers; all but the first are timed")
     args = ap.parse_args(argv)
     gen = torch.Generator(device=DEV).manual_seed(16)
     images = torch.randn((args.batch, 3, args.size, args.size), device=DEV, generator=gen).half()
@@ -193,15 +193,15 @@ def main(argv=None):
     training, trained = None, None
     if args.train:
         trained = TrainedHead(gen, args.batch, stack.features)
-        start = torch.cuda.Event(enable_timing=True)
-        end = torch.cuda.Event(enable_timing=True)
-        losses = [-trained.train(features, labels, g).logprob.mean()]                    # (the first step alone: allocations, launches for the first time)
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        logprobs = [trained.train(features, labels, g).logprob]                          # (the first step alone: allocations, launches for the first time)
         start.record()
         for _ in range(args.train - 1):
-            losses.append(-trained.train(features, labels, g).logprob.mean())
+            logprobs.append(trained.train(features, labels, g).logprob)
         end.record()
         torch.cuda.synchronize()
-        training = dict(steps=args.train, ms_per_step=round(start.elapsed_time(end) / max(args.train - 1, 1), 4), losses=[round(v.item(), 4) for v in losses])
+        training = dict(steps=args.train, ms_per_step=round(start.elapsed_time(end) / (args.train - 1), 4) if args.train > 1 else None,
+                        losses=[round(-v.mean().item(), 4) for v in logprobs])
     print(json.dumps({
         "workload": f"VGG-16, batch {args.batch}, {args.size}x{args.size}, F({args.m},3), {args.points} points, fp16; fully connected layers in 4 bits, groups of {args.group}",
         "ms": times, "entropy": round(answers.entropy.mean().item(), 4), "log_probability": round(answers.logprob.mean().item(), 4),
