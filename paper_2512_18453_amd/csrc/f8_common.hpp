@@ -1,5 +1,6 @@
 // Device-side pieces shared by the kernels of matrices in 8-bit floating point.
 #pragma once
+#include "f8_quotient.hpp"
 #include "q4_common.hpp"
 
 namespace nova {
@@ -86,38 +87,24 @@ __device__ __forceinline__ float scale_of(unsigned bits)
 }
 
 // Codes of quotients by one scale as nova.h defines them: divided in binary32, kept within the largest code (a scale that is subnormal can be too small by half); 0 for
-// scales of 0 and NaN.  With the scale's inverse r, rounded, and a first quotient q = v r, q + (v - q s) r is v / s rounded once: compared with the division for every
-// significand of s and all v next to a border between codes, and half a billion random pairs.  Values and scale are moved by a power of two first where something on the way could
-// be subnormal that matters.  Six instructions, none of them a branch, where a division is ten.
+// scales of 0 and NaN.
 template <int FORMAT>
-struct F8Encoder {
-    float scale, inverse, factor;
-    __device__ __forceinline__ explicit F8Encoder(float s)
-    {
-        factor = s < 0x1p-60f ? 0x1p100f : s > 0x1p100f ? 0x1p-100f : 1.0f;
-        scale = s * factor;
-        inverse = 1.0f / scale;
-    }
-    __device__ __forceinline__ float quotient(float v) const
-    {
-        constexpr float L = kLargestCode<FORMAT>;
-        const float moved = v * factor, q = moved * inverse;
-        const float exact = __builtin_copysignf(fma32(fma32(-q, scale, moved), inverse, q), v);          // (a remainder of 0 makes -0 to 0)
-        return __builtin_amdgcn_fmed3f(exact, -L, L);
-    }
+struct F8Encoder : F8Divisor<float> {
+    __device__ __forceinline__ explicit F8Encoder(float s) : F8Divisor<float>(s) {}
+    __device__ __forceinline__ float kept(float v) const { return __builtin_amdgcn_fmed3f(quotient(v), -kLargestCode<FORMAT>, kLargestCode<FORMAT>); }
     // eight codes, in two words
     __device__ __forceinline__ void encode(const float (&v)[8], unsigned (&words)[2]) const
     {
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            const unsigned codes = f8_codes<FORMAT>(quotient(v[4 * w]), quotient(v[4 * w + 1]), quotient(v[4 * w + 2]), quotient(v[4 * w + 3]));
+            const unsigned codes = f8_codes<FORMAT>(kept(v[4 * w]), kept(v[4 * w + 1]), kept(v[4 * w + 2]), kept(v[4 * w + 3]));
             words[w] = scale > 0.0f ? codes : 0;
         }
     }
     // two, in 16 bits
     __device__ __forceinline__ void encode(const float (&v)[2], uint16_t &half) const
     {
-        const unsigned codes = f8_codes<FORMAT>(quotient(v[0]), quotient(v[1]), 0.0f, 0.0f);
+        const unsigned codes = f8_codes<FORMAT>(kept(v[0]), kept(v[1]), 0.0f, 0.0f);
         half = scale > 0.0f ? (uint16_t)codes : 0;
     }
 };
