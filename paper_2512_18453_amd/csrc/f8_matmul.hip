@@ -98,8 +98,8 @@ constexpr int kLaidOut = -1;
 struct F8RowsOf { const void *x; int64_t ld; int K; };           // what A is quantised from
 
 // Whether it saves more than it costs: every workgroup does the same, and LDS holds no more than 32768 elements.  Up to four rows it does (in us, with a launch of its own
-// first and without: 1 row by 32768 x 4096 33.6, 29.2; 1 by 25088 x 4096 25.4, 22.6; 4 by 4096 x 16384 20.9, 19.9); more rows save less of what is loaded of A (a panel has 16),
-// and then the workgroups' elements count: 8 by 2048 x 4096 10.3, 7.9; 6 by 4096 x 4096 10.3, 10.1; 7 10.4, 10.8; 16 by 2048 x 4096 9.8, 10.6; 8 by 2048 x 16384 14.8, 17.1.
+// first and without: 1 row by 32768 x 4096 32.6, 29.4; 1 by 25088 x 4096 25.7, 22.4; 4 by 4096 x 16384 21.3, 20.3); more rows save less of what is loaded of A (a panel has 16),
+// and then the workgroups' elements count: 8 by 2048 x 4096 10.3, 7.9; 6 by 4096 x 4096 10.5, 10.0; 7 10.5, 10.7; 16 by 2048 x 4096 10.5, 10.5; 8 by 2048 x 16384 15.2, 16.9.
 static bool quantised_on_the_way(int M, int N, const F8Shape &p)
 {
     const size_t elements = (size_t)M * p.split_chunks * kF8Chunk, workgroups = (size_t)ceil_div(N, 16) * p.splits;
@@ -413,9 +413,9 @@ static F8Shape f8_shape(int M, int N, int K, bool full)
     p.splits = 1;
     if (M <= 64) {
         p.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-        // More than 16 rows and 32 MB of weights: two panels of columns share the rows that a wave loads (32 rows by 25088 x 4096 32.8 -> 29.9 us, 64 by 4096 x 25088
-        // 47 -> 40; 32 by 4096 x 4096, where workgroups count for more, 11.0 -> 12.1).  Fewer workgroups than compute units, of long sums, are cut.  A workgroup is
-        // four waves (1 row by 4096 x 25088 19.5 us, with eight 21.0), eight where it has a compute unit for itself (1 by 25088 x 4096 22.1, with four 24.1).
+        // More than 16 rows and 32 MB of weights: two panels of columns share the rows that a wave loads (32 rows by 25088 x 4096 32.8 -> 30.1 us, 64 by 4096 x 25088
+        // 48 -> 39.5; 32 by 4096 x 4096, where workgroups count for more, 11.2 -> 12.3).  Fewer workgroups than compute units, of long sums, are cut.  A workgroup is
+        // four waves (1 row by 4096 x 25088 20.2 us, with eight 21.8), eight where it has a compute unit for itself (1 by 25088 x 4096 22.4, with four 24.3).
         const int64_t panels = (N + 15) / 16;
         p.nt = p.mt > 1 && panels * chunks >= 16384 ? 2 : 1;
         const int64_t groups = (panels + p.nt - 1) / p.nt;
@@ -425,7 +425,7 @@ static F8Shape f8_shape(int M, int N, int K, bool full)
     } else {
         // An estimate in us of each way.  128 x 128: one or two workgroups per compute unit, so a chunk of one or both; 256 x 256: one.  (From 1024 x 4096 x 4096 and
         // 8192 x 8192 x 8192, with 128 columns of B per scale.)  A cut sum's pieces are written and read, and another kernel joins them.  On 45 drawn calls of 65 to 4096 rows the
-        // way and cut that it chooses took 1.014 times as long as the best of up to 16 tried, on the average; on the 45 it was fitted with, 1.03.
+        // way and cut that it chooses took 1.016 times as long as the best of up to 16 tried, on the average, 1.13 at the most.
         double least = 0;
         for (int kind = 1; kind <= (full ? 1 : 2); ++kind)
             for (int splits = 1; splits <= 16 && splits <= chunks; ++splits) {
