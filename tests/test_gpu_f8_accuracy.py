@@ -109,3 +109,22 @@ def test_what_is_left_beside_a_loud_product(quiet, left):
     operands = [nova.nova_f8_pack(v.to(torch.float8_e4m3fn).to(DEV), torch.ones((len(v), K // 128), device=DEV), 1) for v in (a, b)]
     for dtype, each in ((F16, left), (BF16, left), (F32, quiet)):
         assert bool((nova.nova_f8_matmul(*operands, M, N, K, block_b=1, dtype=dtype) == each * (K // 8 * 7)).all())
+
+
+@pytest.mark.parametrize("formats", [(0, 0), (0, 1), (1, 0), (1, 1)])
+def test_every_product_of_two_codes(formats):
+    """One product per sum: exact in bfloat16's and binary32's bits, subnormal codes included; an infinite or NaN code makes what it should."""
+    every = [torch.arange(256, dtype=torch.uint8).view(plain.FORMATS[f]) for f in formats]
+    values = [v.double() for v in every]
+    want = values[0][:, None] * values[1][None, :]
+    one = torch.ones((256, 1), device=DEV)
+    A, B = (torch.zeros((256, 128), dtype=torch.uint8) for _ in range(2))
+    A[:, 77], B[:, 77] = every[0].view(torch.uint8), every[1].view(torch.uint8)
+    # elsewhere zero times zero; beside an infinity or NaN nothing else is multiplied
+    Bq = nova.nova_f8_pack(B.to(DEV), one, 1)
+    for rows in (1, 16, 32, 64, 256):
+        for first in range(0, 256, rows) if rows > 1 else (1, 130):
+            Aq = nova.nova_f8_pack(A[first:first + rows].to(DEV), one[:rows], 1)
+            for dtype in (F32, BF16):
+                got = nova.nova_f8_matmul(Aq, Bq, rows, 256, 128, block_b=1, format_a=formats[0], format_b=formats[1], dtype=dtype)
+                torch.testing.assert_close(got.cpu().double(), want[first:first + rows], rtol=0, atol=0, equal_nan=True)
